@@ -1,5 +1,6 @@
 """Thin ctypes binding of the C ABI in include/wq.h, include/wq_attention.h,
-include/wq_fused.h and include/wq_probe.h.
+include/wq_fused.h, include/wq_cache.h, include/wq_window.h,
+include/wq_logits.h and include/wq_probe.h.
 
 Only argument marshalling happens here: torch tensors are turned into device
 pointers and sizes, the current HIP stream is passed through, and non-OK
@@ -29,7 +30,9 @@ GROUP = 32
 # Every function declared in the headers under include/.
 EXPORTED = ("wq_status_string", "wq_last_error_message", "wq_version", "wq_pack", "wq_gemv",
             "wq_decode_linears", "wq_decode_linears_noalloc", "wq_paged_attention_workspace_size",
-            "wq_paged_attention", "wq_fused_linears", "wq_fused_check", "wq_stream_read")
+            "wq_paged_attention", "wq_fused_linears", "wq_fused_check", "wq_stream_read",
+            "wq_cache_append", "wq_cache_copy_pages", "wq_page_workspace_size", "wq_cache_reserve", "wq_cache_free",
+            "wq_cache_fork", "wq_cache_compact")
 
 # Limits of wq_decode_linears_noalloc (include/wq.h).
 NOALLOC_MAX_LINEARS = 1024
@@ -110,6 +113,17 @@ def lib() -> ctypes.CDLL:
     L.wq_fused_check.restype = ctypes.c_int
     L.wq_stream_read.argtypes = [vp, i64, vp, vp]
     L.wq_stream_read.restype = ctypes.c_int
+    sz = ctypes.c_size_t
+    for name, args in (
+            ("wq_cache_append", [vp] * 7 + [i64] * 9 + [vp]),
+            ("wq_cache_copy_pages", [vp, i64, i64, i64, vp, vp, i64, vp]),
+            ("wq_page_workspace_size", [i64, i64, ctypes.POINTER(sz)]),
+            ("wq_cache_reserve", [vp] * 4 + [i64] * 4 + [vp, vp, sz, vp]),
+            ("wq_cache_free", [vp] * 4 + [i64] * 7 + [vp]),
+            ("wq_cache_fork", [vp, i64] + [vp] * 5 + [i64] * 7 + [vp, vp, sz, vp]),
+            ("wq_cache_compact", [vp, i64, i64] + [vp] * 5 + [i64] * 3 + [vp, sz, vp])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
 
@@ -348,6 +362,183 @@ def wq_fused_check(device=None, stream=None) -> None:
 
     stream = torch.cuda.current_stream(device) if stream is None else stream
     _check(lib().wq_fused_check(stream.cuda_stream))
+
+
+# ------------------------------------------------------- paged cache upkeep
+
+def _rows_tensor(t, name, dtype, shape, align=8):
+    """Address and row stride of `t` [rows, heads, dim], whose rows may lie
+    apart (a slice of a wider array) but are contiguous in themselves."""
+    if not isinstance(t, _torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    stride, head, one = t.stride()
+    if t.shape[0] == 1:
+        stride = (t.shape[1] * t.shape[2] + align - 1) // align * align
+    if (one != 1 and t.shape[2] > 1) or (head != t.shape[2] and t.shape[1] > 1):
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), stride
+
+
+def _workspace(workspace, t):
+    if workspace is None:
+        return None, 0
+    if workspace.device != t.device or workspace.dtype not in _BYTES or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the device of the other arguments")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def _cache_dims(cache, name):
+    if cache.dim() != 4:
+        raise ValueError(f"{name} must be [pages, HKV, P, D]")
+    if cache.element_size() != 2:
+        raise TypeError(f"{name} must hold 16-bit values (got {cache.dtype})")
+    return cache.shape
+
+
+def cache_append(k, v, k_cache, v_cache, block_table, seq_lens, q_starts=None, stream=None) -> None:
+    """Write the keys k and values v [T, HKV, D] of new tokens to their slots in
+    the paged caches [pages, HKV, P, D] (the caches' 16-bit type).  seq_lens
+    [S] counts the new tokens; rows q_starts[s] to q_starts[s + 1] (int32,
+    [S + 1]) are the last tokens of sequence s, or row s its last one when
+    q_starts is None.  Rows of k and v may lie apart (slices of the QKV
+    projection's output)."""
+    _torch or _load_torch()
+    num_pages, hkv, page, d = _cache_dims(k_cache, "k_cache")
+    kind = k_cache.dtype
+    if block_table.dim() != 2 or k.dim() != 3:
+        raise ValueError("k must be [T, HKV, D] and block_table [S, max_pages]")
+    num_seqs, max_pages = block_table.shape
+    shape = (k.shape[0], hkv, d)
+    pk, ks = _rows_tensor(k, "k", kind, shape)
+    pv, vs = _rows_tensor(v, "v", kind, shape)
+    pkc = _dev_tensor(k_cache, "k_cache", (kind,), k_cache.shape)
+    pvc = _dev_tensor(v_cache, "v_cache", (kind,), k_cache.shape)
+    pt = _dev_tensor(block_table, "block_table", _INTS, (num_seqs, max_pages))
+    pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
+    ps = None if q_starts is None else _dev_tensor(q_starts, "q_starts", _INTS, (num_seqs + 1,))
+    if shape[0] == 0:
+        return
+    _check((_lib or lib()).wq_cache_append(pk, pv, pkc, pvc, pt, pl, ps, num_seqs, shape[0], hkv, d, ks, vs, page, num_pages,
+                                           max_pages, _stream(stream, k_cache)))
+
+
+class CacheSet:
+    """The caches of all layers, marshalled once: tensors [pages, HKV, P, D] of
+    one shape and 16-bit type on one device.  Keeps the tensors alive."""
+
+    def __init__(self, caches):
+        _torch or _load_torch()
+        caches = list(caches)
+        if not caches:
+            raise ValueError("a cache set needs at least one cache")
+        first = caches[0]
+        self.num_pages, self.kv_heads, self.page, self.head_dim = _cache_dims(first, "caches[0]")
+        self.array = (ctypes.c_void_p * len(caches))(
+            *[_dev_tensor(c, f"caches[{i}]", (first.dtype,), first.shape) for i, c in enumerate(caches)])
+        if any(c.device != first.device for c in caches):
+            raise ValueError("the caches must be on one device")
+        self.caches = caches
+        self.page_bytes = 2 * self.kv_heads * self.page * self.head_dim
+
+
+def cache_set(caches) -> CacheSet:
+    return CacheSet(caches)
+
+
+def page_workspace_size(num_pages: int, num_seqs: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().wq_page_workspace_size(num_pages, num_seqs, ctypes.byref(out)))
+    return int(out.value)
+
+
+def page_workspace(num_pages: int, num_seqs: int, device="cuda"):
+    """A device workspace for cache_reserve, cache_fork and cache_compact."""
+    import torch
+
+    return torch.empty(page_workspace_size(num_pages, num_seqs), dtype=torch.uint8, device=device)
+
+
+def cache_copy_pages(caches: CacheSet, src, dst, stream=None) -> None:
+    """Copy page src[i] to page dst[i] (int32 [n]) in every cache of the set."""
+    n = src.shape[0] if src.dim() == 1 else -1
+    ps = _dev_tensor(src, "src", _INTS, (n,))
+    pd = _dev_tensor(dst, "dst", _INTS, (n,))
+    _check((_lib or lib()).wq_cache_copy_pages(caches.array, len(caches.array), caches.page_bytes, caches.num_pages, ps, pd, n,
+                                               _stream(stream, caches.caches[0])))
+
+
+def _pool(block_table, refs):
+    _torch or _load_torch()
+    if block_table.dim() != 2 or refs.dim() != 1:
+        raise ValueError("block_table must be [S, max_pages] and refs [pages]")
+    return (_dev_tensor(block_table, "block_table", _INTS, block_table.shape), _dev_tensor(refs, "refs", _INTS, refs.shape),
+            block_table.shape[0], block_table.shape[1], refs.shape[0])
+
+
+def cache_reserve(block_table, refs, old_lens, new_lens, page_size: int, shortfall, workspace=None, stream=None) -> None:
+    """Give sequences that grow from old_lens to new_lens (int32 [S]) the pages
+    they lack, lowest free page first.  shortfall (int32 [1]) becomes 0, or the
+    number of pages too few, and then nothing else changes."""
+    pt, pr, num_seqs, max_pages, num_pages = _pool(block_table, refs)
+    po = _dev_tensor(old_lens, "old_lens", _INTS, (num_seqs,))
+    pn = _dev_tensor(new_lens, "new_lens", _INTS, (num_seqs,))
+    pf = _dev_tensor(shortfall, "shortfall", _INTS, (1,))
+    if workspace is None:
+        workspace = page_workspace(num_pages, num_seqs, refs.device)
+    pw, nw = _workspace(workspace, refs)
+    _check((_lib or lib()).wq_cache_reserve(pt, pr, po, pn, num_seqs, page_size, num_pages, max_pages, pf, pw, nw, _stream(stream, refs)))
+
+
+def cache_free(block_table, refs, seq_lens, seqs, page_size: int, window: int = 0, sinks: int = 0, stream=None) -> None:
+    """Take from the sequences listed in seqs (int32 [n]) the pages that hold
+    neither one of the first `sinks` tokens nor one that the next token sees
+    through a window of `window` tokens; all pages when both are 0."""
+    pt, pr, num_seqs, max_pages, num_pages = _pool(block_table, refs)
+    pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
+    n = seqs.shape[0] if seqs.dim() == 1 else -1
+    ps = _dev_tensor(seqs, "seqs", _INTS, (n,))
+    _check((_lib or lib()).wq_cache_free(pt, pr, pl, ps, n, window, sinks, num_seqs, page_size, num_pages, max_pages, _stream(stream, refs)))
+
+
+def cache_fork(caches: CacheSet, block_table, refs, seq_lens, src, dst, shortfall, workspace=None, stream=None) -> None:
+    """Make sequence dst[i] a copy of sequence src[i] (int32 [n]): full pages are
+    shared, a partly filled last page is copied in every cache."""
+    pt, pr, num_seqs, max_pages, num_pages = _pool(block_table, refs)
+    if num_pages != caches.num_pages:
+        raise ValueError(f"refs has {num_pages} pages, the caches {caches.num_pages}")
+    pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
+    n = src.shape[0] if src.dim() == 1 else -1
+    ps = _dev_tensor(src, "src", _INTS, (n,))
+    pd = _dev_tensor(dst, "dst", _INTS, (n,))
+    pf = _dev_tensor(shortfall, "shortfall", _INTS, (1,))
+    if workspace is None:
+        workspace = page_workspace(num_pages, num_seqs, refs.device)
+    pw, nw = _workspace(workspace, refs)
+    _check((_lib or lib()).wq_cache_fork(caches.array, len(caches.array), pt, pr, pl, ps, pd, n, num_seqs, caches.kv_heads, caches.head_dim,
+                                         caches.page, num_pages, max_pages, pf, pw, nw, _stream(stream, refs)))
+
+
+def cache_compact(caches: CacheSet, block_table, refs, new_table, new_refs, live, workspace=None, stream=None) -> None:
+    """Move the pages in use to the numbers below their count, which live (int32
+    [1]) receives; new_table and new_refs (which may be block_table and refs)
+    receive the table and the counts with the new numbers."""
+    pt, pr, num_seqs, max_pages, num_pages = _pool(block_table, refs)
+    if num_pages != caches.num_pages:
+        raise ValueError(f"refs has {num_pages} pages, the caches {caches.num_pages}")
+    pnt = _dev_tensor(new_table, "new_table", _INTS, block_table.shape)
+    pnr = _dev_tensor(new_refs, "new_refs", _INTS, refs.shape)
+    pl = _dev_tensor(live, "live", _INTS, (1,))
+    if workspace is None:
+        workspace = page_workspace(num_pages, num_seqs, refs.device)
+    pw, nw = _workspace(workspace, refs)
+    _check((_lib or lib()).wq_cache_compact(caches.array, len(caches.array), caches.page_bytes, pt, pr, pnt, pnr, pl, num_seqs, num_pages,
+                                            max_pages, pw, nw, _stream(stream, refs)))
 
 
 # ------------------------------------------------------- measurement probe

@@ -1,0 +1,337 @@
+"""GPU tests of the paged cache's upkeep: every table, count and cached value
+equals the entry-by-entry model (all results are integers or copies, so they
+are compared bit for bit)."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import cache_model
+from gpu_util import announce, require_gpu
+
+pytestmark = pytest.mark.gpu
+
+HALVES = ("float16", "bfloat16")
+
+
+def dev(a):
+    import torch
+
+    return torch.from_numpy(np.ascontiguousarray(np.asarray(a, dtype=np.int32))).cuda()
+
+
+def halves(rng, shape):
+    """Random 16-bit patterns, NaNs and infinities among them."""
+    return rng.integers(0, 1 << 16, size=shape, dtype=np.uint16)
+
+
+def to_gpu(a, dtype="float16"):
+    import torch
+
+    return torch.from_numpy(a.view(np.int16).copy()).cuda().view(getattr(torch, dtype))
+
+
+def bits(t):
+    import torch
+
+    return t.view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def random_pool(rng, seqs, width, pages, fill):
+    """Tables in which about `fill` of the entries hold a page of their own."""
+    order = list(rng.permutation(pages))
+    table = [[-1] * width for _ in range(seqs)]
+    refs = [0] * pages
+    for s in range(seqs):
+        for e in range(width):
+            if order and rng.random() < fill:
+                p = int(order.pop())
+                table[s][e] = p
+                refs[p] = 1
+    return table, refs
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("heads,dim,page,news", [
+    (1, 8, 1, [1, 1, 1]), (8, 128, 16, [1] * 40), (3, 64, 8, [0, 5, 0, 0, 17, 1, 0]), (2, 40, 32, [100, 1, 63, 0]),
+    (4, 128, 16, [3000, 2, 1500]), (1, 1024, 4, [7, 9]), (2, 64, 16, [0] * 70 + [33] + [0] * 70 + [5]),
+])
+def test_append(dtype, heads, dim, page, news):
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    announce(f"append {dtype} heads={heads} dim={dim} page={page} news={len(news)}")
+    rng = np.random.default_rng(sum(news) + dim)
+    lens = [n + int(rng.integers(0, 3 * page)) for n in news]
+    width = max(cache_model.pages_of(n, page) for n in lens) + 1
+    pages = sum(cache_model.pages_of(n, page) for n in lens) + 3
+    order = [int(p) for p in rng.permutation(pages)]
+    table = [[order.pop() if e < cache_model.pages_of(n, page) else -1 for e in range(width)] for n in lens]
+    total = sum(news)
+    # The rows lie in a wider array, as in a projection's output.
+    wide = halves(rng, (total, heads + 3, dim + 0))
+    wide2 = halves(rng, (total, 2 * heads + 1, dim))
+    kc, vc = halves(rng, (pages, heads, page, dim)), halves(rng, (pages, heads, page, dim))
+    starts = None if all(n == 1 for n in news) else np.concatenate([[0], np.cumsum(news)])
+    gk, gv = to_gpu(kc, dtype), to_gpu(vc, dtype)
+    k, v = to_gpu(wide, dtype)[:, 1:1 + heads], to_gpu(wide2, dtype)[:, heads:2 * heads]
+    wq.cache_append(k, v, gk, gv, dev(table), dev(lens), q_starts=None if starts is None else dev(starts))
+    cache_model.append(wide[:, 1:1 + heads], wide2[:, heads:2 * heads], kc, vc, table, lens, starts, page)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(gk), kc) and np.array_equal(bits(gv), vc)
+
+
+def test_append_skips_what_has_no_place():
+    """Lengths below the new tokens, beyond the row, missing and wrong pages: nothing else is written."""
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    rng = np.random.default_rng(5)
+    page, pages, heads, dim = 4, 6, 2, 16
+    table = [[0, 1], [2, -1], [7, 3], [-5, 4], [5, 5]]
+    lens, starts = [1, 7, 8, 8, 40], [2, 5, 8, 11, 12, 16]
+    total = 20  # rows before the first and after the last sequence's
+    k, v = halves(rng, (total, heads, dim)), halves(rng, (total, heads, dim))
+    kc, vc = halves(rng, (pages, heads, page, dim)), halves(rng, (pages, heads, page, dim))
+    gk, gv = to_gpu(kc), to_gpu(vc)
+    wq.cache_append(to_gpu(k), to_gpu(v), gk, gv, dev(table), dev(lens), q_starts=dev(starts))
+    cache_model.append(k, v, kc, vc, table, lens, starts, page)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(gk), kc) and np.array_equal(bits(gv), vc)
+
+
+def test_append_and_copy_beyond_32_bit_offsets():
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    heads, dim, page = 8, 128, 16
+    pages = (5 << 30) // (heads * dim * page * 2)
+    k = torch.zeros((pages, heads, page, dim), dtype=torch.float16, device="cuda")
+    v = torch.zeros_like(k)
+    rows = torch.randn((2, heads, dim), device="cuda").half()
+    table = dev([[0, pages - 1]])
+    wq.cache_append(rows, -rows, k, v, table, dev([page + 3]), q_starts=dev([0, 2]))
+    assert torch.equal(k[pages - 1, :, 1:3], rows.transpose(0, 1)) and torch.equal(v[pages - 1, :, 1:3], -rows.transpose(0, 1))
+    wq.cache_copy_pages(wq.cache_set([k, v]), dev([pages - 1]), dev([pages - 2]))
+    assert torch.equal(k[pages - 2], k[pages - 1]) and torch.equal(v[pages - 2], v[pages - 1])
+    assert int(torch.count_nonzero(k)) == 2 * int(torch.count_nonzero(rows))
+
+
+@pytest.mark.parametrize("pages,heads,dim,page,arrays,count", [(9, 1, 8, 1, 1, 4), (50, 3, 64, 8, 5, 25), (300, 8, 128, 16, 7, 111), (20, 2, 128, 256, 256, 3), (5, 1, 8, 1, 2, 0)])
+def test_copy_pages(pages, heads, dim, page, arrays, count):
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    rng = np.random.default_rng(pages)
+    caches = [halves(rng, (pages, heads, page, dim)) for _ in range(arrays)]
+    order = rng.permutation(pages)
+    src, dst = order[:count].copy(), order[count:2 * count].copy()
+    if count > 3:
+        src[1], dst[2] = -1, pages  # skipped
+    g = [to_gpu(c) for c in caches]
+    wq.cache_copy_pages(wq.cache_set(g), dev(src), dev(dst))
+    for a, b in zip(src, dst):
+        if 0 <= a < pages and 0 <= b < pages:
+            for c in caches:
+                c[b] = c[a]
+    assert all(np.array_equal(bits(t), c) for t, c in zip(g, caches))
+
+
+@pytest.mark.parametrize("seqs,width,pages,page,fill", [
+    (1, 1, 1, 16, 0.0), (1, 1, 1, 16, 1.0), (5, 7, 40, 4, 0.5), (64, 70, 4097, 16, 0.3), (300, 33, 2048, 8, 0.1),
+    (3, 1500, 6000, 16, 0.2), (40, 20, 500000, 16, 0.5), (1000, 12, 9000, 1, 0.4),
+])
+def test_reserve(seqs, width, pages, page, fill):
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    announce(f"reserve seqs={seqs} width={width} pages={pages}")
+    rng = np.random.default_rng(seqs + pages)
+    table, refs = random_pool(rng, seqs, width, pages, fill)
+    for p in rng.integers(0, pages, pages // 3):  # pages held by other tables
+        refs[p] = max(refs[p], 1)
+    old = [int(rng.integers(-2, width * page + 1)) for _ in range(seqs)]
+    new = [int(rng.integers(-2, width * page + 2 * page)) for _ in range(seqs)]
+    for attempt in range(2):
+        gt, gr, gs = dev(table), dev(refs), dev([77])
+        wq.cache_reserve(gt, gr, dev(old), dev(new), page, gs)
+        t, r = [row[:] for row in table], refs[:]
+        short = cache_model.reserve(t, r, old, new, page)
+        assert gs.item() == short
+        assert gt.tolist() == t and gr.tolist() == r
+        if attempt == 0:  # again with too few free pages (or none wanted)
+            refs = [1] * (pages - 1) + [0]
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (0, 5), (1, 0), (7, 0), (16, 4), (50, 17), (1 << 30, 0), (33, 1 << 30)])
+@pytest.mark.parametrize("page", [1, 8, 16])
+def test_free(window, sinks, page):
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    rng = np.random.default_rng(window % 1000 + sinks % 1000 + page)
+    seqs, width = 9, 300 // page + 2
+    pages = seqs * width
+    table, refs = random_pool(rng, seqs, width, pages, 0.8)
+    table[1][1] = table[0][0]  # a shared page, and an entry that names none
+    if table[0][0] >= 0:
+        refs[table[0][0]] += 1
+    table[3][0] = pages + 5
+    lens = [int(rng.integers(0, width * page + 1)) for _ in range(seqs)]
+    listed = [0, 1, 3, 7, 8, -1, seqs]
+    gt, gr = dev(table), dev(refs)
+    wq.cache_free(gt, gr, dev(lens), dev(listed), page, window=window, sinks=sinks)
+    cache_model.free(table, refs, lens, listed, page, min(window, 1 << 12), min(sinks, 1 << 12))
+    assert gt.tolist() == table and gr.tolist() == refs
+
+
+def test_free_of_a_sequence_listed_twice():
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    gt, gr = dev([[0, 2, -1]]), dev([1, 3, 2])
+    wq.cache_free(gt, gr, dev([9]), dev([0]).expand(1).contiguous(), 4)
+    assert gt.tolist() == [[-1, -1, -1]] and gr.tolist() == [0, 3, 1]
+    gt, gr = dev([[0, 2, -1], [1, -1, -1]]), dev([1, 1, 2])
+    wq.cache_free(gt, gr, dev([9, 2]), dev([0, 0]), 4)
+    assert gt.tolist() == [[-1, -1, -1], [1, -1, -1]] and gr.tolist() == [0, 1, 1]
+
+
+@pytest.mark.parametrize("seqs,beams,page,heads,dim,arrays,top", [(1, 2, 16, 1, 8, 1, 40), (12, 4, 16, 8, 128, 6, 300), (5, 3, 1, 2, 64, 4, 9), (70, 6, 8, 1, 64, 2, 33), (2, 2, 64, 4, 128, 64, 500)])
+def test_fork(seqs, beams, page, heads, dim, arrays, top):
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    announce(f"fork seqs={seqs} beams={beams} page={page}")
+    rng = np.random.default_rng(seqs * beams + page)
+    lens = [int(rng.integers(0, top)) for _ in range(seqs)]
+    lens[0] = page * max(1, top // page // 2)  # no part page
+    width = cache_model.pages_of(top, page) + 1
+    pages = sum(cache_model.pages_of(n, page) for n in lens) + seqs * beams + 3
+    table, refs, order = [], [0] * pages, list(rng.permutation(pages))
+    for n in lens:
+        row = [int(order.pop()) if e < cache_model.pages_of(n, page) else -1 for e in range(width)]
+        for p in row:
+            if p >= 0:
+                refs[p] = 1
+        table.append(row)
+    if width > 3 and lens[-1] > 2 * page:
+        refs[table[-1][0]] -= 1  # its window has left the first page behind
+        table[-1][0] = -1
+    src = [s for s in range(seqs) for _ in range(beams - 1)]
+    dst = list(range(seqs, seqs * beams))
+    table += [[-1] * width for _ in dst]
+    lens += [0] * len(dst)
+    if seqs > 20:
+        src[3], dst[5] = -1, 1 << 20  # skipped
+        lens[7] = width * page + 1    # does not fit its row
+    caches = [halves(rng, (pages, heads, page, dim)) for _ in range(arrays)]
+    g = [to_gpu(c) for c in caches]
+    gt, gr, gl, gs = dev(table), dev(refs), dev(lens), dev([5])
+    wq.cache_fork(wq.cache_set(g), gt, gr, gl, dev(src), dev(dst), gs)
+    assert cache_model.fork(caches, table, refs, lens, src, dst, page) == 0
+    assert gs.item() == 0 and gt.tolist() == table and gr.tolist() == refs and gl.tolist() == lens
+    assert all(np.array_equal(bits(t), c) for t, c in zip(g, caches))
+
+
+def test_fork_without_enough_pages_changes_nothing():
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    rng = np.random.default_rng(3)
+    caches = [halves(rng, (4, 1, 4, 8))]
+    g = [to_gpu(c) for c in caches]
+    table, refs, lens = [[0, 1], [-1, -1], [-1, -1]], [1, 1, 0, 1], [6, 0, 0]
+    gt, gr, gl, gs = dev(table), dev(refs), dev(lens), dev([0])
+    wq.cache_fork(wq.cache_set(g), gt, gr, gl, dev([0, 0]), dev([1, 2]), gs)
+    assert gs.item() == 1 and gt.tolist() == table and gr.tolist() == refs and gl.tolist() == lens
+    assert np.array_equal(bits(g[0]), caches[0])
+    empty = dev([]).view(0)
+    gs.fill_(9)
+    wq.cache_fork(wq.cache_set(g), gt, gr, gl, empty, empty, gs)
+    assert gs.item() == 0 and gt.tolist() == table
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("pages,live,seqs,width", [(1, 0, 1, 1), (1, 1, 1, 1), (64, 64, 4, 16), (100, 37, 5, 12), (2048, 1100, 30, 40), (5000, 700, 9, 80), (6100, 6000, 60, 100), (150000, 70000, 300, 250)])
+def test_compact(pages, live, seqs, width, in_place):
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    announce(f"compact pages={pages} live={live}")
+    rng = np.random.default_rng(pages + live)
+    refs, table = [0] * pages, [[-1] * width for _ in range(seqs)]
+    for i, p in enumerate(rng.permutation(pages)[:live]):
+        refs[int(p)] = 1 + i % 3
+        table[i % seqs][i // seqs % width] = int(p)
+    heads, page, dim = (2, 4, 16) if pages < 10000 else (1, 1, 8)
+    caches = [halves(rng, (pages, heads, page, dim)) for _ in range(3)]
+    g = [to_gpu(c) for c in caches]
+    gt, gr, gl = dev(table), dev(refs), dev([-1])
+    nt, nr = (gt, gr) if in_place else (torch.full_like(gt, 7), torch.full_like(gr, 7))
+    wq.cache_compact(wq.cache_set(g), gt, gr, nt, nr, gl)
+    t, r, n = cache_model.compact(caches, table, refs)
+    assert gl.item() == n and nt.tolist() == t and nr.tolist() == r
+    assert all(np.array_equal(bits(a), c) for a, c in zip(g, caches))
+    if not in_place:
+        assert gt.tolist() == table and gr.tolist() == refs
+
+
+def test_upkeep_in_a_graph_and_on_another_stream():
+    """A decoding step's upkeep, captured, replayed and compared after every replay."""
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    rng = np.random.default_rng(11)
+    page, heads, dim, pages, width, window, sinks = 4, 2, 64, 64, 40, 12, 4
+    table, refs, lens = [[-1] * width for _ in range(3)], [0] * pages, [5, 0, 17]
+    assert cache_model.reserve(table, refs, [0, 0, 0], lens, page) == 0
+    kc, vc = halves(rng, (pages, heads, page, dim)), halves(rng, (pages, heads, page, dim))
+    rows = halves(rng, (3, heads, dim))
+    gt, gr, gl, gs = dev(table), dev(refs), dev(lens), dev([0])
+    gk, gv, gx = to_gpu(kc), to_gpu(vc), to_gpu(rows)
+    after, every, work = torch.empty_like(gl), dev([0, 1, 2]), wq.page_workspace(pages, 3)
+    one = torch.ones_like(gl)
+
+    def step():
+        torch.add(gl, one, out=after)
+        wq.cache_reserve(gt, gr, gl, after, page, gs, workspace=work)
+        wq.cache_append(gx, gx, gk, gv, gt, after)
+        wq.cache_free(gt, gr, after, every, page, window=window, sinks=sinks)
+        gl.copy_(after)
+
+    def model_step():
+        nonlocal lens
+        new = [n + 1 for n in lens]
+        assert cache_model.reserve(table, refs, lens, new, page) == 0
+        cache_model.append(rows, rows, kc, vc, table, new, None, page)
+        cache_model.free(table, refs, new, [0, 1, 2], page, window, sinks)
+        lens = new
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        model_step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for replay in range(40):
+            graph.replay()
+            model_step()
+            if replay % 5 == 0:
+                side.synchronize()
+            assert gt.tolist() == table and gr.tolist() == refs and gl.tolist() == lens, replay
+            assert np.array_equal(bits(gk), kc) and np.array_equal(bits(gv), vc)
+    torch.cuda.synchronize()
