@@ -1,0 +1,398 @@
+// From logits to the next token (gfx950, wave64): penalties for repeated words,
+// biases, a grammar's mask and the best word, in one pass over the logits.
+//
+// The logits are read once and written once, which is what bounds large
+// batches.  A workgroup takes a tile of one row's words.  What it has to know of
+// the row's history is how often each word of its tile occurs, so it scans the
+// history once (a few thousand words, from L2) into counters in LDS, adds the
+// positions of listed biases beside them, and then streams its tile: 16 bytes
+// per lane and load, whatever word the row starts at, as long as input and
+// output rows lie alike.  The best word of each tile goes to the workspace and
+// pick_kernel takes the best of a row's.  Integer LDS atomics are the only
+// ones, so results do not depend on the order they run in.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "wq_device.h"
+#include "wq_host.h"
+#include "wq_internal.h"
+#include "wq_logits.h"
+
+namespace wq {
+namespace logits {
+namespace {
+
+using dev::gbl;
+using dev::u32x4;
+using namespace host;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kPickThreads = 64;
+constexpr uint32_t kPrompt = 0x80000000u;  // the word occurs in the prompt; below it the times it was generated
+constexpr int kMinTile = 2048, kMaxTile = 8192;
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+
+struct Params {
+    wq_logits_call c;
+    float* best;         // [rows][tiles] largest value of each tile
+    int32_t* best_word;  // [rows][tiles], -1: none
+    int32_t tile, tiles;
+};
+
+template <typename T>
+struct Type;
+template <>
+struct Type<_Float16> {
+    static constexpr int kPer = 8;
+};
+template <>
+struct Type<__bf16> {
+    static constexpr int kPer = 8;
+};
+template <>
+struct Type<float> {
+    static constexpr int kPer = 4;
+};
+
+// The larger of two candidates; the lower word where they are equal, and none
+// (word -1) only where both are none.
+__device__ __forceinline__ void better(float& v, int& w, float v2, int w2) {
+    if (w2 >= 0 && (w < 0 || v2 > v || (v2 == v && w2 < w))) {
+        v = v2;
+        w = w2;
+    }
+}
+
+template <int kCount>
+__device__ __forceinline__ void best_of_wave(float& v, int& w) {
+#pragma unroll
+    for (int d = kCount / 2; d >= 1; d >>= 1) {
+        const float v2 = __shfl_xor(v, d);
+        const int w2 = __shfl_xor(w, d);
+        better(v, w, v2, w2);
+    }
+}
+
+struct Row {
+    float repetition, frequency, presence;
+    const float* bias;  // bias value of list position i
+};
+
+// A word's value.  `uses`: the counter of its history; `listed`: its position
+// in the bias list plus one, or 0.
+__device__ __forceinline__ float adjusted(float x, uint32_t uses, uint32_t listed, const Row& r) {
+#pragma clang fp contract(off)
+    if (uses) {
+        x = x > 0.0f ? x / r.repetition : x * r.repetition;
+        const uint32_t c = uses & ~kPrompt;
+        const float taken = r.frequency * (float)c;
+        x = x - taken;
+        if (c) x = x - r.presence;
+    }
+    if (listed) x = x + r.bias[listed - 1];
+    return x;
+}
+
+template <typename T, bool HISTORY, bool BIAS, bool VECTOR>
+__global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
+    extern __shared__ __align__(16) uint32_t smem[];
+    constexpr int kPer = Type<T>::kPer;
+    __shared__ float sh_v[kWaves];
+    __shared__ int sh_w[kWaves];
+    uint32_t* uses = smem;                                   // [tile + kPer] where HISTORY
+    uint32_t* listed = smem + (HISTORY ? p.tile + kPer : 0);  // [tile + kPer] where BIAS
+    const wq_logits_call& c = p.c;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.y;
+    const T* x = reinterpret_cast<const T*>(c.logits) + row * c.logits_stride;
+    T* y = reinterpret_cast<T*>(c.out) + row * c.out_stride;
+    const uint32_t* mask = c.mask ? c.mask + row * c.mask_stride : nullptr;
+    const int vocab = (int)c.vocab;
+
+    // Words before the row's first 16-byte boundary belong to the first tile.
+    const int head = VECTOR ? (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)) : 0;
+    const int begin = blockIdx.x == 0 ? 0 : min(vocab, head + (int)blockIdx.x * p.tile);
+    const int end = min(vocab, head + ((int)blockIdx.x + 1) * p.tile);
+    // The word of LDS entry 0.  With vectors, the first whole vector has entry
+    // kPer, so that a vector's counters are whole 16-byte pieces of LDS.
+    const int from = VECTOR && blockIdx.x == 0 ? min(head, end) : begin;  // words from here on come in vectors
+    const int base = VECTOR ? from - kPer : begin;
+
+    Row r{1.0f, 0.0f, 0.0f, nullptr};
+    if constexpr (HISTORY) {
+        if (c.repetition) r.repetition = c.repetition[row];
+        if (c.frequency) r.frequency = c.frequency[row];
+        if (c.presence) r.presence = c.presence[row];
+    }
+    if constexpr (HISTORY || BIAS) {
+        const int entries = (p.tile + kPer) * (HISTORY + BIAS);
+        for (int i = tid * 4; i < entries; i += kThreads * 4) *reinterpret_cast<u32x4*>(smem + i) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    if constexpr (HISTORY) {
+        const int32_t* h = c.history + row * c.history_size;
+        int n = (int)c.history_size, prompt = 0;
+        if (c.history_lens) n = min(max(c.history_lens[row], 0), n);
+        if (c.prompt_lens) prompt = c.prompt_lens[row];
+        auto use = [&](int i, int w) {
+            if (w >= begin && w < end) {
+                if (i < prompt) atomicOr(&uses[w - base], kPrompt);
+                else atomicAdd(&uses[w - base], 1u);
+            }
+        };
+        // Four words at a time from the first 16-byte boundary on.
+        const int lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4);
+        if (tid < lead) use(tid, h[tid]);
+        for (int i = lead + tid * 4; i < n; i += kThreads * 4) {
+            if (i + 4 <= n) {
+                const int4v w = *reinterpret_cast<const int4v*>(h + i);
+                use(i, w.x);
+                use(i + 1, w.y);
+                use(i + 2, w.z);
+                use(i + 3, w.w);
+            } else {
+                for (int j = i; j < n; ++j) use(j, h[j]);
+            }
+        }
+    }
+    if constexpr (BIAS) {
+        const int32_t* ids = c.bias_ids + row * c.bias_size;
+        r.bias = c.bias_values + row * c.bias_size;
+        int n = (int)c.bias_size;
+        if (c.bias_lens) n = min(max(c.bias_lens[row], 0), n);
+        for (int i = tid; i < n; i += kThreads) {
+            const int w = ids[i];
+            if (w >= begin && w < end) atomicMax(&listed[w - base], (uint32_t)i + 1u);
+        }
+    }
+    if constexpr (HISTORY || BIAS) __syncthreads();
+
+    float top = -INFINITY;
+    int word = -1;
+    auto take = [&](float v, int w, bool allowed) {
+        if (allowed && (v > top || (word < 0 && v == v))) {
+            top = v;
+            word = w;
+        }
+    };
+    auto one = [&](int w) {
+        const bool allowed = !mask || (mask[w >> 5] >> (w & 31) & 1);
+        const float v = adjusted((float)x[w], HISTORY ? uses[w - base] : 0, BIAS ? listed[w - base] : 0, r);
+        y[w] = (T)(allowed ? v : -INFINITY);
+        take(v, w, allowed);
+    };
+    if constexpr (!VECTOR) {
+        for (int w = begin + tid; w < end; w += kThreads) one(w);
+    } else {
+        typedef T Vec __attribute__((ext_vector_type(kPer)));
+        if (blockIdx.x == 0 && tid < from) one(tid);
+        const int vectors = (end - from) / kPer;
+        constexpr int kUnroll = 4;
+        const int words = (vocab + 31) >> 5;
+        for (int i0 = tid; i0 < vectors; i0 += kThreads * kUnroll) {
+            Vec in[kUnroll];
+            uint32_t ok[kUnroll];
+#pragma unroll
+            for (int j = 0; j < kUnroll; ++j) {
+                const int i = min(i0 + j * kThreads, vectors - 1), w = from + i * kPer;
+                in[j] = *gbl(reinterpret_cast<const Vec*>(x + w));
+                ok[j] = ~0u;
+                if (mask) {
+                    const uint32_t lo = mask[w >> 5], hi = mask[min((w >> 5) + 1, words - 1)];
+                    ok[j] = __builtin_amdgcn_alignbit(hi, lo, w & 31);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kUnroll; ++j) {
+                const int i = i0 + j * kThreads, w = from + i * kPer;
+                if (i >= vectors) break;
+                float v[kPer];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) v[e] = (float)in[j][e];
+                if constexpr (HISTORY || BIAS) {
+                    u32x4 used[kPer / 4] = {}, named[kPer / 4] = {};
+                    u32x4 any = {0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < kPer / 4; ++e) {
+                        if constexpr (HISTORY) any |= used[e] = *reinterpret_cast<const u32x4*>(uses + (w - base) + 4 * e);
+                        if constexpr (BIAS) any |= named[e] = *reinterpret_cast<const u32x4*>(listed + (w - base) + 4 * e);
+                    }
+                    if (any.x | any.y | any.z | any.w) {
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) v[e] = adjusted(v[e], used[e / 4][e % 4], named[e / 4][e % 4], r);
+                    }
+                }
+                Vec out;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const bool allowed = ok[j] >> e & 1;
+                    take(v[e], w + e, allowed);
+                    out[e] = (T)(allowed ? v[e] : -INFINITY);
+                }
+                *gbl(reinterpret_cast<Vec*>(y + w)) = out;
+            }
+        }
+        const int rest = from + vectors * kPer + tid;
+        if (rest < end) one(rest);
+    }
+    if (!c.token) return;
+    best_of_wave<64>(top, word);
+    if ((tid & 63) == 0) {
+        sh_v[tid >> 6] = top;
+        sh_w[tid >> 6] = word;
+    }
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) better(top, word, sh_v[i], sh_w[i]);
+        if (p.tiles == 1) {
+            c.token[row] = word;
+        } else {
+            p.best[row * p.tiles + blockIdx.x] = top;
+            p.best_word[row * p.tiles + blockIdx.x] = word;
+        }
+    }
+}
+
+// The best of a row's tiles; one wave per row.
+__global__ __launch_bounds__(kPickThreads) void pick_kernel(const Params p) {
+    const int64_t row = blockIdx.x;
+    float top = -INFINITY;
+    int word = -1;
+    for (int i = threadIdx.x; i < p.tiles; i += kPickThreads) better(top, word, p.best[row * p.tiles + i], p.best_word[row * p.tiles + i]);
+    best_of_wave<64>(top, word);
+    if (threadIdx.x == 0) p.c.token[row] = word;
+}
+
+// ------------------------------------------------------------------ host
+
+// Words of a tile: long ones scan a history less often, short ones give every
+// CU some.
+int64_t tile_of(int64_t rows, int64_t vocab) {
+    int64_t t = kMaxTile;
+    while (t > kMinTile && rows * ((vocab + t - 1) / t) < 1024) t /= 2;
+    return t;
+}
+int64_t tiles_of(int64_t vocab, int64_t tile) { return (vocab + tile - 1) / tile; }
+
+size_t workspace_of(int64_t rows, int64_t vocab) {
+    const int64_t tiles = tiles_of(vocab, tile_of(rows, vocab));
+    return tiles > 1 ? (size_t)(rows * tiles * 8 + 15) / 16 * 16 : 0;
+}
+
+wq_status check_sizes(const char* fn, int64_t rows, int64_t vocab, int64_t dtype) {
+    WQ_TRY(in_range(fn, "rows", rows, 1, WQ_LOGITS_MAX_ROWS));
+    WQ_TRY(in_range(fn, "vocab", vocab, 1, WQ_LOGITS_MAX_VOCAB));
+    if (dtype != WQ_DTYPE_F16 && dtype != WQ_DTYPE_BF16 && dtype != WQ_DTYPE_F32)
+        return err(WQ_ERR_UNSUPPORTED, "%s: dtype must be one of WQ_DTYPE_* (got %lld)", fn, (long long)dtype);
+    return WQ_OK;
+}
+
+template <typename T, bool HISTORY, bool BIAS>
+void launch_as(const Params& p, bool vector, hipStream_t stream) {
+    const dim3 grid((unsigned)p.tiles, (unsigned)p.c.rows);
+    const size_t lds = (size_t)(HISTORY + BIAS) * (p.tile + Type<T>::kPer) * 4;
+    if (vector) hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, true>), grid, dim3(kThreads), lds, stream, p);
+    else hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, false>), grid, dim3(kThreads), lds, stream, p);
+}
+
+template <typename T>
+void launch_type(const Params& p, hipStream_t stream) {
+    // 16-byte accesses need input and output rows that lie alike, row by row.
+    const uintptr_t apart = reinterpret_cast<uintptr_t>(p.c.logits) - reinterpret_cast<uintptr_t>(p.c.out);
+    const bool vector = apart % 16 == 0 && (p.c.rows == 1 || (p.c.logits_stride - p.c.out_stride) * (int64_t)sizeof(T) % 16 == 0);
+    const bool history = p.c.history != nullptr, bias = p.c.bias_ids != nullptr;
+    if (history && bias) launch_as<T, true, true>(p, vector, stream);
+    else if (history) launch_as<T, true, false>(p, vector, stream);
+    else if (bias) launch_as<T, false, true>(p, vector, stream);
+    else launch_as<T, false, false>(p, vector, stream);
+}
+
+}  // namespace
+}  // namespace logits
+}  // namespace wq
+
+using namespace wq::logits;
+using wq::host::aligned;
+using wq::host::err;
+using wq::host::in_range;
+using wq::host::overlaps;
+using wq::host::span;
+using wq::host::Span;
+
+extern "C" {
+
+wq_status wq_process_logits_workspace_size(int64_t rows, int64_t vocab, int64_t dtype, size_t* bytes) {
+    static const char* fn = "wq_process_logits_workspace_size";
+    if (!bytes) return err(WQ_ERR_INVALID_ARG, "%s: null output pointer", fn);
+    WQ_TRY(check_sizes(fn, rows, vocab, dtype));
+    *bytes = workspace_of(rows, vocab);
+    return WQ_OK;
+}
+
+wq_status wq_process_logits(const wq_logits_call* call, void* workspace, size_t workspace_bytes, void* stream) {
+    static const char* fn = "wq_process_logits";
+    if (!call || !call->logits || !call->out) return err(WQ_ERR_INVALID_ARG, "%s: null pointer", fn);
+    Params p{};
+    p.c = *call;
+    const wq_logits_call& c = p.c;
+    WQ_TRY(check_sizes(fn, c.rows, c.vocab, c.dtype));
+    const int64_t size = c.dtype == WQ_DTYPE_F32 ? 4 : 2, words = (c.vocab + 31) / 32;
+    constexpr int64_t kMaxStride = (int64_t)1 << 32;
+    WQ_TRY(in_range(fn, "logits_stride", c.logits_stride, c.vocab, kMaxStride));
+    WQ_TRY(in_range(fn, "out_stride", c.out_stride, c.vocab, kMaxStride));
+    if (c.mask) WQ_TRY(in_range(fn, "mask_stride", c.mask_stride, words, kMaxStride));
+    if (c.history) {
+        WQ_TRY(in_range(fn, "history_size", c.history_size, 1, WQ_LOGITS_MAX_HISTORY));
+    } else if (c.history_lens || c.prompt_lens || c.repetition || c.frequency || c.presence) {
+        return err(WQ_ERR_INVALID_ARG, "%s: lengths and penalties need a history", fn);
+    }
+    if (c.bias_ids) {
+        WQ_TRY(in_range(fn, "bias_size", c.bias_size, 1, WQ_LOGITS_MAX_BIAS));
+        if (!c.bias_values) return err(WQ_ERR_INVALID_ARG, "%s: bias_ids without bias_values", fn);
+    } else if (c.bias_values || c.bias_lens) {
+        return err(WQ_ERR_INVALID_ARG, "%s: bias values or lengths without bias_ids", fn);
+    }
+    if (!aligned(c.logits, size) || !aligned(c.out, size)) return err(WQ_ERR_MISALIGNED, "%s: logits and out must be aligned to their elements", fn);
+    const void* const fours[] = {c.token, c.mask, c.history, c.history_lens, c.prompt_lens, c.repetition, c.frequency, c.presence, c.bias_ids, c.bias_values, c.bias_lens};
+    for (const void* f : fours)
+        if (!aligned(f, 4)) return err(WQ_ERR_MISALIGNED, "%s: every list must be 4-byte aligned", fn);
+
+    const uint64_t rows = (uint64_t)c.rows;
+    const size_t ws = c.token ? workspace_of(c.rows, c.vocab) : 0;
+    if (ws > 0) {
+        if (!workspace || workspace_bytes < ws)
+            return err(WQ_ERR_INVALID_ARG, "%s: a workspace of %zu bytes is needed (got %zu)", fn, ws, workspace ? workspace_bytes : (size_t)0);
+        if (!aligned(workspace, 16)) return err(WQ_ERR_MISALIGNED, "%s: workspace must be 16-byte aligned", fn);
+    }
+    const Span out = span(c.out, ((rows - 1) * c.out_stride + c.vocab) * size), in = span(c.logits, ((rows - 1) * c.logits_stride + c.vocab) * size);
+    const Span token = span(c.token, c.token ? rows * 4 : 0), work = span(workspace, ws);
+    auto list = [&](const void* ptr, uint64_t bytes) { return span(ptr, ptr ? bytes : 0); };
+    const Span inputs[] = {list(c.mask, ((rows - 1) * c.mask_stride + words) * 4), list(c.history, rows * c.history_size * 4), list(c.history_lens, rows * 4),
+                           list(c.prompt_lens, rows * 4), list(c.repetition, rows * 4), list(c.frequency, rows * 4), list(c.presence, rows * 4),
+                           list(c.bias_ids, rows * c.bias_size * 4), list(c.bias_values, rows * c.bias_size * 4), list(c.bias_lens, rows * 4)};
+    for (const Span& s : inputs)
+        if (overlaps(s, out) || overlaps(s, token) || overlaps(s, work)) return err(WQ_ERR_INVALID_ARG, "%s: an output or the workspace overlaps an input", fn);
+    const bool in_place = c.out == c.logits && (c.out_stride == c.logits_stride || c.rows == 1);
+    if ((overlaps(out, in) && !in_place) || overlaps(out, token) || overlaps(out, work) || overlaps(in, token) || overlaps(in, work) || overlaps(token, work))
+        return err(WQ_ERR_INVALID_ARG, "%s: out, token and the workspace must not overlap", fn);
+
+    p.tile = (int32_t)tile_of(c.rows, c.vocab);
+    p.tiles = (int32_t)tiles_of(c.vocab, p.tile);
+    p.best = static_cast<float*>(workspace);
+    p.best_word = ws ? reinterpret_cast<int32_t*>(p.best + rows * p.tiles) : nullptr;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    if (c.dtype == WQ_DTYPE_F16) launch_type<_Float16>(p, st);
+    else if (c.dtype == WQ_DTYPE_BF16) launch_type<__bf16>(p, st);
+    else launch_type<float>(p, st);
+    if (c.token && p.tiles > 1) hipLaunchKernelGGL(pick_kernel, dim3((unsigned)c.rows), dim3(kPickThreads), 0, st, p);
+    return wq::host::hip_result(fn, hipGetLastError());
+}
+
+}  // extern "C"

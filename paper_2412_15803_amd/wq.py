@@ -32,7 +32,7 @@ EXPORTED = ("wq_status_string", "wq_last_error_message", "wq_version", "wq_pack"
             "wq_decode_linears", "wq_decode_linears_noalloc", "wq_paged_attention_workspace_size",
             "wq_paged_attention", "wq_fused_linears", "wq_fused_check", "wq_stream_read",
             "wq_cache_append", "wq_cache_copy_pages", "wq_page_workspace_size", "wq_cache_reserve", "wq_cache_free",
-            "wq_cache_fork", "wq_cache_compact")
+            "wq_cache_fork", "wq_cache_compact", "wq_process_logits_workspace_size", "wq_process_logits")
 
 # Limits of wq_decode_linears_noalloc (include/wq.h).
 NOALLOC_MAX_LINEARS = 1024
@@ -67,6 +67,13 @@ class WqFusedLinear(ctypes.Structure):
         ("prologue", ctypes.c_int32),
         ("eps", ctypes.c_float),
     ]
+
+
+class WqLogitsCall(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in (
+        "logits", "out", "token", "mask", "history", "history_lens", "prompt_lens", "repetition", "frequency", "presence",
+        "bias_ids", "bias_values", "bias_lens")] + [(name, ctypes.c_int64) for name in (
+            "rows", "vocab", "logits_stride", "out_stride", "mask_stride", "history_size", "bias_size", "dtype")]
 
 
 class WQError(RuntimeError):
@@ -121,7 +128,9 @@ def lib() -> ctypes.CDLL:
             ("wq_cache_reserve", [vp] * 4 + [i64] * 4 + [vp, vp, sz, vp]),
             ("wq_cache_free", [vp] * 4 + [i64] * 7 + [vp]),
             ("wq_cache_fork", [vp, i64] + [vp] * 5 + [i64] * 7 + [vp, vp, sz, vp]),
-            ("wq_cache_compact", [vp, i64, i64] + [vp] * 5 + [i64] * 3 + [vp, sz, vp])):
+            ("wq_cache_compact", [vp, i64, i64] + [vp] * 5 + [i64] * 3 + [vp, sz, vp]),
+            ("wq_process_logits_workspace_size", [i64, i64, i64, ctypes.POINTER(sz)]),
+            ("wq_process_logits", [vp, vp, sz, vp])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -150,11 +159,12 @@ def _check(status: int) -> None:
 
 _torch = None
 _WORDS = _HALVES = _FLOATS = _INTS = _BYTES = ()
+_DTYPES = {}  # WQ_DTYPE_* of include/wq_logits.h
 _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _raw_stream
+    global _torch, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _DTYPES, _raw_stream
     import torch
 
     _WORDS = (torch.int32, torch.uint32)
@@ -162,6 +172,7 @@ def _load_torch():
     _FLOATS = (torch.float32,)
     _INTS = (torch.int32,)
     _BYTES = (torch.uint8,)
+    _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
     # The current stream's handle without building a Stream object.
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _torch = torch
@@ -539,6 +550,87 @@ def cache_compact(caches: CacheSet, block_table, refs, new_table, new_refs, live
     pw, nw = _workspace(workspace, refs)
     _check((_lib or lib()).wq_cache_compact(caches.array, len(caches.array), caches.page_bytes, pt, pr, pnt, pnr, pl, num_seqs, num_pages,
                                             max_pages, pw, nw, _stream(stream, refs)))
+
+
+# ------------------------------------------------------- logits to token
+
+def logits_workspace(logits):
+    """A device workspace (uint8 tensor, or None) for process_logits."""
+    _torch or _load_torch()
+    n = ctypes.c_size_t(0)
+    _check(lib().wq_process_logits_workspace_size(logits.shape[0], logits.shape[1], _DTYPES[logits.dtype], ctypes.byref(n)))
+    return _torch.empty(n.value, dtype=_torch.uint8, device=logits.device) if n.value else None
+
+
+def _row_stride(t, name, shape):
+    """Address and row stride of a device tensor whose rows may lie apart."""
+    if not isinstance(t, _torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    stride, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), stride if shape[0] > 1 else max(stride, shape[1])
+
+
+def process_logits(logits, out, token=None, mask=None, history=None, history_lens=None, prompt_lens=None, repetition=None,
+                   frequency=None, presence=None, bias_ids=None, bias_values=None, bias_lens=None, workspace=None, stream=None) -> None:
+    """Penalties, biases and a grammar's mask on logits [R, V] (fp16, bf16 or
+    fp32; rows may lie apart), into out (which may be logits), and the best
+    word of each row into token (int32 [R], -1 where none is allowed).
+
+    mask [R, ceil(V / 32)] int32/uint32: bit w % 32 of word w / 32 allows word
+    w.  history [R, H] int32: the prompt's words (prompt_lens of them), then the
+    generated ones (history_lens in all).  repetition, frequency, presence
+    fp32 [R].  bias_ids int32 and bias_values fp32 [R, B], bias_lens of them used.
+    What is None is left out (include/wq_logits.h has the formulas)."""
+    _torch or _load_torch()
+    if logits.dim() != 2:
+        raise ValueError("logits must be [R, V]")
+    shape = logits.shape
+    rows, vocab = shape
+    kind = _DTYPES.get(logits.dtype)
+    if kind is None or out.dtype != logits.dtype:
+        raise TypeError(f"logits and out must share one of {tuple(_DTYPES)} (got {logits.dtype}, {out.dtype})")
+    px, xs = _row_stride(logits, "logits", shape)
+    py, ys = _row_stride(out, "out", shape)
+    one = (rows,)
+    pt = _dev_tensor(token, "token", _INTS, one) if token is not None else None
+    pm = ms = 0
+    if mask is not None:
+        if mask.dtype not in _WORDS:
+            raise TypeError(f"mask has dtype {mask.dtype}, expected one of {_WORDS}")
+        pm, ms = _row_stride(mask, "mask", (rows, (vocab + 31) // 32))
+    hs = bs = 0
+    ph = phl = ppl = pr = pf = pp = pbi = pbv = pbl = None
+    if history is not None:
+        hs = history.shape[-1]
+        ph = _dev_tensor(history, "history", _INTS, (rows, hs))
+    if history_lens is not None:
+        phl = _dev_tensor(history_lens, "history_lens", _INTS, one)
+    if prompt_lens is not None:
+        ppl = _dev_tensor(prompt_lens, "prompt_lens", _INTS, one)
+    if repetition is not None:
+        pr = _dev_tensor(repetition, "repetition", _FLOATS, one)
+    if frequency is not None:
+        pf = _dev_tensor(frequency, "frequency", _FLOATS, one)
+    if presence is not None:
+        pp = _dev_tensor(presence, "presence", _FLOATS, one)
+    if bias_ids is not None:
+        bs = bias_ids.shape[-1]
+        pbi = _dev_tensor(bias_ids, "bias_ids", _INTS, (rows, bs))
+    if bias_values is not None:
+        pbv = _dev_tensor(bias_values, "bias_values", _FLOATS, (rows, bs))
+    if bias_lens is not None:
+        pbl = _dev_tensor(bias_lens, "bias_lens", _INTS, one)
+    if workspace is None and token is not None:
+        workspace = logits_workspace(logits)
+    pw, nw = _workspace(workspace, logits)
+    call = WqLogitsCall(px, py, pt, pm or None, ph, phl, ppl, pr, pf, pp, pbi, pbv, pbl, rows, vocab, xs, ys, ms, hs, bs, kind)
+    _check((_lib or lib()).wq_process_logits(ctypes.addressof(call), pw, nw, _stream(stream, logits)))
 
 
 # ------------------------------------------------------- measurement probe
