@@ -1,0 +1,1148 @@
+// Causal attention with a sliding window and sinks over a paged KV cache
+// (gfx950, wave64), for single tokens and for prompts: one pass over the
+// visible keys and values with the running maximum and sum of the softmax.
+//
+// Rows.  A kv head serves G query heads, so the n new tokens of a sequence are
+// n G rows (row r: token r / G, head r % G) against the same keys and values.
+// Both kernels put rows on the columns of the matrix cores and compute
+// S^T = K Q^T and O^T = V^T P^T.  A lane then holds scores of one row only: the
+// softmax needs one exchange between lanes per tile, the factors that rescale O
+// are a lane's own, and S^T leaves the matrix cores in the layout that the next
+// product takes P^T in, with the tokens of a tile in another order, which V is
+// read in as well.  P never leaves the registers.
+//
+//   few_kernel   sequences with up to 16 rows (decoding).  Bound by the bytes
+//                of the cache: no LDS, keys and values go from memory to the
+//                matrix cores' registers, 32 tokens per wave and step, and the
+//                cache is split over workgroups by the sequences' lengths.
+//   tile_kernel  all others.  Bound by the matrix cores: 128 rows per
+//                workgroup, 64-token tiles through LDS.
+//
+// Where the cache is split, merge kernels join the parts.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "wq_device.h"
+#include "wq_host.h"
+#include "wq_internal.h"
+#include "wq_window.h"
+
+namespace wq {
+namespace window {
+namespace {
+
+using dev::gbl;
+using dev::u32x4;
+using namespace host;
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kFewRows = 16;    // rows of few_kernel
+constexpr int kFewTokens = 32;  // tokens of one of its steps
+constexpr int kTileRows = 128;  // rows of a workgroup of tile_kernel, 32 per wave
+constexpr int kTileTokens = 64;
+constexpr float kRescale = 8.0f;  // see Softmax
+
+template <typename T>
+struct Type;
+template <>
+struct Type<_Float16> {
+    typedef _Float16 Vec8 __attribute__((ext_vector_type(8)));
+    static constexpr uint16_t kNaN = 0x7E00;
+    static constexpr uint32_t kExponent = 0x7C00;
+    static __device__ __forceinline__ float4v mfma16(Vec8 a, Vec8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float16v mfma32(Vec8 a, Vec8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Type<__bf16> {
+    typedef __bf16 Vec8 __attribute__((ext_vector_type(8)));
+    static constexpr uint16_t kNaN = 0x7FC0;
+    static constexpr uint32_t kExponent = 0x7F80;
+    static __device__ __forceinline__ float4v mfma16(Vec8 a, Vec8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float16v mfma32(Vec8 a, Vec8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+template <typename T>
+__device__ __forceinline__ uint16_t bits_of(float x) {
+    return __builtin_bit_cast(uint16_t, static_cast<T>(x));
+}
+template <typename T>
+__device__ __forceinline__ float value_of(uint32_t bits) {
+    return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(bits)));
+}
+
+// The word with those of its two 16-bit values cleared that are not finite.
+template <typename T>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+    constexpr uint32_t e = Type<T>::kExponent;
+    const uint32_t lo = (w & e) == e ? 0u : w & 0xFFFFu, hi = (w >> 16 & e) == e ? 0u : w & 0xFFFF0000u;
+    return lo | hi;
+}
+// A value that is not finite as it is, 0 for the others.
+template <typename T>
+__device__ __forceinline__ float other_part(uint32_t bits) {
+    return (bits & Type<T>::kExponent) == Type<T>::kExponent ? value_of<T>(bits) : 0.0f;
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+struct Params {
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    const int32_t* table;
+    const int32_t* lens;
+    const int32_t* starts;
+    uint16_t* out;
+    int64_t max_pages, q_stride, out_stride;
+    int64_t page_stride;  // elements of a page
+    int32_t num_seqs, num_tokens, max_query, num_pages, hq, hkv, group, log2_page, max_seq_len;
+    int32_t window, sinks;
+    float c;           // |scale| log2(e): scores in log2 units
+    uint32_t q_and, q_xor;  // scale < 0 changes the signs of q, scale = 0 makes it zero (with c = 1)
+    // few_kernel
+    int32_t units;     // per kv head
+    int32_t few_slots; // rows of a unit's partial results
+    float* few_acc;    // [unit][kv head][few_slots][head_dim]
+    float2* few_ml;    // [unit][kv head][few_slots]: (m, l)
+    // tile_kernel
+    int32_t splits;
+    float* tile_acc;   // [token][q head][splits][head_dim]
+    float2* tile_ml;
+    int32_t tiles_too; // tile_kernel runs as well
+};
+
+// ------------------------------------------------------------- sequences
+
+struct Seq {
+    int first, n, len;  // first row of q, new tokens, tokens
+    bool bad;           // its outputs are NaN
+    __device__ __forceinline__ bool few(const Params& p) const { return n * p.group <= kFewRows || !p.tiles_too; }
+};
+
+__device__ __forceinline__ Seq seq_of(const Params& p, int s) {
+    Seq q;
+    q.first = s;
+    q.n = 1;
+    if (p.starts) {
+        q.first = p.starts[s];
+        const int end = p.starts[s + 1];
+        q.n = q.first < 0 || end > p.num_tokens || end < q.first ? 0 : end - q.first;
+    }
+    q.len = p.lens[s];
+    q.bad = q.len > p.max_seq_len || q.len > (p.max_pages << p.log2_page) || q.n > q.len || q.n > p.max_query;
+    return q;
+}
+
+// The tokens that new tokens at positions [lo, hi] see, in tiles of TOKENS:
+// those of the sinks below `start`, then all from `start` on.
+template <int TOKENS>
+struct Tiles {
+    int first;       // no token below it is in the window of the first
+    int start;       // first, down to a multiple of TOKENS
+    int sink_tiles, count;
+    __device__ __forceinline__ Tiles(const Params& p, int lo, int hi) {
+        first = max(0, lo - p.window + 1);
+        start = first & ~(TOKENS - 1);
+        sink_tiles = (min(p.sinks, start) + TOKENS - 1) / TOKENS;
+        count = sink_tiles + (hi - start + TOKENS) / TOKENS;
+    }
+    __device__ __forceinline__ int token(int tile) const { return tile < sink_tiles ? tile * TOKENS : start + (tile - sink_tiles) * TOKENS; }
+};
+
+__device__ __forceinline__ bool sees(const Params& p, int place, int t) { return t <= place && (t < p.sinks || t > place - p.window); }
+
+// ------------------------------------------------------------ lane tools
+
+__device__ __forceinline__ int inclusive_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1, 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2, 3
+    return v;
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+
+// The values of lanes l and l ^ 32 (HALVES) or l and l ^ 16, lower lane first.
+template <bool HALVES>
+__device__ __forceinline__ void pair_values(float x, float& lo, float& hi) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    uint32_t e0, e1;
+    if constexpr (HALVES) {
+        auto p = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+        e0 = p[0];
+        e1 = p[1];
+    } else {
+        auto p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+        e0 = p[0];
+        e1 = p[1];
+    }
+    lo = __builtin_bit_cast(float, e0);
+    hi = __builtin_bit_cast(float, e1);
+}
+template <bool HALVES>
+__device__ __forceinline__ float pair_max(float x) {
+    float a, b;
+    pair_values<HALVES>(x, a, b);
+    return fmaxf(a, b);
+}
+template <bool HALVES>
+__device__ __forceinline__ float pair_sum(float x) {
+    float a, b;
+    pair_values<HALVES>(x, a, b);
+    return a + b;
+}
+
+// Softmax.  m is the reference that a row's weights 2^(c s - c m) are formed
+// against, l this lane's share of their sum.  m follows the row's largest score
+// only when that passes it by more than kRescale in log2 units, so a wave
+// rarely has to rescale its accumulators; weights then reach at most 2^8, within
+// range of both 16-bit types, and their sums are fp32.
+struct Softmax {
+    float m = -INFINITY, l = 0.0f;
+    // Given the row's largest new score: whether any row of the wave needs a new
+    // reference, and if so the factor for this row (1 where it keeps its own, so
+    // that no row's bits depend on the others).
+    __device__ __forceinline__ bool advance(float mx, float c, float& factor) {
+        const bool need = (mx - m) * c > kRescale;
+        if (!__builtin_amdgcn_ballot_w64(need)) return false;
+        factor = need ? exp2_((m - mx) * c) : 1.0f;
+        m = need ? mx : m;
+        l *= factor;
+        return true;
+    }
+    // c m, or 0 while nothing is visible (every weight is then 2^-inf = 0).
+    __device__ __forceinline__ float base(float c) const { return m == -INFINITY ? 0.0f : m * c; }
+};
+
+// ------------------------------------------------------ few rows: the split
+//
+// The visible tokens of every few-row sequence are cut into steps of 32 tokens
+// and the steps into units, each one workgroup's (per kv head).  The lengths
+// are on the device, so every wave works the cut out for itself: T steps to a
+// unit, T the least that makes at most `units` of them (each sequence at least
+// one), and then which sequence unit u falls in.  The steps of a sequence are
+// dealt evenly over its units.
+struct Unit {
+    int seq, steps, chunk, first, count;  // steps of the sequence; which of its `count` units, the first of them
+};
+
+__device__ __forceinline__ int few_steps(const Params& p, int s) {
+    const Seq q = seq_of(p, s);
+    if (q.n == 0 || !q.few(p)) return 0;
+    if (q.bad) return 1;
+    return max(1, Tiles<kFewTokens>(p, q.len - q.n, q.len - 1).count);
+}
+
+__device__ __forceinline__ bool unit_of(const Params& p, int u, Unit& out) {
+    if (p.units == p.num_seqs) {
+        out = Unit{u, few_steps(p, u), 0, u, 1};
+        return out.steps > 0;
+    }
+    const int lane = threadIdx.x & 63;
+    const int per = (p.num_seqs + 63) / 64;  // lane i has sequences [i per, (i + 1) per)
+    const int s0 = min(lane * per, p.num_seqs), s1 = min(s0 + per, p.num_seqs);
+    const int steps0 = s0 < s1 ? few_steps(p, s0) : 0;
+    auto steps_of = [&](int s) { return s == s0 ? steps0 : few_steps(p, s); };
+    int sum = 0;
+    for (int s = s0; s < s1; ++s) sum += steps_of(s);
+    const int total = last_lane(inclusive_scan(sum));
+    // sum of ceil(steps / T) <= total / T + sequences <= units.
+    const int t = max(1, (total + p.units - p.num_seqs - 1) / (p.units - p.num_seqs));
+    auto units_of = [&](int steps) { return (steps + t - 1) / t; };
+    int mine = 0;
+    for (int s = s0; s < s1; ++s) mine += units_of(steps_of(s));
+    int first = inclusive_scan(mine) - mine;
+    const bool here = u >= first && u < first + mine;
+    const uint64_t owner = __builtin_amdgcn_ballot_w64(here);
+    if (owner == 0) return false;
+    int s = s0, steps = steps0, n = units_of(steps0);
+    if (here) {
+        while (u >= first + n) {
+            first += n;
+            steps = few_steps(p, ++s);
+            n = units_of(steps);
+        }
+    }
+    const int from = __builtin_ctzll(owner);
+    out.seq = __builtin_amdgcn_readlane(s, from);
+    out.steps = __builtin_amdgcn_readlane(steps, from);
+    out.first = __builtin_amdgcn_readlane(first, from);
+    out.count = __builtin_amdgcn_readlane(n, from);
+    out.chunk = u - out.first;
+    return true;
+}
+
+// Output address of row r of a sequence.
+__device__ __forceinline__ uint16_t* out_row(const Params& p, const Seq& q, int kvh, int r, int dim) {
+    return p.out + (int64_t)(q.first + r / p.group) * p.out_stride + (int64_t)(kvh * p.group + r % p.group) * dim;
+}
+
+// o = acc / l; rows that see nothing are zero.
+template <typename T>
+__device__ __forceinline__ uint16_t finish(const Params& p, float acc, float l) {
+    if (p.window == 0 && p.sinks == 0) return l != l ? Type<T>::kNaN : 0;
+    return l != l ? Type<T>::kNaN : bits_of<T>(acc / l);
+}
+
+// One step's keys and values in registers.  Lane (i = lane % 16, g = lane / 16):
+//   k[a][ks]  key of token 8 (i / 4) + 4 a + i % 4, dims 32 ks + 8 g .. + 7;
+//   v[j]      value of token 8 g + j, dims VW i .. VW i + VW - 1.
+// The matrix cores' row i of key tile a is then token 8 (i / 4) + 4 a + i % 4, so
+// that they leave the scores of tokens 8 g + 4 a + r in lane group g: the
+// tokens whose values it holds.
+template <int D>
+struct Step {
+    static constexpr int kKs = D / 32, kVw = D / 16;
+    typedef uint32_t VLoad __attribute__((ext_vector_type(kVw / 2)));
+    u32x4 k[2][kKs];
+    VLoad v[8];
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void few_kernel(const Params p) {
+    using Vec8 = typename Type<T>::Vec8;
+    constexpr int kKs = Step<D>::kKs, kVw = Step<D>::kVw;
+    using VLoad = typename Step<D>::VLoad;
+    __shared__ float sh_acc[kWaves][kFewRows][D];
+    __shared__ float sh_m[kWaves][kFewRows], sh_l[kWaves][kFewRows];
+
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % p.hkv, u = blockIdx.x / p.hkv;
+    Unit un;
+    if (!unit_of(p, u, un)) return;
+    const Seq q = seq_of(p, un.seq);
+    const int rows = q.n * p.group;
+    if (q.bad) {
+        for (int64_t x = tid; x < (int64_t)rows * D; x += kThreads) out_row(p, q, kvh, (int)(x / D), D)[x % D] = Type<T>::kNaN;
+        return;
+    }
+    const Tiles<kFewTokens> tiles(p, q.len - q.n, q.len - 1);
+    const int begin = (int)((int64_t)tiles.count * un.chunk / un.count), end = (int)((int64_t)tiles.count * (un.chunk + 1) / un.count);
+    const int place = q.len - q.n + min(i / p.group, q.n - 1);  // of the lane's row
+    const int last = q.len - 1;
+
+    Vec8 qf[kKs];
+    {
+        const int r = min(i, rows - 1);
+        const uint16_t* src = p.q + (int64_t)(q.first + r / p.group) * p.q_stride + (int64_t)(kvh * p.group + r % p.group) * D + g * 8;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            u32x4 w = *gbl(reinterpret_cast<const u32x4*>(src + ks * 32));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (w[e] & p.q_and) ^ p.q_xor;
+            qf[ks] = __builtin_bit_cast(Vec8, w);
+        }
+    }
+
+    const int32_t* trow = p.table + (int64_t)un.seq * p.max_pages;
+    const int page_mask = (1 << p.log2_page) - 1;
+    const bool whole = p.log2_page >= 3;  // 8 aligned tokens share a page
+    const uint16_t* kbase = p.k + ((int64_t)kvh << p.log2_page) * D;
+    const uint16_t* vbase = p.v + ((int64_t)kvh << p.log2_page) * D;
+    int bad = 0;
+
+    // Visible to some row: only the pages of such tokens are looked up; others
+    // stand for page 0 and are masked.
+    auto used = [&](int t) { return t <= last && (t < p.sinks || t >= tiles.first); };
+    auto lookup = [&](int t) { return used(t) ? trow[t >> p.log2_page] : 0; };
+    // Element offset of token t in a kv head's part of the cache.
+    auto offset = [&](int page, int t) {
+        if ((uint32_t)page >= (uint32_t)p.num_pages) {
+            bad = 1;
+            page = 0;
+        }
+        return (int64_t)page * p.page_stride + (int64_t)(t & page_mask) * D;
+    };
+    // The table entries of a step; those of the next step are fetched while one
+    // is loaded, so that no load waits for them.
+    struct Pages {
+        int k[2], v;
+    };
+    auto pages_of = [&](int step) {
+        const int t0 = tiles.token(step);
+        Pages pg{};
+        const int kt = t0 + (i >> 2) * 8, vt = t0 + g * 8;
+        if (whole) {
+            // A group of 8 has one page: that of its first used token.
+            auto of_group = [&](int t) { return lookup(min(t < p.sinks ? t : max(t, tiles.first), t + 7)); };
+            pg.k[0] = pg.k[1] = of_group(kt);
+            pg.v = of_group(vt);
+        } else {
+            pg.k[0] = lookup(kt + (i & 3));
+            pg.k[1] = lookup(kt + 4 + (i & 3));
+        }
+        return pg;
+    };
+    auto load = [&](Step<D>& s, int step, const Pages& pg) {
+        const int t0 = tiles.token(step);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const uint16_t* src = kbase + offset(pg.k[a], t0 + (i >> 2) * 8 + a * 4 + (i & 3)) + g * 8;
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) s.k[a][ks] = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(src + ks * 32)));
+        }
+        if (whole) {
+            const uint16_t* src = vbase + offset(pg.v, t0 + g * 8) + i * kVw;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s.v[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const VLoad*>(src + j * D)));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int t = t0 + g * 8 + j;
+                s.v[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const VLoad*>(vbase + offset(lookup(t), t) + i * kVw)));
+            }
+        }
+    };
+
+    Softmax sm;
+    float4v o[kVw];
+#pragma unroll
+    for (int m = 0; m < kVw; ++m) o[m] = float4v{0, 0, 0, 0};
+
+    auto compute = [&](Step<D>& s, int step) {
+        const int t0 = tiles.token(step);
+        float4v st[2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            st[a] = float4v{0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) st[a] = Type<T>::mfma16(__builtin_bit_cast(Vec8, s.k[a][ks]), qf[ks], st[a]);
+        }
+        // Every row sees every token of the step, or some are masked.
+        const int lo = q.len - q.n;
+        const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
+        uint32_t partly = 0;  // tokens that only some rows see and whose values are not all finite
+        if (!all) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int t = t0 + g * 8 + j;
+                if (!sees(p, place, t)) st[j / 4][j % 4] = -INFINITY;
+                const bool any = used(t), every = t <= lo && (t < p.sinks || t > last - p.window);
+                bool clean = true;
+#pragma unroll
+                for (int e = 0; e < kVw / 2; ++e) {
+                    const uint32_t w = s.v[j][e], f = finite_part<T>(w);
+                    clean = clean && (w == f || every);
+                    s.v[j][e] = every ? w : any ? f : 0u;
+                }
+                if (any && !clean) partly |= 1u << j;
+            }
+        }
+        float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
+        mx = pair_max<true>(pair_max<false>(mx));
+        float f;
+        if (sm.advance(mx, p.c, f)) {
+#pragma unroll
+            for (int m = 0; m < kVw; ++m) o[m] *= f;
+        }
+        if (__builtin_amdgcn_ballot_w64(partly != 0)) {
+            // What is not finite goes to the rows that see it, token by token (after
+            // the rescaling, whose first factor is 0).
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t who = __builtin_amdgcn_ballot_w64(partly >> j & 1);
+                for (int g2 = 0; g2 < 4; ++g2) {
+                    if (!(who >> (16 * g2) & 0xFFFF)) continue;
+                    const int t = t0 + g2 * 8 + j;
+                    const uint16_t* src = vbase + offset(lookup(t), t);
+                    if (!sees(p, place, t)) continue;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const VLoad w = *gbl(reinterpret_cast<const VLoad*>(src + (g * 4 + r) * kVw));
+#pragma unroll
+                        for (int m = 0; m < kVw; ++m) o[m][r] += other_part<T>(w[m / 2] >> (16 * (m & 1)));
+                    }
+                }
+            }
+        }
+        const float base = sm.base(p.c);
+        Vec8 pf;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
+            sm.l += w;
+            pf[j] = static_cast<T>(w);
+        }
+        // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
+#pragma unroll
+        for (int m = 0; m < kVw; ++m) {
+            u32x4 vf;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                vf[j] = __builtin_amdgcn_perm(s.v[2 * j + 1][m / 2], s.v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
+            o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf), pf, o[m]);
+        }
+    };
+
+    // Waves take steps in turn; a step's loads are in flight while the one
+    // before is computed.
+    {
+        int step = begin + wave;
+        if (step < end) {
+            Step<D> a, b;
+            Pages pg = pages_of(step);
+            load(a, step, pg);
+            pg = pages_of(min(step + kWaves, end - 1));
+            bool in_a = true;
+            while (step + kWaves < end) {
+                load(b, step + kWaves, pg);
+                pg = pages_of(min(step + 2 * kWaves, end - 1));
+                compute(a, step);
+                step += kWaves;
+                if (step + kWaves >= end) {
+                    in_a = false;
+                    break;
+                }
+                load(a, step + kWaves, pg);
+                pg = pages_of(min(step + 2 * kWaves, end - 1));
+                compute(b, step);
+                step += kWaves;
+            }
+            if (in_a) compute(a, step);
+            else compute(b, step);
+        }
+    }
+
+    // The waves' states are joined through LDS.  A wave that met a page outside
+    // the cache leaves a NaN sum.
+    float l = pair_sum<true>(pair_sum<false>(sm.l));
+    if (__builtin_amdgcn_ballot_w64(bad != 0)) l = NAN;
+    if (g == 0) {
+        sh_m[wave][i] = sm.m;
+        sh_l[wave][i] = l;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int m = 0; m < kVw; m += 4)
+            *reinterpret_cast<float4v*>(&sh_acc[wave][i][(g * 4 + r) * kVw + m]) = float4v{o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
+    __syncthreads();
+    for (int x = tid; x < rows * D; x += kThreads) {
+        const int r = x / D, d = x % D;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, sh_m[w][r]);
+        const float ms = m == -INFINITY ? 0.0f : m;
+        float sum = 0.0f, acc = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = sh_m[w][r] == -INFINITY ? 0.0f : exp2_((sh_m[w][r] - ms) * p.c);
+            sum += sh_l[w][r] == 0.0f ? 0.0f : sh_l[w][r] * f;
+            acc += sh_m[w][r] == -INFINITY ? 0.0f : sh_acc[w][r][d] * f;
+        }
+        if (un.count == 1) {
+            out_row(p, q, kvh, r, D)[d] = finish<T>(p, acc, sum);
+        } else {
+            const int64_t slot = ((int64_t)u * p.hkv + kvh) * p.few_slots + r;
+            p.few_acc[slot * D + d] = acc;
+            if (d == 0) p.few_ml[slot] = make_float2(m, sum);
+        }
+    }
+}
+
+// Joins `count` parts of one row; part i at slot base + i step.  256 threads.
+template <typename T, int D>
+__device__ __forceinline__ void merge_row(const Params& p, const float* acc, const float2* ml, int64_t base, int64_t step, int count, uint16_t* dst) {
+    constexpr int kCols = D / 4, kSlots = kThreads / kCols;
+    __shared__ float sh_m[kSlots], sh_l[kSlots];
+    __shared__ float4v sh_a[kSlots][kCols];
+    const int slot = threadIdx.x / kCols, col = threadIdx.x % kCols;
+    float m = -INFINITY, l = 0.0f;
+    float4v a = {0, 0, 0, 0};
+    constexpr int kBatch = 4;
+    for (int c0 = slot; c0 < count; c0 += kSlots * kBatch) {
+        float2 h[kBatch];
+        float4v v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t at = base + min(c0 + j * kSlots, count - 1) * step;
+            h[j] = ml[at];
+            v[j] = *reinterpret_cast<const float4v*>(acc + at * D + col * 4);
+        }
+        float to = m;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (c0 + j * kSlots < count) to = fmaxf(to, h[j].x);
+        const float ms = to == -INFINITY ? 0.0f : to;
+        const float f0 = m == -INFINITY ? 0.0f : exp2_((m - ms) * p.c);
+        l *= f0;
+        a *= f0;
+        m = to;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (c0 + j * kSlots >= count) continue;
+            if (h[j].y == 0.0f) continue;  // the part saw nothing
+            const float f = h[j].x == -INFINITY ? 1.0f : exp2_((h[j].x - ms) * p.c);
+            l = fmaf(h[j].y, f, l);
+            a += v[j] * f;
+        }
+    }
+    if (col == 0) {
+        sh_m[slot] = m;
+        sh_l[slot] = l;
+    }
+    sh_a[slot][col] = a;
+    __syncthreads();
+    if ((int)threadIdx.x < D) {
+        const float* col_a = reinterpret_cast<const float*>(&sh_a[0][0]) + threadIdx.x;
+        float top = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) top = fmaxf(top, sh_m[s]);
+        const float ms = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f, total = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s) {
+            if (sh_l[s] == 0.0f) continue;
+            const float f = sh_m[s] == -INFINITY ? 1.0f : exp2_((sh_m[s] - ms) * p.c);
+            sum = fmaf(sh_l[s], f, sum);
+            total = fmaf(col_a[s * D], f, total);
+        }
+        dst[threadIdx.x] = finish<T>(p, total, sum);
+    }
+}
+
+// One workgroup per (sequence, kv head, row).
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void few_merge_kernel(const Params p) {
+    const int kvh = blockIdx.x % p.hkv, r = blockIdx.x / p.hkv % p.few_slots, s = blockIdx.x / p.hkv / p.few_slots;
+    const Seq q = seq_of(p, s);
+    if (q.bad || !q.few(p) || r >= q.n * p.group) return;
+    // The sequence's first unit, found as the split finds a unit's sequence.
+    const int lane = threadIdx.x & 63;
+    int before = 0, total = 0;
+    for (int t = lane; t < p.num_seqs; t += 64) total += few_steps(p, t);
+    total = last_lane(inclusive_scan(total));
+    const int per = max(1, (total + p.units - p.num_seqs - 1) / (p.units - p.num_seqs));
+    for (int t = lane; t < s; t += 64) before += (few_steps(p, t) + per - 1) / per;
+    const int first = last_lane(inclusive_scan(before));
+    const int count = (few_steps(p, s) + per - 1) / per;
+    if (count <= 1) return;
+    merge_row<T, D>(p, p.few_acc, p.few_ml, ((int64_t)first * p.hkv + kvh) * p.few_slots + r, (int64_t)p.hkv * p.few_slots, count,
+                    out_row(p, q, kvh, r, D));
+}
+
+// ----------------------------------------------------------- many rows
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t addr) {
+    return *reinterpret_cast<__attribute__((address_space(3))) V*>((lds_u8*)(size_t)addr);
+}
+template <typename V>
+__device__ __forceinline__ void lds_write(uint32_t addr, V v) {
+    *reinterpret_cast<__attribute__((address_space(3))) V*>((lds_u8*)(size_t)addr) = v;
+}
+// Four 16-bit values of a 4 x 16 block of each 16-lane group, turned: lane 4 r +
+// c reads values 4 c .. 4 c + 3 of row r, lane i gets value i of rows 0 .. 3.
+__device__ __forceinline__ u32x2 lds_read_turned(uint32_t addr) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(lds_u8*)(size_t)addr));
+}
+
+// 16 bytes per lane from memory straight into LDS, lane after lane.  Written out
+// because the compiler puts a wait for every load in flight before any LDS read
+// that follows its own form; the waits are written out too.
+__device__ __forceinline__ void dma16(const uint16_t* src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void dma_done_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Tiles in LDS: a token's D values are 16-byte pieces, piece c at place c ^ s(t).
+// The places are chosen by permuting which piece each lane fetches.
+//   keys    16 consecutive lanes read the same piece of 16 tokens: s spreads
+//           them over all banks;
+//   values  32 lanes read 64 bytes of each of 4 tokens: s moves each token's to
+//           banks of its own.
+template <int D>
+__device__ __forceinline__ int key_place(int t) {
+    return D == 128 ? t & 15 : t >> 1 & 7;
+}
+template <int D>
+__device__ __forceinline__ int value_place(int t) {
+    return D == 128 ? (t & 3) << 2 : (t >> 1 & 1) << 2;
+}
+
+// Workgroups: kv heads fastest (each XCD then has its own, whose keys and
+// values stay in its L2), then splits, then row tiles.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
+    using Vec8 = typename Type<T>::Vec8;
+    constexpr int kKs = D / 16;                      // key pieces of 16 dims
+    constexpr int kDt = D / 32;                      // output tiles of 32 dims
+    constexpr int kPieces = D / 8;                   // 16-byte pieces of a token
+    constexpr uint32_t kTileBytes = kTileTokens * D * 2;
+    constexpr int kLoads = kTileBytes / 16 / kThreads;  // per lane and array
+    constexpr int kTokensPerLoad = 64 / kPieces;        // of one wave
+    __shared__ __align__(16) uint8_t sh_tiles[2][2][kTileBytes];
+    __shared__ unsigned long long sh_partly[2];
+
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % p.hkv, split = blockIdx.x / p.hkv % p.splits;
+    int tile = blockIdx.x / p.hkv / p.splits;
+
+    // The sequence of this row tile.
+    int s = -1;
+    for (int s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        int n = 0;
+        if (s0 + lane < p.num_seqs) {
+            const Seq q = seq_of(p, s0 + lane);
+            n = q.few(p) ? 0 : (q.n * p.group + kTileRows - 1) / kTileRows;
+        }
+        const int inc = inclusive_scan(n);
+        const uint64_t owner = __builtin_amdgcn_ballot_w64(tile >= inc - n && tile < inc);
+        if (owner) {
+            const int j = __builtin_ctzll(owner);
+            s = s0 + j;
+            tile -= __builtin_amdgcn_readlane(inc - n, j);
+            break;
+        }
+        tile -= last_lane(inc);
+    }
+    if (s < 0) return;
+    s = __builtin_amdgcn_readfirstlane(s);
+    const Seq q = seq_of(p, s);
+    const int all_rows = q.n * p.group;
+    // The last tiles, which see most, first.
+    const int row0 = ((all_rows + kTileRows - 1) / kTileRows - 1 - tile) * kTileRows;
+    const int rows = min(kTileRows, all_rows - row0);
+    if (q.bad) {
+        if (split == 0)
+            for (int x = tid; x < rows * D; x += kThreads) out_row(p, q, kvh, row0 + x / D, D)[x % D] = Type<T>::kNaN;
+        return;
+    }
+    const int lo = q.len - q.n + row0 / p.group, hi = q.len - q.n + (row0 + rows - 1) / p.group;  // positions of the rows
+    const Tiles<kTileTokens> tiles(p, lo, hi);
+    const int begin = (int)((int64_t)tiles.count * split / p.splits), end = (int)((int64_t)tiles.count * (split + 1) / p.splits);
+
+    const int row = row0 + wave * 32 + i;  // the lane's
+    const bool row_ok = row < all_rows;
+    const int clamped = min(row, all_rows - 1);
+    const int place = q.len - q.n + clamped / p.group;
+    Vec8 qf[kKs];
+    {
+        const uint16_t* src = p.q + (int64_t)(q.first + clamped / p.group) * p.q_stride + (int64_t)(kvh * p.group + clamped % p.group) * D + h * 8;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            u32x4 w = *gbl(reinterpret_cast<const u32x4*>(src + ks * 16));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (w[e] & p.q_and) ^ p.q_xor;
+            qf[ks] = __builtin_bit_cast(Vec8, w);
+        }
+    }
+
+    const int32_t* trow = p.table + (int64_t)s * p.max_pages;
+    const int page_mask = (1 << p.log2_page) - 1;
+    const uint16_t* kbase = p.k + ((int64_t)kvh << p.log2_page) * D;
+    const uint16_t* vbase = p.v + ((int64_t)kvh << p.log2_page) * D;
+    const uint32_t lds0 = (uint32_t)(size_t)(lds_u8*)&sh_tiles[0][0][0];
+    int bad = 0;
+
+    auto used = [&](int t) { return t <= hi && (t < p.sinks || t >= tiles.first); };
+    auto checked = [&](int page) {
+        if ((uint32_t)page < (uint32_t)p.num_pages) return page;
+        bad = 1;
+        return 0;
+    };
+    // A wave fetches 16 tokens of a tile.  With 16 or more to a page they share
+    // one page, whose number is a scalar load.
+    auto fetch = [&](int step, int buffer) {
+        const int t0 = tiles.token(step) + wave * 16;
+        const uint32_t kdst = lds0 + (buffer * 2) * kTileBytes + wave * (kTileBytes / kWaves);
+        int one = 0;
+        if (p.log2_page >= 4) {
+            const bool any = t0 <= hi && (t0 < p.sinks || t0 + 15 >= tiles.first);
+            if (any) one = checked(((const __attribute__((address_space(4))) int32_t*)trow)[__builtin_amdgcn_readfirstlane(t0 >> p.log2_page)]);
+        }
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int in = j * kTokensPerLoad + lane / kPieces, t = t0 + in, tt = wave * 16 + in;
+            int page = one;
+            if (p.log2_page < 4) page = used(t) ? checked(trow[t >> p.log2_page]) : 0;
+            const int64_t off = (int64_t)page * p.page_stride + (int64_t)(t & page_mask) * D;
+            const int piece = lane % kPieces;
+            dma16(kbase + off + (piece ^ key_place<D>(tt)) * 8, kdst + j * 1024);
+            dma16(vbase + off + (piece ^ value_place<D>(tt)) * 8, kdst + kTileBytes + j * 1024);
+        }
+    };
+
+    float16v o[kDt];
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
+    Softmax sm;
+    if (tid < 2) sh_partly[tid] = 0;
+
+    const uint32_t krow = lds0 + i * (D * 2);
+    const int vr = (lane & 15) >> 2, vd = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;  // row of 4 and dim that the lane reads for a turned load
+
+    if (begin < end) fetch(begin, 0);
+    for (int step = begin; step < end; ++step) {
+        const int buffer = (step - begin) & 1;
+        const int t0 = tiles.token(step);
+        dma_done_and_barrier();  // the tile is there, and the other buffer no longer read
+        if (step + 1 < end) fetch(step + 1, buffer ^ 1);
+        const uint32_t kt = krow + (buffer * 2) * kTileBytes, vt = lds0 + (buffer * 2 + 1) * kTileBytes;
+
+        const int tl = t0 + kTileTokens - 1;
+        const bool all = tl <= lo && (tl < p.sinks || t0 > hi - p.window);  // every row sees every token
+        unsigned long long partly = 0;
+        if (!all) {
+            // Values that no row sees are cleared, and so is what is not finite of
+            // tokens that only some rows see: 0 times it would not be 0.
+#pragma unroll
+            for (int j = 0; j < kTileTokens * kPieces / kThreads; ++j) {
+                const int x = j * kThreads + tid, t = t0 + x / kPieces;
+                if (t <= lo && (t < p.sinks || t > hi - p.window)) continue;
+                const bool any = used(t);
+                const u32x4 w = lds_read<u32x4>(vt + x * 16);
+                u32x4 f;
+                bool same = true;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f[e] = any ? finite_part<T>(w[e]) : 0u;
+                    same = same && f[e] == w[e];
+                }
+                if (same) continue;
+                lds_write(vt + x * 16, f);
+                if (any) atomicOr(&sh_partly[buffer], 1ull << (x / kPieces));
+            }
+            lds_barrier();
+            partly = sh_partly[buffer];
+        }
+        if (tid == 0) sh_partly[buffer ^ 1] = 0;  // read last before the barrier above, written next after the one to come
+
+        float16v st[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[tt][r] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) {
+                const u32x4 w = lds_read<u32x4>(kt + tt * 32 * (D * 2) + ((2 * ks + h) ^ key_place<D>(i)) * 16);
+                st[tt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, w), qf[ks], st[tt]);
+            }
+        }
+        if (!all) {
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!sees(p, place, t0 + tt * 32 + 8 * (r / 4) + 4 * h + r % 4)) st[tt][r] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[tt][r]);
+        mx = pair_max<true>(mx);
+        float f;
+        if (sm.advance(mx, p.c, f)) {
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt) o[dt] *= f;
+        }
+        // What is not finite goes to the rows that see it, token by token.
+                    while (partly) {
+            const int x = __builtin_ctzll(partly), t = t0 + x;
+            partly &= partly - 1;
+            const uint16_t* src = vbase + (int64_t)checked(trow[t >> p.log2_page]) * p.page_stride + (int64_t)(t & page_mask) * D;
+            if (!sees(p, place, t)) continue;
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const u32x2 w = *gbl(reinterpret_cast<const u32x2*>(src + dt * 32 + 8 * r4 + 4 * h));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[dt][4 * r4 + r] += other_part<T>(w[r / 2] >> (16 * (r & 1)));
+                }
+        }
+        const float base = sm.base(p.c);
+        Vec8 pf[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float w = exp2_(fmaf(st[x / 2][(x & 1) * 8 + j], p.c, -base));
+                sm.l += w;
+                pf[x][j] = static_cast<T>(w);
+            }
+        // Product x takes tokens 16 x + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                u32x4 w;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int t = x * 16 + half * 8 + h * 4 + vr, d = dt * 32 + vd;
+                    const u32x2 two = lds_read_turned(vt + t * (D * 2) + ((d / 8) ^ value_place<D>(t)) * 16 + (d & 4) * 2);
+                    w[2 * half] = two.x;
+                    w[2 * half + 1] = two.y;
+                }
+                o[dt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, w), pf[x], o[dt]);
+            }
+    }
+
+    float l = pair_sum<true>(sm.l);
+    // A page outside the cache, met by any wave: the sum of every row is NaN.
+    lds_barrier();
+    if (tid == 0) sh_partly[0] = 0;
+    lds_barrier();
+    if (bad) sh_partly[0] = 1;
+    lds_barrier();
+    if (sh_partly[0]) l = NAN;
+    if (!row_ok) return;
+    if (p.splits == 1) {
+        uint16_t* dst = out_row(p, q, kvh, row, D);
+        const bool blind = p.window == 0 && p.sinks == 0;
+        const float inv = 1.0f / l;
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                uint16_t e[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) e[r] = l != l ? Type<T>::kNaN : blind ? 0 : bits_of<T>(o[dt][r4 * 4 + r] * inv);
+                u32x2 w = {(uint32_t)e[0] | (uint32_t)e[1] << 16, (uint32_t)e[2] | (uint32_t)e[3] << 16};
+                *gbl(reinterpret_cast<u32x2*>(dst + dt * 32 + r4 * 8 + h * 4)) = w;
+            }
+    } else {
+        const int64_t slot = ((int64_t)(q.first + row / p.group) * p.hq + kvh * p.group + row % p.group) * p.splits + split;
+        float* dst = p.tile_acc + slot * D;
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4)
+                *reinterpret_cast<float4v*>(dst + dt * 32 + r4 * 8 + h * 4) =
+                    float4v{o[dt][r4 * 4], o[dt][r4 * 4 + 1], o[dt][r4 * 4 + 2], o[dt][r4 * 4 + 3]};
+        if (h == 0) p.tile_ml[slot] = make_float2(sm.m, l);
+    }
+}
+
+// One workgroup per (token, query head) of the sequences that tile_kernel took.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void tile_merge_kernel(const Params p) {
+    const int head = blockIdx.x % p.hq, token = blockIdx.x / p.hq, lane = threadIdx.x & 63;
+    // The sequence: the last one that starts at or before the token.
+    int s = -1;
+    for (int s0 = 0; s0 < p.num_seqs; s0 += 64) {
+        bool mine = false;
+        if (s0 + lane < p.num_seqs) {
+            const Seq q = seq_of(p, s0 + lane);
+            mine = token >= q.first && token < q.first + q.n && !q.few(p) && !q.bad;
+        }
+        const uint64_t m = __builtin_amdgcn_ballot_w64(mine);
+        if (m) {
+            s = s0 + __builtin_ctzll(m);
+            break;
+        }
+    }
+    if (s < 0) return;
+    merge_row<T, D>(p, p.tile_acc, p.tile_ml, ((int64_t)token * p.hq + head) * p.splits, 1, p.splits,
+                    p.out + (int64_t)token * p.out_stride + (int64_t)head * D);
+}
+
+// ------------------------------------------------------------------ host
+
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Plan {
+    bool few, tiles;
+    int64_t units, few_slots, row_tiles, splits;
+    size_t few_acc, few_ml, tile_acc, tile_ml, total;  // offsets of the parts of the workspace
+};
+
+Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_t hkv, int64_t dim, int64_t max_len, int64_t window, int64_t sinks) {
+    Plan pl{};
+    const int64_t group = hq / hkv;
+    pl.tiles = max_query * group > kFewRows;
+    pl.few = !(pl.tiles && seqs == 1 && tokens * group > kFewRows);
+    // Tokens that a sequence's few new ones see at most.
+    const int64_t few_query = std::min(max_query, std::max<int64_t>(1, kFewRows / group));
+    const int64_t steps = ceil_div(std::min(max_len, sinks + window + few_query), kFewTokens) + 2;
+    pl.few_slots = std::min<int64_t>(kFewRows, max_query * group);
+    pl.units = seqs;
+    if (steps > 16 && seqs * hkv < 1024) {
+        const int64_t want = std::max(ceil_div(768, hkv), 2 * seqs);
+        pl.units = std::max(std::min(want, seqs * ceil_div(steps, kWaves)), seqs + 1);
+    }
+    pl.row_tiles = std::min(ceil_div(tokens * group, kTileRows) + seqs, seqs * ceil_div(std::min(max_query, tokens) * group, kTileRows));
+    const int64_t groups = ceil_div(tokens * group, kTileRows) * hkv;
+    const int64_t seen = ceil_div(std::min(max_len, sinks + window + kTileRows / group + 1), kTileTokens) + 1;
+    pl.splits = groups >= 384 ? 1 : std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, groups), seen / 4, 32}));
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t here = at;
+        at += (size_t)ceil_div(bytes, 16) * 16;
+        return here;
+    };
+    const int64_t few_parts = pl.few && pl.units > seqs ? pl.units * hkv * pl.few_slots : 0;
+    const int64_t tile_parts = pl.tiles && pl.splits > 1 ? tokens * hq * pl.splits : 0;
+    pl.few_acc = take(few_parts * dim * 4);
+    pl.few_ml = take(few_parts * 8);
+    pl.tile_acc = take(tile_parts * dim * 4);
+    pl.tile_ml = take(tile_parts * 8);
+    pl.total = at;
+    return pl;
+}
+
+wq_status check_sizes(const char* fn, int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_t hkv, int64_t dim, int64_t max_len,
+                      int64_t window, int64_t sinks) {
+    WQ_TRY(in_range(fn, "num_seqs", seqs, 1, WQ_WINDOW_MAX_SEQS));
+    WQ_TRY(in_range(fn, "num_tokens", tokens, 1, WQ_WINDOW_MAX_TOKENS));
+    WQ_TRY(in_range(fn, "max_query_len", max_query, 1, tokens));
+    WQ_TRY(in_range(fn, "num_kv_heads", hkv, 1, WQ_WINDOW_MAX_KV_HEADS));
+    if (hq < 1 || hq % hkv != 0)
+        return err(WQ_ERR_INVALID_ARG, "%s: num_q_heads (%lld) must be a positive multiple of num_kv_heads (%lld)", fn, (long long)hq, (long long)hkv);
+    if (hq / hkv > WQ_WINDOW_MAX_GROUP)
+        return err(WQ_ERR_UNSUPPORTED, "%s: at most %d query heads per kv head (got %lld)", fn, WQ_WINDOW_MAX_GROUP, (long long)(hq / hkv));
+    if (dim != 64 && dim != 128) return err(WQ_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128 (got %lld)", fn, (long long)dim);
+    WQ_TRY(in_range(fn, "max_seq_len", max_len, 1, WQ_WINDOW_MAX_SEQ_LEN));
+    WQ_TRY(in_range(fn, "window", window, 0, (int64_t)1 << 30));
+    WQ_TRY(in_range(fn, "sinks", sinks, 0, (int64_t)1 << 30));
+    const Plan pl = plan_of(seqs, tokens, max_query, hq, hkv, dim, max_len, window, sinks);
+    if (pl.units * hkv > INT32_MAX || seqs * pl.few_slots * hkv > INT32_MAX || pl.row_tiles * pl.splits * hkv > INT32_MAX || tokens * hq > INT32_MAX)
+        return err(WQ_ERR_INVALID_ARG, "%s: too many workgroups for one launch", fn);
+    return WQ_OK;
+}
+
+template <typename T, int D>
+hipError_t launch(const Params& p, const Plan& pl, hipStream_t stream) {
+    if (pl.tiles) {
+        hipLaunchKernelGGL((tile_kernel<T, D>), dim3((unsigned)(pl.row_tiles * pl.splits * p.hkv)), dim3(kThreads), 0, stream, p);
+        if (pl.splits > 1) hipLaunchKernelGGL((tile_merge_kernel<T, D>), dim3((unsigned)(p.num_tokens * p.hq)), dim3(kThreads), 0, stream, p);
+    }
+    if (pl.few) {
+        hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(p.units * p.hkv)), dim3(kThreads), 0, stream, p);
+        if (p.units > p.num_seqs)
+            hipLaunchKernelGGL((few_merge_kernel<T, D>), dim3((unsigned)(p.num_seqs * p.few_slots * p.hkv)), dim3(kThreads), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace window
+}  // namespace wq
+
+using namespace wq::window;
+using wq::host::aligned;
+using wq::host::err;
+using wq::host::in_range;
+using wq::host::overlaps;
+using wq::host::span;
+using wq::host::Span;
+
+extern "C" {
+
+wq_status wq_window_attention_workspace_size(int64_t num_seqs, int64_t num_tokens, int64_t max_query_len, int64_t num_q_heads,
+                                             int64_t num_kv_heads, int64_t head_dim, int64_t max_seq_len, int64_t window, int64_t sinks,
+                                             size_t* bytes) {
+    static const char* fn = "wq_window_attention_workspace_size";
+    if (!bytes) return err(WQ_ERR_INVALID_ARG, "%s: null output pointer", fn);
+    WQ_TRY(check_sizes(fn, num_seqs, num_tokens, max_query_len, num_q_heads, num_kv_heads, head_dim, max_seq_len, window, sinks));
+    *bytes = plan_of(num_seqs, num_tokens, max_query_len, num_q_heads, num_kv_heads, head_dim, max_seq_len, window, sinks).total;
+    return WQ_OK;
+}
+
+wq_status wq_window_attention(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache, const int32_t* block_table,
+                              const int32_t* seq_lens, const int32_t* q_starts, uint16_t* out, int64_t num_seqs, int64_t num_tokens,
+                              int64_t max_query_len, int64_t num_q_heads, int64_t num_kv_heads, int64_t head_dim, int64_t q_stride,
+                              int64_t out_stride, int64_t page_size, int64_t num_pages, int64_t max_pages_per_seq, int64_t max_seq_len,
+                              int64_t window, int64_t sinks, float scale, int64_t dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    static const char* fn = "wq_window_attention";
+    if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !out) return err(WQ_ERR_INVALID_ARG, "%s: null pointer", fn);
+    WQ_TRY(check_sizes(fn, num_seqs, num_tokens, max_query_len, num_q_heads, num_kv_heads, head_dim, max_seq_len, window, sinks));
+    if (!wq::host::is_pow2(page_size) || page_size > WQ_WINDOW_MAX_PAGE_SIZE)
+        return err(WQ_ERR_UNSUPPORTED, "%s: page_size must be a power of two in [1, %d] (got %lld)", fn, WQ_WINDOW_MAX_PAGE_SIZE, (long long)page_size);
+    if (dtype != WQ_DTYPE_F16 && dtype != WQ_DTYPE_BF16)
+        return err(WQ_ERR_UNSUPPORTED, "%s: dtype must be WQ_DTYPE_F16 or WQ_DTYPE_BF16 (got %lld)", fn, (long long)dtype);
+    WQ_TRY(in_range(fn, "num_pages", num_pages, 1, INT32_MAX));
+    WQ_TRY(in_range(fn, "max_pages_per_seq", max_pages_per_seq, 1, INT32_MAX));
+    if (!q_starts && (num_tokens != num_seqs || max_query_len != 1))
+        return err(WQ_ERR_INVALID_ARG, "%s: without q_starts there is one new token per sequence (%lld tokens, %lld sequences, max_query_len %lld)", fn,
+                   (long long)num_tokens, (long long)num_seqs, (long long)max_query_len);
+    const int64_t row = num_q_heads * head_dim;
+    for (const int64_t stride : {q_stride, out_stride})
+        if (stride < row || stride % 8 != 0 || stride > ((int64_t)1 << 32))
+            return err(WQ_ERR_INVALID_ARG, "%s: strides must be multiples of 8 of at least num_q_heads * head_dim (got %lld)", fn, (long long)stride);
+    if (!std::isfinite(scale)) return err(WQ_ERR_INVALID_ARG, "%s: scale must be finite", fn);
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+        return err(WQ_ERR_MISALIGNED, "%s: q, out, k_cache and v_cache must be 16-byte aligned", fn);
+    if (!aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(q_starts, 4))
+        return err(WQ_ERR_MISALIGNED, "%s: block_table, seq_lens and q_starts must be 4-byte aligned", fn);
+
+    const Plan pl = plan_of(num_seqs, num_tokens, max_query_len, num_q_heads, num_kv_heads, head_dim, max_seq_len, window, sinks);
+    if (pl.total > 0) {
+        if (!workspace || workspace_bytes < pl.total)
+            return err(WQ_ERR_INVALID_ARG, "%s: a workspace of %zu bytes is needed (got %zu)", fn, pl.total, workspace ? workspace_bytes : (size_t)0);
+        if (!aligned(workspace, 16)) return err(WQ_ERR_MISALIGNED, "%s: workspace must be 16-byte aligned", fn);
+    }
+    const uint64_t cache_bytes = (uint64_t)num_pages * num_kv_heads * page_size * head_dim * 2;
+    const Span so = span(out, ((uint64_t)(num_tokens - 1) * out_stride + row) * 2), sw = span(workspace, pl.total);
+    const Span inputs[] = {span(q, ((uint64_t)(num_tokens - 1) * q_stride + row) * 2), span(k_cache, cache_bytes), span(v_cache, cache_bytes),
+                           span(block_table, (uint64_t)num_seqs * max_pages_per_seq * 4), span(seq_lens, (uint64_t)num_seqs * 4),
+                           span(q_starts, q_starts ? (uint64_t)(num_seqs + 1) * 4 : 0)};
+    for (const Span& in : inputs) {
+        if (overlaps(so, in)) return err(WQ_ERR_INVALID_ARG, "%s: out overlaps an input", fn);
+        if (overlaps(sw, in)) return err(WQ_ERR_INVALID_ARG, "%s: the workspace overlaps an input", fn);
+    }
+    if (overlaps(so, sw)) return err(WQ_ERR_INVALID_ARG, "%s: out overlaps the workspace", fn);
+
+    Params p{};
+    p.q = q;
+    p.k = k_cache;
+    p.v = v_cache;
+    p.table = block_table;
+    p.lens = seq_lens;
+    p.starts = q_starts;
+    p.out = out;
+    p.max_pages = max_pages_per_seq;
+    p.q_stride = q_stride;
+    p.out_stride = out_stride;
+    p.page_stride = num_kv_heads * page_size * head_dim;
+    p.num_seqs = (int32_t)num_seqs;
+    p.num_tokens = (int32_t)num_tokens;
+    p.max_query = (int32_t)max_query_len;
+    p.num_pages = (int32_t)num_pages;
+    p.hq = (int32_t)num_q_heads;
+    p.hkv = (int32_t)num_kv_heads;
+    p.group = (int32_t)(num_q_heads / num_kv_heads);
+    p.log2_page = wq::host::log2_of(page_size);
+    p.max_seq_len = (int32_t)max_seq_len;
+    p.window = (int32_t)window;
+    p.sinks = (int32_t)sinks;
+    p.c = scale == 0.0f ? 1.0f : (float)(std::fabs((double)scale) * 1.4426950408889634);  // log2(e)
+    p.q_and = scale == 0.0f ? 0u : ~0u;
+    p.q_xor = scale < 0.0f ? 0x80008000u : 0u;
+    p.units = (int32_t)pl.units;
+    p.few_slots = (int32_t)pl.few_slots;
+    char* ws = static_cast<char*>(workspace);
+    p.few_acc = reinterpret_cast<float*>(ws + pl.few_acc);
+    p.few_ml = reinterpret_cast<float2*>(ws + pl.few_ml);
+    p.splits = (int32_t)pl.splits;
+    p.tile_acc = reinterpret_cast<float*>(ws + pl.tile_acc);
+    p.tile_ml = reinterpret_cast<float2*>(ws + pl.tile_ml);
+    p.tiles_too = pl.tiles;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    (void)hipGetLastError();
+    hipError_t e;
+    if (dtype == WQ_DTYPE_F16) e = head_dim == 128 ? launch<_Float16, 128>(p, pl, st) : launch<_Float16, 64>(p, pl, st);
+    else e = head_dim == 128 ? launch<__bf16, 128>(p, pl, st) : launch<__bf16, 64>(p, pl, st);
+    return wq::host::hip_result(fn, e);
+}
+
+}  // extern "C"

@@ -32,7 +32,8 @@ EXPORTED = ("wq_status_string", "wq_last_error_message", "wq_version", "wq_pack"
             "wq_decode_linears", "wq_decode_linears_noalloc", "wq_paged_attention_workspace_size",
             "wq_paged_attention", "wq_fused_linears", "wq_fused_check", "wq_stream_read",
             "wq_cache_append", "wq_cache_copy_pages", "wq_page_workspace_size", "wq_cache_reserve", "wq_cache_free",
-            "wq_cache_fork", "wq_cache_compact", "wq_process_logits_workspace_size", "wq_process_logits")
+            "wq_cache_fork", "wq_cache_compact", "wq_process_logits_workspace_size", "wq_process_logits",
+            "wq_window_attention_workspace_size", "wq_window_attention")
 
 # Limits of wq_decode_linears_noalloc (include/wq.h).
 NOALLOC_MAX_LINEARS = 1024
@@ -130,7 +131,9 @@ def lib() -> ctypes.CDLL:
             ("wq_cache_fork", [vp, i64] + [vp] * 5 + [i64] * 7 + [vp, vp, sz, vp]),
             ("wq_cache_compact", [vp, i64, i64] + [vp] * 5 + [i64] * 3 + [vp, sz, vp]),
             ("wq_process_logits_workspace_size", [i64, i64, i64, ctypes.POINTER(sz)]),
-            ("wq_process_logits", [vp, vp, sz, vp])):
+            ("wq_process_logits", [vp, vp, sz, vp]),
+            ("wq_window_attention_workspace_size", [i64] * 9 + [ctypes.POINTER(sz)]),
+            ("wq_window_attention", [vp] * 7 + [i64] * 14 + [ctypes.c_float, i64, vp, sz, vp])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -373,6 +376,61 @@ def wq_fused_check(device=None, stream=None) -> None:
 
     stream = torch.cuda.current_stream(device) if stream is None else stream
     _check(lib().wq_fused_check(stream.cuda_stream))
+
+
+# ------------------------------------------------------- window attention
+
+def window_attention_workspace_size(num_seqs: int, num_tokens: int, max_query_len: int, num_q_heads: int, num_kv_heads: int,
+                                    head_dim: int, max_seq_len: int, window: int, sinks: int) -> int:
+    """Bytes of device workspace wq_window_attention needs (0: none)."""
+    out = ctypes.c_size_t(0)
+    _check(lib().wq_window_attention_workspace_size(num_seqs, num_tokens, max_query_len, num_q_heads, num_kv_heads, head_dim,
+                                                    max_seq_len, window, sinks, ctypes.byref(out)))
+    return int(out.value)
+
+
+def window_workspace(q, num_kv_heads: int, num_seqs: int, max_seq_len: int, window: int, sinks: int = 0, max_query_len: int = 1):
+    """A device workspace (uint8 tensor, or None) for window_attention."""
+    import torch
+
+    n = window_attention_workspace_size(num_seqs, q.shape[0], max_query_len, q.shape[1], num_kv_heads, q.shape[2], max_seq_len, window, sinks)
+    return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+
+
+def window_attention(q, k_cache, v_cache, block_table, seq_lens, out, scale: float, max_seq_len: int, window: int, sinks: int = 0,
+                     q_starts=None, max_query_len: int = 1, workspace=None, stream=None) -> None:
+    """out [T, HQ, D] = causal attention of the new tokens' queries q [T, HQ, D]
+    over the paged caches [pages, HKV, P, D] (all fp16 or all bf16): a token at
+    position p sees token t <= p when t < sinks or t > p - window.  seq_lens [S]
+    counts the new tokens; rows q_starts[s] to q_starts[s + 1] (int32, [S + 1],
+    at most max_query_len of them) belong to the last tokens of sequence s, or
+    row s to its last one when q_starts is None.  Rows of q and out may lie
+    apart (slices of a wider array).  `workspace` is from window_workspace
+    (allocated here when omitted)."""
+    _torch or _load_torch()
+    num_pages, hkv, page, d = _cache_dims(k_cache, "k_cache")
+    kind = k_cache.dtype
+    if q.dim() != 3 or block_table.dim() != 2:
+        raise ValueError("q must be [T, HQ, D] and block_table [S, max_pages]")
+    if kind not in _DTYPES:
+        raise TypeError(f"the caches must be fp16 or bf16 (got {kind})")
+    shape = q.shape
+    num_seqs, max_pages = block_table.shape
+    if shape[2] != d:
+        raise ValueError(f"q has head_dim {shape[2]}, the caches {d}")
+    pq, qs = _rows_tensor(q, "q", kind, shape)
+    po, os_ = _rows_tensor(out, "out", kind, shape)
+    pk = _dev_tensor(k_cache, "k_cache", (kind,), k_cache.shape)
+    pv = _dev_tensor(v_cache, "v_cache", (kind,), k_cache.shape)
+    pt = _dev_tensor(block_table, "block_table", _INTS, (num_seqs, max_pages))
+    pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
+    ps = None if q_starts is None else _dev_tensor(q_starts, "q_starts", _INTS, (num_seqs + 1,))
+    if workspace is None:
+        workspace = window_workspace(q, hkv, num_seqs, max_seq_len, window, sinks, max_query_len)
+    pw, nw = _workspace(workspace, q)
+    _check((_lib or lib()).wq_window_attention(pq, pk, pv, pt, pl, ps, po, num_seqs, shape[0], max_query_len, shape[1], hkv, d, qs, os_, page,
+                                               num_pages, max_pages, max_seq_len, window, sinks, float(scale), _DTYPES[kind], pw, nw,
+                                               _stream(stream, q)))
 
 
 # ------------------------------------------------------- paged cache upkeep
