@@ -154,7 +154,7 @@ struct Tiles {
         first = max(0, lo - p.window + 1);
         start = first & ~(TOKENS - 1);
         sink_tiles = (min(p.sinks, start) + TOKENS - 1) / TOKENS;
-        count = sink_tiles + (hi - start + TOKENS) / TOKENS;
+        count = p.window > 0 || p.sinks > 0 ? sink_tiles + (hi - start + TOKENS) / TOKENS : 0;
     }
     __device__ __forceinline__ int token(int tile) const { return tile < sink_tiles ? tile * TOKENS : start + (tile - sink_tiles) * TOKENS; }
 };
@@ -302,19 +302,20 @@ __device__ __forceinline__ uint16_t finish(const Params& p, float acc, float l) 
 // The matrix cores' row i of key tile a is then token 8 (i / 4) + 4 a + i % 4, so
 // that they leave the scores of tokens 8 g + 4 a + r in lane group g: the
 // tokens whose values it holds.
-template <int D>
-struct Step {
-    static constexpr int kKs = D / 32, kVw = D / 16;
-    typedef uint32_t VLoad __attribute__((ext_vector_type(kVw / 2)));
-    u32x4 k[2][kKs];
-    VLoad v[8];
-};
-
-template <typename T, int D>
+//
+// Keys are fetched again as soon as the scores are formed and values as soon as
+// they are weighted, so a wave always has between half a step and a whole one
+// (16 KB at head_dim 128) in flight, in one set of registers.  Every path
+// issues the same loads (past the last step, of one row again), so that the
+// waits that the compiler counts stay exact; the table entries of a step are
+// asked for before the loads of the one ahead of it, so that waiting for them
+// waits for no key or value.
+// WHOLE: pages of 8 tokens or more, so that 8 aligned tokens share one.
+template <typename T, int D, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 2) void few_kernel(const Params p) {
     using Vec8 = typename Type<T>::Vec8;
-    constexpr int kKs = Step<D>::kKs, kVw = Step<D>::kVw;
-    using VLoad = typename Step<D>::VLoad;
+    constexpr int kKs = D / 32, kVw = D / 16;
+    typedef uint32_t VLoad __attribute__((ext_vector_type(kVw / 2)));
     __shared__ float sh_acc[kWaves][kFewRows][D];
     __shared__ float sh_m[kWaves][kFewRows], sh_l[kWaves][kFewRows];
 
@@ -349,61 +350,65 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const Params p) {
 
     const int32_t* trow = p.table + (int64_t)un.seq * p.max_pages;
     const int page_mask = (1 << p.log2_page) - 1;
-    const bool whole = p.log2_page >= 3;  // 8 aligned tokens share a page
-    const uint16_t* kbase = p.k + ((int64_t)kvh << p.log2_page) * D;
-    const uint16_t* vbase = p.v + ((int64_t)kvh << p.log2_page) * D;
+    const uint16_t* kbase = p.k + ((int64_t)kvh << p.log2_page) * D + g * 8;
+    const uint16_t* vbase = p.v + ((int64_t)kvh << p.log2_page) * D + i * kVw;
     int bad = 0;
 
-    // Visible to some row: only the pages of such tokens are looked up; others
-    // stand for page 0 and are masked.
+    // Visible to some row.  Only pages of such tokens are looked up: a token that
+    // is not stands for `safe`, which is, and is masked.
     auto used = [&](int t) { return t <= last && (t < p.sinks || t >= tiles.first); };
-    auto lookup = [&](int t) { return used(t) ? trow[t >> p.log2_page] : 0; };
-    // Element offset of token t in a kv head's part of the cache.
-    auto offset = [&](int page, int t) {
-        if ((uint32_t)page >= (uint32_t)p.num_pages) {
-            bad = 1;
-            page = 0;
-        }
-        return (int64_t)page * p.page_stride + (int64_t)(t & page_mask) * D;
+    const int safe = p.window > 0 ? last : 0;
+    auto lookup = [&](int t) { return trow[t >> p.log2_page]; };
+    auto checked = [&](int page) {
+        bad |= (uint32_t)page >= (uint32_t)p.num_pages;
+        return (uint32_t)page >= (uint32_t)p.num_pages ? 0 : page;
     };
-    // The table entries of a step; those of the next step are fetched while one
-    // is loaded, so that no load waits for them.
+    auto offset = [&](int page, int t) { return (int64_t)page * p.page_stride + (int64_t)((t & page_mask) * D); };
+    // The token of a lane's keys in step t0 (t0 < 0: past the last step), and the
+    // first of its values.  Of a group of 8 in one page, the first used token
+    // stands for all.
+    auto key_token = [&](int t0, int a) { return t0 + (i >> 2) * 8 + a * 4 + (i & 3); };
+    auto page_token = [&](int t) { return t < p.sinks ? t : max(t, tiles.first); };
     struct Pages {
-        int k[2], v;
+        int k[2], v[8];
     };
-    auto pages_of = [&](int step) {
-        const int t0 = tiles.token(step);
-        Pages pg{};
-        const int kt = t0 + (i >> 2) * 8, vt = t0 + g * 8;
-        if (whole) {
-            // A group of 8 has one page: that of its first used token.
-            auto of_group = [&](int t) { return lookup(min(t < p.sinks ? t : max(t, tiles.first), t + 7)); };
-            pg.k[0] = pg.k[1] = of_group(kt);
-            pg.v = of_group(vt);
+    auto or_safe = [&](int t0, int t) { return t0 >= 0 && used(t) ? t : safe; };
+    auto pages_of = [&](int t0) {
+        Pages pg;
+        if constexpr (WHOLE) {
+            const int kt = t0 + (i >> 2) * 8, vt = t0 + g * 8;
+            pg.k[0] = lookup(or_safe(t0, min(page_token(kt), kt + 7)));
+            pg.v[0] = lookup(or_safe(t0, min(page_token(vt), vt + 7)));
         } else {
-            pg.k[0] = lookup(kt + (i & 3));
-            pg.k[1] = lookup(kt + 4 + (i & 3));
+            for (int a = 0; a < 2; ++a) pg.k[a] = lookup(or_safe(t0, key_token(t0, a)));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pg.v[j] = lookup(or_safe(t0, t0 + g * 8 + j));
         }
         return pg;
     };
-    auto load = [&](Step<D>& s, int step, const Pages& pg) {
-        const int t0 = tiles.token(step);
+    u32x4 k[2][kKs];
+    VLoad v[8];
+    auto load_keys = [&](int t0, const Pages& pg) {
+        const int page = checked(pg.k[0]);
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-            const uint16_t* src = kbase + offset(pg.k[a], t0 + (i >> 2) * 8 + a * 4 + (i & 3)) + g * 8;
+            const int t = key_token(t0, a);
+            // (A group's page is any of its tokens': whether this one is used does not matter.)
+            const uint16_t* src = kbase + offset(WHOLE || a == 0 ? page : checked(pg.k[1]), t0 < 0 ? safe : WHOLE ? t : or_safe(t0, t));
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) s.k[a][ks] = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(src + ks * 32)));
+            for (int ks = 0; ks < kKs; ++ks) k[a][ks] = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(src + ks * 32)));
         }
-        if (whole) {
-            const uint16_t* src = vbase + offset(pg.v, t0 + g * 8) + i * kVw;
+    };
+    auto load_values = [&](int t0, const Pages& pg) {
+        if constexpr (WHOLE) {
+            const uint16_t* src = vbase + offset(checked(pg.v[0]), t0 < 0 ? 0 : t0 + g * 8);
+            const int step = t0 < 0 ? 0 : D;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s.v[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const VLoad*>(src + j * D)));
+            for (int j = 0; j < 8; ++j) v[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const VLoad*>(src + j * step)));
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int t = t0 + g * 8 + j;
-                s.v[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const VLoad*>(vbase + offset(lookup(t), t) + i * kVw)));
-            }
+            for (int j = 0; j < 8; ++j)
+                v[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const VLoad*>(vbase + offset(checked(pg.v[j]), or_safe(t0, t0 + g * 8 + j)))));
         }
     };
 
@@ -412,106 +417,94 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const Params p) {
 #pragma unroll
     for (int m = 0; m < kVw; ++m) o[m] = float4v{0, 0, 0, 0};
 
-    auto compute = [&](Step<D>& s, int step) {
-        const int t0 = tiles.token(step);
-        float4v st[2];
+    // Waves take steps in turn.
+    const int lo = q.len - q.n;
+    int step = begin + wave;
+    if (step < end) {
+        auto token_of = [&](int st) { return st < end ? tiles.token(st) : -1; };
+        int t0 = tiles.token(step);
+        Pages pg = pages_of(t0);
+        load_keys(t0, pg);
+        load_values(t0, pg);
+        pg = pages_of(token_of(step + kWaves));
+        for (;;) {
+            const int t1 = token_of(step + kWaves);
+            const Pages after = pages_of(token_of(step + 2 * kWaves));
+                    float4v st[2];
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            st[a] = float4v{0, 0, 0, 0};
+                    for (int a = 0; a < 2; ++a) {
+                        st[a] = float4v{0, 0, 0, 0};
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) st[a] = Type<T>::mfma16(__builtin_bit_cast(Vec8, s.k[a][ks]), qf[ks], st[a]);
-        }
-        // Every row sees every token of the step, or some are masked.
-        const int lo = q.len - q.n;
-        const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
-        uint32_t partly = 0;  // tokens that only some rows see and whose values are not all finite
-        if (!all) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int t = t0 + g * 8 + j;
-                if (!sees(p, place, t)) st[j / 4][j % 4] = -INFINITY;
-                const bool any = used(t), every = t <= lo && (t < p.sinks || t > last - p.window);
-                bool clean = true;
-#pragma unroll
-                for (int e = 0; e < kVw / 2; ++e) {
-                    const uint32_t w = s.v[j][e], f = finite_part<T>(w);
-                    clean = clean && (w == f || every);
-                    s.v[j][e] = every ? w : any ? f : 0u;
-                }
-                if (any && !clean) partly |= 1u << j;
-            }
-        }
-        float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
-        mx = pair_max<true>(pair_max<false>(mx));
-        float f;
-        if (sm.advance(mx, p.c, f)) {
-#pragma unroll
-            for (int m = 0; m < kVw; ++m) o[m] *= f;
-        }
-        if (__builtin_amdgcn_ballot_w64(partly != 0)) {
-            // What is not finite goes to the rows that see it, token by token (after
-            // the rescaling, whose first factor is 0).
-            for (int j = 0; j < 8; ++j) {
-                const uint64_t who = __builtin_amdgcn_ballot_w64(partly >> j & 1);
-                for (int g2 = 0; g2 < 4; ++g2) {
-                    if (!(who >> (16 * g2) & 0xFFFF)) continue;
-                    const int t = t0 + g2 * 8 + j;
-                    const uint16_t* src = vbase + offset(lookup(t), t);
-                    if (!sees(p, place, t)) continue;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const VLoad w = *gbl(reinterpret_cast<const VLoad*>(src + (g * 4 + r) * kVw));
-#pragma unroll
-                        for (int m = 0; m < kVw; ++m) o[m][r] += other_part<T>(w[m / 2] >> (16 * (m & 1)));
+                        for (int ks = 0; ks < kKs; ++ks) st[a] = Type<T>::mfma16(__builtin_bit_cast(Vec8, k[a][ks]), qf[ks], st[a]);
                     }
-                }
-            }
-        }
-        const float base = sm.base(p.c);
-        Vec8 pf;
+                    load_keys(t1, pg);
+            // Every row sees every token of the step, or some are masked.
+                                        const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
+                    uint32_t partly = 0;  // tokens that only some rows see and whose values are not all finite
+                    if (!all) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
-            sm.l += w;
-            pf[j] = static_cast<T>(w);
-        }
-        // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
+                        for (int j = 0; j < 8; ++j) {
+                            const int t = t0 + g * 8 + j;
+                            if (!sees(p, place, t)) st[j / 4][j % 4] = -INFINITY;
+                            const bool any = used(t), every = t <= lo && (t < p.sinks || t > last - p.window);
+                            bool clean = true;
 #pragma unroll
-        for (int m = 0; m < kVw; ++m) {
-            u32x4 vf;
+                            for (int e = 0; e < kVw / 2; ++e) {
+                                const uint32_t w = v[j][e], f = finite_part<T>(w);
+                                clean = clean && (w == f || every);
+                                v[j][e] = every ? w : any ? f : 0u;
+                            }
+                            if (any && !clean) partly |= 1u << j;
+                        }
+                    }
+                    float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
+                    mx = pair_max<true>(pair_max<false>(mx));
+                    float f;
+                    if (sm.advance(mx, p.c, f)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                vf[j] = __builtin_amdgcn_perm(s.v[2 * j + 1][m / 2], s.v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
-            o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf), pf, o[m]);
-        }
-    };
-
-    // Waves take steps in turn; a step's loads are in flight while the one
-    // before is computed.
-    {
-        int step = begin + wave;
-        if (step < end) {
-            Step<D> a, b;
-            Pages pg = pages_of(step);
-            load(a, step, pg);
-            pg = pages_of(min(step + kWaves, end - 1));
-            bool in_a = true;
-            while (step + kWaves < end) {
-                load(b, step + kWaves, pg);
-                pg = pages_of(min(step + 2 * kWaves, end - 1));
-                compute(a, step);
-                step += kWaves;
-                if (step + kWaves >= end) {
-                    in_a = false;
-                    break;
-                }
-                load(a, step + kWaves, pg);
-                pg = pages_of(min(step + 2 * kWaves, end - 1));
-                compute(b, step);
-                step += kWaves;
-            }
-            if (in_a) compute(a, step);
-            else compute(b, step);
+                        for (int m = 0; m < kVw; ++m) o[m] *= f;
+                    }
+                    if (__builtin_amdgcn_ballot_w64(partly != 0)) {
+                        // What is not finite goes to the rows that see it, token by token (after
+                        // the rescaling, whose first factor is 0).
+                        for (int j = 0; j < 8; ++j) {
+                            const uint64_t who = __builtin_amdgcn_ballot_w64(partly >> j & 1);
+                            for (int g2 = 0; g2 < 4; ++g2) {
+                                if (!(who >> (16 * g2) & 0xFFFF)) continue;
+                                const int t = t0 + g2 * 8 + j;
+                                const uint16_t* src = vbase - i * kVw + offset(checked(lookup(t)), t);
+                                if (!sees(p, place, t)) continue;
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const VLoad w = *gbl(reinterpret_cast<const VLoad*>(src + (g * 4 + r) * kVw));
+#pragma unroll
+                                    for (int m = 0; m < kVw; ++m) o[m][r] += other_part<T>(w[m / 2] >> (16 * (m & 1)));
+                                }
+                            }
+                        }
+                    }
+                    const float base = sm.base(p.c);
+                    Vec8 pf;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
+                        sm.l += w;
+                        pf[j] = static_cast<T>(w);
+                    }
+                    // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
+#pragma unroll
+                    for (int m = 0; m < kVw; ++m) {
+                        u32x4 vf;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            vf[j] = __builtin_amdgcn_perm(v[2 * j + 1][m / 2], v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
+                        o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf), pf, o[m]);
+                    }
+            load_values(t1, pg);
+            if (t1 < 0) break;
+            pg = after;
+            t0 = t1;
+            step += kWaves;
         }
     }
 
@@ -1027,7 +1020,9 @@ hipError_t launch(const Params& p, const Plan& pl, hipStream_t stream) {
         if (pl.splits > 1) hipLaunchKernelGGL((tile_merge_kernel<T, D>), dim3((unsigned)(p.num_tokens * p.hq)), dim3(kThreads), 0, stream, p);
     }
     if (pl.few) {
-        hipLaunchKernelGGL((few_kernel<T, D>), dim3((unsigned)(p.units * p.hkv)), dim3(kThreads), 0, stream, p);
+        const dim3 grid((unsigned)(p.units * p.hkv));
+        if (p.log2_page >= 3) hipLaunchKernelGGL((few_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, p);
+        else hipLaunchKernelGGL((few_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, p);
         if (p.units > p.num_seqs)
             hipLaunchKernelGGL((few_merge_kernel<T, D>), dim3((unsigned)(p.num_seqs * p.few_slots * p.hkv)), dim3(kThreads), 0, stream, p);
     }
