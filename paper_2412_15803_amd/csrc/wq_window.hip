@@ -110,10 +110,12 @@ struct Params {
     float c;           // |scale| log2(e): scores in log2 units
     uint32_t q_and, q_xor;  // scale < 0 changes the signs of q, scale = 0 makes it zero (with c = 1)
     // few_kernel
-    int32_t units;     // per kv head
+    int32_t units;     // per kv head, at most
+    int32_t round;     // units per kv head that run at once
     int32_t few_slots; // rows of a unit's partial results
     float* few_acc;    // [unit][kv head][few_slots][head_dim]
     float2* few_ml;    // [unit][kv head][few_slots]: (m, l)
+    int2* few_units;   // [sequence][kv head]: first unit, units
     // tile_kernel
     int32_t splits;
     float* tile_acc;   // [token][q head][splits][head_dim]
@@ -171,6 +173,15 @@ __device__ __forceinline__ int inclusive_scan(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1, 3
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2, 3
     return v;
+}
+__device__ __forceinline__ int wave_max(int v) {
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
+    return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
@@ -231,9 +242,15 @@ struct Softmax {
 // The visible tokens of every few-row sequence are cut into steps of 32 tokens
 // and the steps into units, each one workgroup's (per kv head).  The lengths
 // are on the device, so every wave works the cut out for itself: T steps to a
-// unit, T the least that makes at most `units` of them (each sequence at least
-// one), and then which sequence unit u falls in.  The steps of a sequence are
-// dealt evenly over its units.
+// unit at most, and then which sequence unit u falls in.  The steps of a
+// sequence are dealt evenly over its units.
+//
+// A launch lasts about r (T + kUnitCost) steps when the units fill r rounds of
+// workgroups (two to a CU).  What counts is that the longest sequences come out
+// even, so T is a whole fraction of the longest: for one round and for two, the
+// smaller such T that fits, and then the better of both.
+constexpr int kUnitCost = 4;
+
 struct Unit {
     int seq, steps, chunk, first, count;  // steps of the sequence; which of its `count` units, the first of them
 };
@@ -243,6 +260,14 @@ __device__ __forceinline__ int few_steps(const Params& p, int s) {
     if (q.n == 0 || !q.few(p)) return 0;
     if (q.bad) return 1;
     return max(1, Tiles<kFewTokens>(p, q.len - q.n, q.len - 1).count);
+}
+
+// ceil(a / b) for 0 <= a <= 2^22, 1 <= b: the estimate is off by one at most.
+__device__ __forceinline__ int ceil_quotient(int a, int b) {
+    const int n = a + b - 1;
+    int q = (int)((float)n * __builtin_amdgcn_rcpf((float)b));
+    const int r = n - q * b;
+    return q + (r >= b ? 1 : r < 0 ? -1 : 0);
 }
 
 __device__ __forceinline__ bool unit_of(const Params& p, int u, Unit& out) {
@@ -255,24 +280,44 @@ __device__ __forceinline__ bool unit_of(const Params& p, int u, Unit& out) {
     const int s0 = min(lane * per, p.num_seqs), s1 = min(s0 + per, p.num_seqs);
     const int steps0 = s0 < s1 ? few_steps(p, s0) : 0;
     auto steps_of = [&](int s) { return s == s0 ? steps0 : few_steps(p, s); };
-    int sum = 0;
-    for (int s = s0; s < s1; ++s) sum += steps_of(s);
+    int sum = 0, most = 0;
+    for (int s = s0; s < s1; ++s) {
+        sum += steps_of(s);
+        most = max(most, steps_of(s));
+    }
     const int total = last_lane(inclusive_scan(sum));
-    // sum of ceil(steps / T) <= total / T + sequences <= units.
-    const int t = max(1, (total + p.units - p.num_seqs - 1) / (p.units - p.num_seqs));
-    auto units_of = [&](int steps) { return (steps + t - 1) / t; };
+    // sum of ceil(steps / T) <= total / T + sequences, so this T always fits.
+    int t = max(1, ceil_quotient(total, p.units - p.num_seqs));
+    if (per == 1) {
+        most = wave_max(most);
+        int cost = 2 * (t + kUnitCost);
+#pragma unroll
+        for (int r = 1; r <= 2; ++r) {
+            const int room = min(r * p.round, p.units);
+            const int k0 = max(1, (int)((float)most * (float)room * __builtin_amdgcn_rcpf((float)max(total, 1))));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int tk = max(1, ceil_quotient(most, max(1, k0 - k)));
+                const int need = last_lane(inclusive_scan(ceil_quotient(sum, tk)));
+                if (need <= room && r * (tk + kUnitCost) < cost) {
+                    cost = r * (tk + kUnitCost);
+                    t = tk;
+                }
+            }
+        }
+    }
     int mine = 0;
-    for (int s = s0; s < s1; ++s) mine += units_of(steps_of(s));
+    for (int s = s0; s < s1; ++s) mine += ceil_quotient(steps_of(s), t);
     int first = inclusive_scan(mine) - mine;
     const bool here = u >= first && u < first + mine;
     const uint64_t owner = __builtin_amdgcn_ballot_w64(here);
     if (owner == 0) return false;
-    int s = s0, steps = steps0, n = units_of(steps0);
+    int s = s0, steps = steps0, n = ceil_quotient(steps0, t);
     if (here) {
         while (u >= first + n) {
             first += n;
             steps = few_steps(p, ++s);
-            n = units_of(steps);
+            n = ceil_quotient(steps, t);
         }
     }
     const int from = __builtin_ctzll(owner);
@@ -326,6 +371,8 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const Params p) {
     if (!unit_of(p, u, un)) return;
     const Seq q = seq_of(p, un.seq);
     const int rows = q.n * p.group;
+    // (The merge reads this only where the sequence has units.)
+    if (p.units > p.num_seqs && un.chunk == 0 && tid == 0) p.few_units[un.seq * p.hkv + kvh] = make_int2(un.first, un.count);
     if (q.bad) {
         for (int64_t x = tid; x < (int64_t)rows * D; x += kThreads) out_row(p, q, kvh, (int)(x / D), D)[x % D] = Type<T>::kNaN;
         return;
@@ -396,7 +443,7 @@ __global__ __launch_bounds__(kThreads, 2) void few_kernel(const Params p) {
             // (A group's page is any of its tokens': whether this one is used does not matter.)
             const uint16_t* src = kbase + offset(WHOLE || a == 0 ? page : checked(pg.k[1]), t0 < 0 ? safe : WHOLE ? t : or_safe(t0, t));
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) k[a][ks] = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(src + ks * 32)));
+            for (int ks = 0; ks < kKs; ++ks) k[a][ks] = *gbl(reinterpret_cast<const u32x4*>(src + ks * 32));
         }
     };
     auto load_values = [&](int t0, const Pages& pg) {
@@ -610,19 +657,10 @@ __device__ __forceinline__ void merge_row(const Params& p, const float* acc, con
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void few_merge_kernel(const Params p) {
     const int kvh = blockIdx.x % p.hkv, r = blockIdx.x / p.hkv % p.few_slots, s = blockIdx.x / p.hkv / p.few_slots;
+    const int2 units = p.few_units[s * p.hkv + kvh];
     const Seq q = seq_of(p, s);
-    if (q.bad || !q.few(p) || r >= q.n * p.group) return;
-    // The sequence's first unit, found as the split finds a unit's sequence.
-    const int lane = threadIdx.x & 63;
-    int before = 0, total = 0;
-    for (int t = lane; t < p.num_seqs; t += 64) total += few_steps(p, t);
-    total = last_lane(inclusive_scan(total));
-    const int per = max(1, (total + p.units - p.num_seqs - 1) / (p.units - p.num_seqs));
-    for (int t = lane; t < s; t += 64) before += (few_steps(p, t) + per - 1) / per;
-    const int first = last_lane(inclusive_scan(before));
-    const int count = (few_steps(p, s) + per - 1) / per;
-    if (count <= 1) return;
-    merge_row<T, D>(p, p.few_acc, p.few_ml, ((int64_t)first * p.hkv + kvh) * p.few_slots + r, (int64_t)p.hkv * p.few_slots, count,
+    if (q.bad || !q.few(p) || r >= q.n * p.group || units.y <= 1) return;
+    merge_row<T, D>(p, p.few_acc, p.few_ml, ((int64_t)units.x * p.hkv + kvh) * p.few_slots + r, (int64_t)p.hkv * p.few_slots, units.y,
                     out_row(p, q, kvh, r, D));
 }
 
@@ -953,10 +991,13 @@ __global__ __launch_bounds__(kThreads) void tile_merge_kernel(const Params p) {
 
 constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+constexpr int64_t kRound = 512;  // workgroups of few_kernel that run at once: two to a CU
+constexpr int64_t kWhole = 32;   // steps up to which a sequence is not cut
+
 struct Plan {
     bool few, tiles;
-    int64_t units, few_slots, row_tiles, splits;
-    size_t few_acc, few_ml, tile_acc, tile_ml, total;  // offsets of the parts of the workspace
+    int64_t units, round, few_slots, row_tiles, splits;
+    size_t few_acc, few_ml, few_units, tile_acc, tile_ml, total;  // offsets of the parts of the workspace
 };
 
 Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_t hkv, int64_t dim, int64_t max_len, int64_t window, int64_t sinks) {
@@ -969,9 +1010,11 @@ Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_
     const int64_t steps = ceil_div(std::min(max_len, sinks + window + few_query), kFewTokens) + 2;
     pl.few_slots = std::min<int64_t>(kFewRows, max_query * group);
     pl.units = seqs;
-    if (steps > 16 && seqs * hkv < 1024) {
-        const int64_t want = std::max(ceil_div(768, hkv), 2 * seqs);
+    pl.round = std::max<int64_t>(1, kRound / hkv);
+    if (steps > kWhole && seqs * hkv < 2 * kRound) {
+        const int64_t want = std::max(2 * pl.round, 2 * seqs);
         pl.units = std::max(std::min(want, seqs * ceil_div(steps, kWaves)), seqs + 1);
+        pl.round = std::min(pl.round, pl.units);
     }
     pl.row_tiles = std::min(ceil_div(tokens * group, kTileRows) + seqs, seqs * ceil_div(std::min(max_query, tokens) * group, kTileRows));
     const int64_t groups = ceil_div(tokens * group, kTileRows) * hkv;
@@ -987,6 +1030,7 @@ Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_
     const int64_t tile_parts = pl.tiles && pl.splits > 1 ? tokens * hq * pl.splits : 0;
     pl.few_acc = take(few_parts * dim * 4);
     pl.few_ml = take(few_parts * 8);
+    pl.few_units = take(few_parts ? seqs * hkv * 8 : 0);
     pl.tile_acc = take(tile_parts * dim * 4);
     pl.tile_ml = take(tile_parts * 8);
     pl.total = at;
@@ -1124,10 +1168,12 @@ wq_status wq_window_attention(const uint16_t* q, const uint16_t* k_cache, const 
     p.q_and = scale == 0.0f ? 0u : ~0u;
     p.q_xor = scale < 0.0f ? 0x80008000u : 0u;
     p.units = (int32_t)pl.units;
+    p.round = (int32_t)pl.round;
     p.few_slots = (int32_t)pl.few_slots;
     char* ws = static_cast<char*>(workspace);
     p.few_acc = reinterpret_cast<float*>(ws + pl.few_acc);
     p.few_ml = reinterpret_cast<float2*>(ws + pl.few_ml);
+    p.few_units = reinterpret_cast<int2*>(ws + pl.few_units);
     p.splits = (int32_t)pl.splits;
     p.tile_acc = reinterpret_cast<float*>(ws + pl.tile_acc);
     p.tile_ml = reinterpret_cast<float2*>(ws + pl.tile_ml);
