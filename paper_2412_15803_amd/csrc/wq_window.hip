@@ -25,6 +25,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "wq_device.h"
 #include "wq_host.h"
@@ -668,6 +669,14 @@ __global__ __launch_bounds__(kThreads) void few_merge_kernel(const Params p) {
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+    if constexpr (N > 0) {
+        unrolled<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
 template <typename V>
 __device__ __forceinline__ V lds_read(uint32_t addr) {
     return *reinterpret_cast<__attribute__((address_space(3))) V*>((lds_u8*)(size_t)addr);
@@ -687,6 +696,11 @@ __device__ __forceinline__ u32x2 lds_read_turned(uint32_t addr) {
 // that follows its own form; the waits are written out too.
 __device__ __forceinline__ void dma16(const uint16_t* src, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds) : "memory");
+}
+// The same from base + offset + IMM bytes to IMM bytes further on.
+template <int IMM>
+__device__ __forceinline__ void dma16_at(const uint16_t* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(offset), "s"(base), "s"(lds), "n"(IMM) : "memory");
 }
 __device__ __forceinline__ void dma_done_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -708,7 +722,8 @@ __device__ __forceinline__ int value_place(int t) {
 
 // Workgroups: kv heads fastest (each XCD then has its own, whose keys and
 // values stay in its L2), then splits, then row tiles.
-template <typename T, int D>
+// WHOLE: pages of 16 tokens or more.
+template <typename T, int D, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
     using Vec8 = typename Type<T>::Vec8;
     constexpr int kKs = D / 16;                      // key pieces of 16 dims
@@ -788,25 +803,37 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
         bad = 1;
         return 0;
     };
-    // A wave fetches 16 tokens of a tile.  With 16 or more to a page they share
-    // one page, whose number is a scalar load.
+    // A wave fetches 16 tokens of a tile.  In pages of 16 or more they share one,
+    // whose number is a scalar load: a lane's offsets from the first token are then
+    // the same in every tile, and the addresses cost no vector instruction.
+    const int piece = lane % kPieces, in = lane / kPieces;
+    uint32_t key_off[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) key_off[j] = (uint32_t)(in * D + (piece ^ key_place<D>(j * kTokensPerLoad + in)) * 8) * 2;
+    const uint32_t value_off = (uint32_t)(in * D + (piece ^ value_place<D>(in)) * 8) * 2;
     auto fetch = [&](int step, int buffer) {
         const int t0 = tiles.token(step) + wave * 16;
         const uint32_t kdst = lds0 + (buffer * 2) * kTileBytes + wave * (kTileBytes / kWaves);
-        int one = 0;
-        if (p.log2_page >= 4) {
+        if constexpr (WHOLE) {
+            // Tokens that no row sees stand for page 0 and are masked.
             const bool any = t0 <= hi && (t0 < p.sinks || t0 + 15 >= tiles.first);
-            if (any) one = checked(((const __attribute__((address_space(4))) int32_t*)trow)[__builtin_amdgcn_readfirstlane(t0 >> p.log2_page)]);
-        }
+            int page = 0;
+            if (any) page = checked(((const __attribute__((address_space(4))) int32_t*)trow)[__builtin_amdgcn_readfirstlane(t0 >> p.log2_page)]);
+            const int64_t off = (int64_t)__builtin_amdgcn_readfirstlane(page) * p.page_stride + (int64_t)((t0 & page_mask) * D);
+            const uint16_t *ks = kbase + off, *vs = vbase + off;
+            unrolled<kLoads>([&](auto j) {
+                dma16_at<j * 1024>(ks, key_off[j], kdst);
+                dma16_at<j * 1024>(vs, value_off, kdst + kTileBytes);
+            });
+        } else {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int in = j * kTokensPerLoad + lane / kPieces, t = t0 + in, tt = wave * 16 + in;
-            int page = one;
-            if (p.log2_page < 4) page = used(t) ? checked(trow[t >> p.log2_page]) : 0;
-            const int64_t off = (int64_t)page * p.page_stride + (int64_t)(t & page_mask) * D;
-            const int piece = lane % kPieces;
-            dma16(kbase + off + (piece ^ key_place<D>(tt)) * 8, kdst + j * 1024);
-            dma16(vbase + off + (piece ^ value_place<D>(tt)) * 8, kdst + kTileBytes + j * 1024);
+            for (int j = 0; j < kLoads; ++j) {
+                const int t = t0 + j * kTokensPerLoad + in;
+                const int page = used(t) ? checked(trow[t >> p.log2_page]) : 0;
+                const int64_t off = (int64_t)page * p.page_stride + (int64_t)(t & page_mask) * D;
+                dma16(kbase + off + (key_off[j] / 2 - in * D), kdst + j * 1024);
+                dma16(vbase + off + (value_off / 2 - in * D), kdst + kTileBytes + j * 1024);
+            }
         }
     };
 
@@ -818,8 +845,18 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
     Softmax sm;
     if (tid < 2) sh_partly[tid] = 0;
 
-    const uint32_t krow = lds0 + i * (D * 2);
+    // LDS addresses in buffer 0.  A key piece's place depends on the piece and the
+    // token modulo 16, a value's on its 64 bytes and the token modulo 4, so that
+    // everything else of an address is an instruction's own offset.
+    uint32_t ka[kKs], va[kDt];
+#pragma unroll
+    for (int ks = 0; ks < kKs; ++ks) ka[ks] = lds0 + i * (D * 2) + ((2 * ks + h) ^ key_place<D>(i)) * 16;
     const int vr = (lane & 15) >> 2, vd = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;  // row of 4 and dim that the lane reads for a turned load
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt) {
+        const int d = dt * 32 + vd, t = h * 4 + vr;
+        va[dt] = lds0 + kTileBytes + t * (D * 2) + ((d / 8) ^ value_place<D>(t)) * 16 + (d & 4) * 2;
+    }
 
     if (begin < end) fetch(begin, 0);
     for (int step = begin; step < end; ++step) {
@@ -827,7 +864,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
         const int t0 = tiles.token(step);
         dma_done_and_barrier();  // the tile is there, and the other buffer no longer read
         if (step + 1 < end) fetch(step + 1, buffer ^ 1);
-        const uint32_t kt = krow + (buffer * 2) * kTileBytes, vt = lds0 + (buffer * 2 + 1) * kTileBytes;
+        const uint32_t at = buffer * 2 * kTileBytes;
 
         const int tl = t0 + kTileTokens - 1;
         const bool all = tl <= lo && (tl < p.sinks || t0 > hi - p.window);  // every row sees every token
@@ -840,7 +877,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
                 const int x = j * kThreads + tid, t = t0 + x / kPieces;
                 if (t <= lo && (t < p.sinks || t > hi - p.window)) continue;
                 const bool any = used(t);
-                const u32x4 w = lds_read<u32x4>(vt + x * 16);
+                const u32x4 w = lds_read<u32x4>(lds0 + kTileBytes + at + x * 16);
                 u32x4 f;
                 bool same = true;
 #pragma unroll
@@ -849,7 +886,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
                     same = same && f[e] == w[e];
                 }
                 if (same) continue;
-                lds_write(vt + x * 16, f);
+                lds_write(lds0 + kTileBytes + at + x * 16, f);
                 if (any) atomicOr(&sh_partly[buffer], 1ull << (x / kPieces));
             }
             lds_barrier();
@@ -864,10 +901,18 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
             for (int r = 0; r < 16; ++r) st[tt][r] = 0.0f;
 #pragma unroll
             for (int ks = 0; ks < kKs; ++ks) {
-                const u32x4 w = lds_read<u32x4>(kt + tt * 32 * (D * 2) + ((2 * ks + h) ^ key_place<D>(i)) * 16);
+                const u32x4 w = lds_read<u32x4>(ka[ks] + at + tt * 32 * (D * 2));
                 st[tt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, w), qf[ks], st[tt]);
             }
         }
+        // Reads ahead of the products that use them.
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int x = 0; x < 2 * kKs - 6; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
         if (!all) {
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
@@ -916,16 +961,17 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
         for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                u32x4 w;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int t = x * 16 + half * 8 + h * 4 + vr, d = dt * 32 + vd;
-                    const u32x2 two = lds_read_turned(vt + t * (D * 2) + ((d / 8) ^ value_place<D>(t)) * 16 + (d & 4) * 2);
-                    w[2 * half] = two.x;
-                    w[2 * half + 1] = two.y;
-                }
+                const u32x2 a = lds_read_turned(va[dt] + at + x * 16 * (D * 2)), b = lds_read_turned(va[dt] + at + (x * 16 + 8) * (D * 2));
+                const u32x4 w = {a.x, a.y, b.x, b.y};
                 o[dt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, w), pf[x], o[dt]);
             }
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+        for (int x = 0; x < 4 * kDt - 4; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     }
 
     float l = pair_sum<true>(sm.l);
@@ -1060,7 +1106,9 @@ wq_status check_sizes(const char* fn, int64_t seqs, int64_t tokens, int64_t max_
 template <typename T, int D>
 hipError_t launch(const Params& p, const Plan& pl, hipStream_t stream) {
     if (pl.tiles) {
-        hipLaunchKernelGGL((tile_kernel<T, D>), dim3((unsigned)(pl.row_tiles * pl.splits * p.hkv)), dim3(kThreads), 0, stream, p);
+        const dim3 grid((unsigned)(pl.row_tiles * pl.splits * p.hkv));
+        if (p.log2_page >= 4) hipLaunchKernelGGL((tile_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, p);
+        else hipLaunchKernelGGL((tile_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, p);
         if (pl.splits > 1) hipLaunchKernelGGL((tile_merge_kernel<T, D>), dim3((unsigned)(p.num_tokens * p.hq)), dim3(kThreads), 0, stream, p);
     }
     if (pl.few) {
