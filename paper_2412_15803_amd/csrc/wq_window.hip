@@ -1070,7 +1070,7 @@ Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_
     pl.row_tiles = std::min(ceil_div(tokens * group, kTileRows) + seqs, seqs * ceil_div(std::min(max_query, tokens) * group, kTileRows));
     const int64_t groups = ceil_div(tokens * group, kTileRows) * hkv;
     const int64_t seen = ceil_div(std::min(max_len, sinks + window + kTileRows / group + 1), kTileTokens) + 1;
-    pl.splits = groups >= 384 ? 1 : std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, groups), seen / 4, 32}));
+    pl.splits = groups >= 384 ? 1 : std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, groups), seen / 16, 32}));
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t here = at;
