@@ -51,6 +51,9 @@ constexpr int kFewRows = 16;    // rows of few_kernel
 constexpr int kFewTokens = 32;  // tokens of one of its steps
 constexpr int kTileRows = 128;  // rows of a workgroup of tile_kernel, 32 per wave
 constexpr int kTileTokens = 64;
+// Tiles of which some row of a workgroup does not see every token: where its
+// rows' windows begin and end, (rows / 64 + 2) each, and where the sinks end.
+constexpr int kEdges = 16;
 constexpr float kRescale = 8.0f;  // see Softmax
 
 template <typename T>
@@ -367,6 +370,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
     typedef uint32_t VLoad __attribute__((ext_vector_type(kVw / 2)));
     __shared__ float sh_acc[WAVES][kFewRows][D];
     __shared__ float sh_m[WAVES][kFewRows], sh_l[WAVES][kFewRows];
+    // Tokens that only some rows see and whose values are not all finite, once
+    // for each lane that met one.  16 new tokens at most have 15 such tokens at
+    // the end and 15 where their windows begin, in 16 lanes each.
+    constexpr int kOthers = 512;
+    __shared__ int sh_others, sh_other[kOthers];
 
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -381,6 +389,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
         for (int64_t x = tid; x < (int64_t)rows * D; x += (WAVES * 64)) out_row(p, q, kvh, (int)(x / D), D)[x % D] = Type<T>::kNaN;
         return;
     }
+    if (tid == 0) sh_others = 0;
+    __syncthreads();
     const Tiles<kFewTokens> tiles(p, q.len - q.n, q.len - 1);
     const int begin = (int)((int64_t)tiles.count * un.chunk / un.count), end = (int)((int64_t)tiles.count * (un.chunk + 1) / un.count);
     const int place = q.len - q.n + min(i / p.group, q.n - 1);  // of the lane's row
@@ -481,76 +491,56 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
         for (;;) {
             const int t1 = token_of(step + WAVES);
             const Pages after = pages_of(token_of(step + 2 * WAVES));
-                    float4v st[2];
+            float4v st[2];
 #pragma unroll
-                    for (int a = 0; a < 2; ++a) {
-                        st[a] = float4v{0, 0, 0, 0};
+            for (int a = 0; a < 2; ++a) {
+                st[a] = float4v{0, 0, 0, 0};
 #pragma unroll
-                        for (int ks = 0; ks < kKs; ++ks) st[a] = Type<T>::mfma16(__builtin_bit_cast(Vec8, k[a][ks]), qf[ks], st[a]);
-                    }
-                    load_keys(t1, pg);
+                for (int ks = 0; ks < kKs; ++ks) st[a] = Type<T>::mfma16(__builtin_bit_cast(Vec8, k[a][ks]), qf[ks], st[a]);
+            }
+            load_keys(t1, pg);
             // Every row sees every token of the step, or some are masked.
-                                        const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
-                    uint32_t partly = 0;  // tokens that only some rows see and whose values are not all finite
-                    if (!all) {
+                                const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
+            if (!all) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int t = t0 + g * 8 + j;
-                            if (!sees(p, place, t)) st[j / 4][j % 4] = -INFINITY;
-                            const bool any = used(t), every = t <= lo && (t < p.sinks || t > last - p.window);
-                            bool clean = true;
+                for (int j = 0; j < 8; ++j) {
+                    const int t = t0 + g * 8 + j;
+                    if (!sees(p, place, t)) st[j / 4][j % 4] = -INFINITY;
+                    const bool any = used(t), every = t <= lo && (t < p.sinks || t > last - p.window);
+                    bool clean = true;
 #pragma unroll
-                            for (int e = 0; e < kVw / 2; ++e) {
-                                const uint32_t w = v[j][e], f = finite_part<T>(w);
-                                clean = clean && (w == f || every);
-                                v[j][e] = every ? w : any ? f : 0u;
-                            }
-                            if (any && !clean) partly |= 1u << j;
-                        }
+                    for (int e = 0; e < kVw / 2; ++e) {
+                        const uint32_t w = v[j][e], f = finite_part<T>(w);
+                        clean = clean && (w == f || every);
+                        v[j][e] = every ? w : any ? f : 0u;
                     }
-                    float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
-                    mx = pair_max<true>(pair_max<false>(mx));
-                    float f;
-                    if (sm.advance(mx, p.c, f)) {
+                    if (any && !clean) sh_other[min(atomicAdd(&sh_others, 1), kOthers - 1)] = t;
+                }
+            }
+            float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
+            mx = pair_max<true>(pair_max<false>(mx));
+            float f;
+            if (sm.advance(mx, p.c, f)) {
 #pragma unroll
-                        for (int m = 0; m < kVw; ++m) o[m] *= f;
-                    }
-                    if (__builtin_amdgcn_ballot_w64(partly != 0)) {
-                        // What is not finite goes to the rows that see it, token by token (after
-                        // the rescaling, whose first factor is 0).
-                        for (int j = 0; j < 8; ++j) {
-                            const uint64_t who = __builtin_amdgcn_ballot_w64(partly >> j & 1);
-                            for (int g2 = 0; g2 < 4; ++g2) {
-                                if (!(who >> (16 * g2) & 0xFFFF)) continue;
-                                const int t = t0 + g2 * 8 + j;
-                                const uint16_t* src = vbase - i * kVw + offset(checked(lookup(t)), t);
-                                if (!sees(p, place, t)) continue;
+                for (int m = 0; m < kVw; ++m) o[m] *= f;
+            }
+            const float base = sm.base(p.c);
+            Vec8 pf;
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) {
-                                    const VLoad w = *gbl(reinterpret_cast<const VLoad*>(src + (g * 4 + r) * kVw));
+            for (int j = 0; j < 8; ++j) {
+                const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
+                sm.l += w;
+                pf[j] = static_cast<T>(w);
+            }
+            // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
 #pragma unroll
-                                    for (int m = 0; m < kVw; ++m) o[m][r] += other_part<T>(w[m / 2] >> (16 * (m & 1)));
-                                }
-                            }
-                        }
-                    }
-                    const float base = sm.base(p.c);
-                    Vec8 pf;
+            for (int m = 0; m < kVw; ++m) {
+                u32x4 vf;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
-                        sm.l += w;
-                        pf[j] = static_cast<T>(w);
-                    }
-                    // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
-#pragma unroll
-                    for (int m = 0; m < kVw; ++m) {
-                        u32x4 vf;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            vf[j] = __builtin_amdgcn_perm(v[2 * j + 1][m / 2], v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
-                        o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf), pf, o[m]);
-                    }
+                for (int j = 0; j < 4; ++j)
+                    vf[j] = __builtin_amdgcn_perm(v[2 * j + 1][m / 2], v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
+                o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf), pf, o[m]);
+            }
             load_values(t1, pg);
             if (t1 < 0) break;
             pg = after;
@@ -585,6 +575,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
             const float f = sh_m[w][r] == -INFINITY ? 0.0f : exp2_((sh_m[w][r] - ms) * p.c);
             sum += sh_l[w][r] == 0.0f ? 0.0f : sh_l[w][r] * f;
             acc += sh_m[w][r] == -INFINITY ? 0.0f : sh_acc[w][r][d] * f;
+        }
+        // What is not finite goes to the rows that see it, whatever its weight.
+        for (int x2 = 0; x2 < min(sh_others, kOthers); ++x2) {
+            const int t = sh_other[x2];
+            if (sees(p, lo + r / p.group, t)) acc += other_part<T>(vbase[offset(checked(lookup(t)), t) - i * kVw + d]);
         }
         if (un.count == 1) {
             out_row(p, q, kvh, r, D)[d] = finish<T>(p, acc, sum);
@@ -705,6 +700,7 @@ template <int IMM>
 __device__ __forceinline__ void dma16_at(const uint16_t* base, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(offset), "s"(base), "s"(lds), "n"(IMM) : "memory");
 }
+// A barrier behind which every wave's loads are done.
 __device__ __forceinline__ void dma_done_and_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -723,27 +719,16 @@ __device__ __forceinline__ int value_place(int t) {
     return D == 128 ? (t & 3) << 2 : (t >> 1 & 1) << 2;
 }
 
-// Workgroups: kv heads fastest (each XCD then has its own, whose keys and
-// values stay in its L2), then splits, then row tiles.
-// WHOLE: pages of 16 tokens or more.
-template <typename T, int D, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
-    using Vec8 = typename Type<T>::Vec8;
-    constexpr int kKs = D / 16;                      // key pieces of 16 dims
-    constexpr int kDt = D / 32;                      // output tiles of 32 dims
-    constexpr int kPieces = D / 8;                   // 16-byte pieces of a token
-    constexpr uint32_t kTileBytes = kTileTokens * D * 2;
-    constexpr int kLoads = kTileBytes / 16 / kThreads;  // per lane and array
-    constexpr int kTokensPerLoad = 64 / kPieces;        // of one wave
-    __shared__ __align__(16) uint8_t sh_tiles[2][2][kTileBytes];
-    __shared__ unsigned long long sh_partly[2];
+struct RowTile {
+    int s;
+    Seq seq;
+    int row0, rows;
+};
 
-    const int tid = threadIdx.x, lane = tid & 63, i = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kvh = blockIdx.x % p.hkv, split = blockIdx.x / p.hkv % p.splits;
-    int tile = blockIdx.x / p.hkv / p.splits;
-
-    // The sequence of this row tile.
+// Row tile `tile`, the sequences in order; of a sequence the last tiles, which
+// see most, come first.
+__device__ __forceinline__ bool find_tile(const Params& p, int tile, RowTile& out) {
+    const int lane = threadIdx.x & 63;
     int s = -1;
     for (int s0 = 0; s0 < p.num_seqs; s0 += 64) {
         int n = 0;
@@ -761,13 +746,55 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
         }
         tile -= last_lane(inc);
     }
-    if (s < 0) return;
-    s = __builtin_amdgcn_readfirstlane(s);
-    const Seq q = seq_of(p, s);
-    const int all_rows = q.n * p.group;
-    // The last tiles, which see most, first.
-    const int row0 = ((all_rows + kTileRows - 1) / kTileRows - 1 - tile) * kTileRows;
-    const int rows = min(kTileRows, all_rows - row0);
+    if (s < 0) return false;
+    out.s = __builtin_amdgcn_readfirstlane(s);
+    out.seq = seq_of(p, out.s);
+    const int all_rows = out.seq.n * p.group;
+    out.row0 = ((all_rows + kTileRows - 1) / kTileRows - 1 - tile) * kTileRows;
+    out.rows = min(kTileRows, all_rows - out.row0);
+    return true;
+}
+
+// A lane's outputs: of its row, dims 32 dt + 8 (r / 4) + 4 h + r % 4.
+template <typename T, int D, int DT>
+__device__ __forceinline__ void write_rows(const Params& p, uint16_t* dst, const float16v (&o)[DT], float l, int h) {
+    const bool blind = p.window == 0 && p.sinks == 0;
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            uint16_t e[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) e[r] = l != l ? Type<T>::kNaN : blind ? 0 : bits_of<T>(o[dt][r4 * 4 + r] * inv);
+            const u32x2 w = {(uint32_t)e[0] | (uint32_t)e[1] << 16, (uint32_t)e[2] | (uint32_t)e[3] << 16};
+            *gbl(reinterpret_cast<u32x2*>(dst + dt * 32 + r4 * 8 + h * 4)) = w;
+        }
+}
+
+// Workgroups: kv heads fastest (each XCD then has its own, whose keys and
+// values stay in its L2), then splits, then row tiles.
+// WHOLE: pages of 16 tokens or more.
+template <typename T, int D, bool WHOLE>
+__global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
+    using Vec8 = typename Type<T>::Vec8;
+    constexpr int kKs = D / 16;                      // key pieces of 16 dims
+    constexpr int kDt = D / 32;                      // output tiles of 32 dims
+    constexpr int kPieces = D / 8;                   // 16-byte pieces of a token
+    constexpr uint32_t kTileBytes = kTileTokens * D * 2;
+    constexpr int kLoads = kTileBytes / 16 / kThreads;  // per lane and array
+    constexpr int kTokensPerLoad = 64 / kPieces;        // of one wave
+    __shared__ __align__(16) uint8_t sh_tiles[2][2][kTileBytes];
+    __shared__ unsigned long long sh_partly[kEdges];
+    __shared__ int sh_edge[kEdges], sh_bad;
+
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % p.hkv, split = blockIdx.x / p.hkv % p.splits;
+    RowTile rt;
+    if (!find_tile(p, blockIdx.x / p.hkv / p.splits, rt)) return;
+    const Seq& q = rt.seq;
+    const int s = rt.s, row0 = rt.row0, rows = rt.rows, all_rows = q.n * p.group;
     if (q.bad) {
         if (split == 0)
             for (int x = tid; x < rows * D; x += kThreads) out_row(p, q, kvh, row0 + x / D, D)[x % D] = Type<T>::kNaN;
@@ -846,7 +873,9 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
     Softmax sm;
-    if (tid < 2) sh_partly[tid] = 0;
+    if (tid < kEdges) sh_partly[tid] = 0;
+    if (tid == 0) sh_bad = 0;
+    int edges = 0;
 
     // LDS addresses in buffer 0.  A key piece's place depends on the piece and the
     // token modulo 16, a value's on its 64 bytes and the token modulo 4, so that
@@ -861,6 +890,51 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
         va[dt] = lds0 + kTileBytes + t * (D * 2) + ((d / 8) ^ value_place<D>(t)) * 16 + (d & 4) * 2;
     }
 
+    // Values that no row sees are cleared in LDS, and so is what is not finite of
+    // tokens that only some rows see: 0 times it would not be 0.  Such tokens are
+    // noted; what was not finite is added at the end to the rows that see it.
+    auto clean = [&](int t0, uint32_t at) {
+        const int edge = min(edges++, kEdges - 1);
+        if (tid == 0) sh_edge[edge] = t0;
+#pragma unroll 1
+        for (int x = tid; x < kTileTokens * kPieces; x += kThreads) {
+            const int t = t0 + x / kPieces;
+            if (t <= lo && (t < p.sinks || t > hi - p.window)) continue;
+            const bool any = used(t);
+            const u32x4 w = lds_read<u32x4>(at + x * 16);
+            u32x4 f;
+            bool same = true;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[e] = any ? finite_part<T>(w[e]) : 0u;
+                same = same && f[e] == w[e];
+            }
+            if (same) continue;
+            lds_write(at + x * 16, f);
+            if (any) atomicOr(&sh_partly[edge], 1ull << (x / kPieces));
+        }
+        lds_barrier();
+    };
+    auto add_others = [&] {
+        for (int e = 0; e < min(edges, kEdges); ++e) {
+            uint64_t tokens = sh_partly[e];
+            while (tokens) {
+                const int t = sh_edge[e] + __builtin_ctzll(tokens);
+                tokens &= tokens - 1;
+                const uint16_t* src = vbase + (int64_t)checked(trow[t >> p.log2_page]) * p.page_stride + (int64_t)(t & page_mask) * D;
+                if (!sees(p, place, t)) continue;
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+                    for (int r4 = 0; r4 < 4; ++r4) {
+                        const u32x2 w = *gbl(reinterpret_cast<const u32x2*>(src + dt * 32 + 8 * r4 + 4 * h));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[dt][4 * r4 + r] += other_part<T>(w[r / 2] >> (16 * (r & 1)));
+                    }
+            }
+        }
+    };
+
     if (begin < end) fetch(begin, 0);
     for (int step = begin; step < end; ++step) {
         const int buffer = (step - begin) & 1;
@@ -871,43 +945,19 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 
         const int tl = t0 + kTileTokens - 1;
         const bool all = tl <= lo && (tl < p.sinks || t0 > hi - p.window);  // every row sees every token
-        unsigned long long partly = 0;
-        if (!all) {
-            // Values that no row sees are cleared, and so is what is not finite of
-            // tokens that only some rows see: 0 times it would not be 0.
-#pragma unroll
-            for (int j = 0; j < kTileTokens * kPieces / kThreads; ++j) {
-                const int x = j * kThreads + tid, t = t0 + x / kPieces;
-                if (t <= lo && (t < p.sinks || t > hi - p.window)) continue;
-                const bool any = used(t);
-                const u32x4 w = lds_read<u32x4>(lds0 + kTileBytes + at + x * 16);
-                u32x4 f;
-                bool same = true;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f[e] = any ? finite_part<T>(w[e]) : 0u;
-                    same = same && f[e] == w[e];
-                }
-                if (same) continue;
-                lds_write(lds0 + kTileBytes + at + x * 16, f);
-                if (any) atomicOr(&sh_partly[buffer], 1ull << (x / kPieces));
-            }
-            lds_barrier();
-            partly = sh_partly[buffer];
-        }
-        if (tid == 0) sh_partly[buffer ^ 1] = 0;  // read last before the barrier above, written next after the one to come
+        if (!all) clean(t0, lds0 + kTileBytes + at);
 
         float16v st[2];
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) st[tt][r] = 0.0f;
+        // Products that follow each other are of different sums.
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) {
-                const u32x4 w = lds_read<u32x4>(ka[ks] + at + tt * 32 * (D * 2));
-                st[tt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, w), qf[ks], st[tt]);
-            }
-        }
+        for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt)
+                st[tt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, lds_read<u32x4>(ka[ks] + at + tt * 32 * (D * 2))), qf[ks], st[tt]);
         // Reads ahead of the products that use them.
         __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
@@ -934,21 +984,6 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 #pragma unroll
             for (int dt = 0; dt < kDt; ++dt) o[dt] *= f;
         }
-        // What is not finite goes to the rows that see it, token by token.
-                    while (partly) {
-            const int x = __builtin_ctzll(partly), t = t0 + x;
-            partly &= partly - 1;
-            const uint16_t* src = vbase + (int64_t)checked(trow[t >> p.log2_page]) * p.page_stride + (int64_t)(t & page_mask) * D;
-            if (!sees(p, place, t)) continue;
-#pragma unroll
-            for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const u32x2 w = *gbl(reinterpret_cast<const u32x2*>(src + dt * 32 + 8 * r4 + 4 * h));
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[dt][4 * r4 + r] += other_part<T>(w[r / 2] >> (16 * (r & 1)));
-                }
-        }
         const float base = sm.base(p.c);
         Vec8 pf[4];
 #pragma unroll
@@ -961,9 +996,9 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
             }
         // Product x takes tokens 16 x + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
 #pragma unroll
-        for (int dt = 0; dt < kDt; ++dt)
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
+            for (int dt = 0; dt < kDt; ++dt) {
                 const u32x2 a = lds_read_turned(va[dt] + at + x * 16 * (D * 2)), b = lds_read_turned(va[dt] + at + (x * 16 + 8) * (D * 2));
                 const u32x4 w = {a.x, a.y, b.x, b.y};
                 o[dt] = Type<T>::mfma32(__builtin_bit_cast(Vec8, w), pf[x], o[dt]);
@@ -979,27 +1014,13 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 
     float l = pair_sum<true>(sm.l);
     // A page outside the cache, met by any wave: the sum of every row is NaN.
+    if (bad) sh_bad = 1;
     lds_barrier();
-    if (tid == 0) sh_partly[0] = 0;
-    lds_barrier();
-    if (bad) sh_partly[0] = 1;
-    lds_barrier();
-    if (sh_partly[0]) l = NAN;
+    if (sh_bad) l = NAN;
+    add_others();
     if (!row_ok) return;
     if (p.splits == 1) {
-        uint16_t* dst = out_row(p, q, kvh, row, D);
-        const bool blind = p.window == 0 && p.sinks == 0;
-        const float inv = 1.0f / l;
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                uint16_t e[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) e[r] = l != l ? Type<T>::kNaN : blind ? 0 : bits_of<T>(o[dt][r4 * 4 + r] * inv);
-                u32x2 w = {(uint32_t)e[0] | (uint32_t)e[1] << 16, (uint32_t)e[2] | (uint32_t)e[3] << 16};
-                *gbl(reinterpret_cast<u32x2*>(dst + dt * 32 + r4 * 8 + h * 4)) = w;
-            }
+        write_rows<T, D>(p, out_row(p, q, kvh, row, D), o, l, h);
     } else {
         const int64_t slot = ((int64_t)(q.first + row / p.group) * p.hq + kvh * p.group + row % p.group) * p.splits + split;
         float* dst = p.tile_acc + slot * D;
