@@ -363,22 +363,25 @@ __device__ __forceinline__ uint16_t finish(const Params& p, float acc, float l) 
 // WAVES: 4 where the cache is split, 8 where a workgroup takes a sequence whole
 // (516 tokens of 64 dims, 2 kv heads: 8.9 -> 8.2 us; 64 sequences of up to 2004, 4
 // kv heads: 28.3 -> 22.6 against the split).
-template <typename T, int D, bool WHOLE, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(const Params p) {
-    using Vec8 = typename Type<T>::Vec8;
-    constexpr int kKs = D / 32, kVw = D / 16;
-    typedef uint32_t VLoad __attribute__((ext_vector_type(kVw / 2)));
-    __shared__ float sh_acc[WAVES][kFewRows][D];
-    __shared__ float sh_m[WAVES][kFewRows], sh_l[WAVES][kFewRows];
+template <int D, int WAVES>
+struct FewShared {
+    float acc[WAVES][kFewRows][D];
+    float m[WAVES][kFewRows], l[WAVES][kFewRows];
     // Tokens that only some rows see and whose values are not all finite, once
     // for each lane that met one.  16 new tokens at most have 15 such tokens at
     // the end and 15 where their windows begin, in 16 lanes each.
-    constexpr int kOthers = 512;
-    __shared__ int sh_others, sh_other[kOthers];
+    int others, other[512];
+};
 
+template <typename T, int D, bool WHOLE, int WAVES>
+__device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D, WAVES>& sh) {
+    constexpr int kOthers = sizeof(sh.other) / sizeof(sh.other[0]);
+    using Vec8 = typename Type<T>::Vec8;
+    constexpr int kKs = D / 32, kVw = D / 16;
+    typedef uint32_t VLoad __attribute__((ext_vector_type(kVw / 2)));
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kvh = blockIdx.x % p.hkv, u = blockIdx.x / p.hkv;
+    const int kvh = block % p.hkv, u = block / p.hkv;
     Unit un;
     if (!unit_of(p, u, un)) return;
     const Seq q = seq_of(p, un.seq);
@@ -389,7 +392,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
         for (int64_t x = tid; x < (int64_t)rows * D; x += (WAVES * 64)) out_row(p, q, kvh, (int)(x / D), D)[x % D] = Type<T>::kNaN;
         return;
     }
-    if (tid == 0) sh_others = 0;
+    if (tid == 0) sh.others = 0;
     __syncthreads();
     const Tiles<kFewTokens> tiles(p, q.len - q.n, q.len - 1);
     const int begin = (int)((int64_t)tiles.count * un.chunk / un.count), end = (int)((int64_t)tiles.count * (un.chunk + 1) / un.count);
@@ -514,7 +517,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
                         clean = clean && (w == f || every);
                         v[j][e] = every ? w : any ? f : 0u;
                     }
-                    if (any && !clean) sh_other[min(atomicAdd(&sh_others, 1), kOthers - 1)] = t;
+                    if (any && !clean) sh.other[min(atomicAdd(&sh.others, 1), kOthers - 1)] = t;
                 }
             }
             float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
@@ -554,31 +557,31 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
     float l = pair_sum<true>(pair_sum<false>(sm.l));
     if (__builtin_amdgcn_ballot_w64(bad != 0)) l = NAN;
     if (g == 0) {
-        sh_m[wave][i] = sm.m;
-        sh_l[wave][i] = l;
+        sh.m[wave][i] = sm.m;
+        sh.l[wave][i] = l;
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int m = 0; m < kVw; m += 4)
-            *reinterpret_cast<float4v*>(&sh_acc[wave][i][(g * 4 + r) * kVw + m]) = float4v{o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
+            *reinterpret_cast<float4v*>(&sh.acc[wave][i][(g * 4 + r) * kVw + m]) = float4v{o[m][r], o[m + 1][r], o[m + 2][r], o[m + 3][r]};
     __syncthreads();
     for (int x = tid; x < rows * D; x += (WAVES * 64)) {
         const int r = x / D, d = x % D;
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, sh_m[w][r]);
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, sh.m[w][r]);
         const float ms = m == -INFINITY ? 0.0f : m;
         float sum = 0.0f, acc = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = sh_m[w][r] == -INFINITY ? 0.0f : exp2_((sh_m[w][r] - ms) * p.c);
-            sum += sh_l[w][r] == 0.0f ? 0.0f : sh_l[w][r] * f;
-            acc += sh_m[w][r] == -INFINITY ? 0.0f : sh_acc[w][r][d] * f;
+            const float f = sh.m[w][r] == -INFINITY ? 0.0f : exp2_((sh.m[w][r] - ms) * p.c);
+            sum += sh.l[w][r] == 0.0f ? 0.0f : sh.l[w][r] * f;
+            acc += sh.m[w][r] == -INFINITY ? 0.0f : sh.acc[w][r][d] * f;
         }
         // What is not finite goes to the rows that see it, whatever its weight.
-        for (int x2 = 0; x2 < min(sh_others, kOthers); ++x2) {
-            const int t = sh_other[x2];
+        for (int x2 = 0; x2 < min(sh.others, kOthers); ++x2) {
+            const int t = sh.other[x2];
             if (sees(p, lo + r / p.group, t)) acc += other_part<T>(vbase[offset(checked(lookup(t)), t) - i * kVw + d]);
         }
         if (un.count == 1) {
@@ -589,6 +592,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(con
             if (d == 0) p.few_ml[slot] = make_float2(m, sum);
         }
     }
+}
+
+template <typename T, int D, bool WHOLE, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void few_kernel(const Params p) {
+    __shared__ __align__(16) FewShared<D, WAVES> sh;
+    few_body<T, D, WHOLE, WAVES>(p, blockIdx.x, sh);
 }
 
 // Joins `count` parts of one row; part i at slot base + i step.  256 threads.
@@ -775,8 +784,15 @@ __device__ __forceinline__ void write_rows(const Params& p, uint16_t* dst, const
 // Workgroups: kv heads fastest (each XCD then has its own, whose keys and
 // values stay in its L2), then splits, then row tiles.
 // WHOLE: pages of 16 tokens or more.
+template <int D>
+struct TileShared {
+    uint8_t tiles[2][2][kTileTokens * D * 2];  // keys, values
+    unsigned long long partly[kEdges];
+    int edge[kEdges], bad;
+};
+
 template <typename T, int D, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
+__device__ __forceinline__ void tile_body(const Params& p, int block, TileShared<D>& sh) {
     using Vec8 = typename Type<T>::Vec8;
     constexpr int kKs = D / 16;                      // key pieces of 16 dims
     constexpr int kDt = D / 32;                      // output tiles of 32 dims
@@ -784,15 +800,12 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
     constexpr uint32_t kTileBytes = kTileTokens * D * 2;
     constexpr int kLoads = kTileBytes / 16 / kThreads;  // per lane and array
     constexpr int kTokensPerLoad = 64 / kPieces;        // of one wave
-    __shared__ __align__(16) uint8_t sh_tiles[2][2][kTileBytes];
-    __shared__ unsigned long long sh_partly[kEdges];
-    __shared__ int sh_edge[kEdges], sh_bad;
 
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kvh = blockIdx.x % p.hkv, split = blockIdx.x / p.hkv % p.splits;
+    const int kvh = block % p.hkv, split = block / p.hkv % p.splits;
     RowTile rt;
-    if (!find_tile(p, blockIdx.x / p.hkv / p.splits, rt)) return;
+    if (!find_tile(p, block / p.hkv / p.splits, rt)) return;
     const Seq& q = rt.seq;
     const int s = rt.s, row0 = rt.row0, rows = rt.rows, all_rows = q.n * p.group;
     if (q.bad) {
@@ -806,6 +819,9 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 
     const int row = row0 + wave * 32 + i;  // the lane's
     const bool row_ok = row < all_rows;
+    // Positions of the wave's rows, of which there may be none.
+    const bool idle = row0 + wave * 32 >= all_rows;
+    const int wlo = q.len - q.n + min(row0 + wave * 32, all_rows - 1) / p.group, whi = q.len - q.n + min(row0 + wave * 32 + 31, all_rows - 1) / p.group;
     const int clamped = min(row, all_rows - 1);
     const int place = q.len - q.n + clamped / p.group;
     Vec8 qf[kKs];
@@ -824,7 +840,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
     const int page_mask = (1 << p.log2_page) - 1;
     const uint16_t* kbase = p.k + ((int64_t)kvh << p.log2_page) * D;
     const uint16_t* vbase = p.v + ((int64_t)kvh << p.log2_page) * D;
-    const uint32_t lds0 = (uint32_t)(size_t)(lds_u8*)&sh_tiles[0][0][0];
+    const uint32_t lds0 = (uint32_t)(size_t)(lds_u8*)&sh.tiles[0][0][0];
     int bad = 0;
 
     auto used = [&](int t) { return t <= hi && (t < p.sinks || t >= tiles.first); };
@@ -841,15 +857,22 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) key_off[j] = (uint32_t)(in * D + (piece ^ key_place<D>(j * kTokensPerLoad + in)) * 8) * 2;
     const uint32_t value_off = (uint32_t)(in * D + (piece ^ value_place<D>(in)) * 8) * 2;
+    // A token that no row sees stands for `safe`, which one does, and is masked.
+    // The page of the tile after the one that is fetched is asked for in advance.
+    const int safe = p.window > 0 ? hi : 0;
+    auto page_of = [&](int step) {
+        const int t0 = tiles.token(step) + wave * 16;
+        const int t = step < end && t0 <= hi && (t0 < p.sinks || t0 + 15 >= tiles.first) ? t0 : safe;
+        return ((const __attribute__((address_space(4))) int32_t*)trow)[__builtin_amdgcn_readfirstlane(t >> p.log2_page)];
+    };
+    int page_ahead = WHOLE && begin < end ? page_of(begin) : 0;
     auto fetch = [&](int step, int buffer) {
         const int t0 = tiles.token(step) + wave * 16;
         const uint32_t kdst = lds0 + (buffer * 2) * kTileBytes + wave * (kTileBytes / kWaves);
         if constexpr (WHOLE) {
-            // Tokens that no row sees stand for page 0 and are masked.
-            const bool any = t0 <= hi && (t0 < p.sinks || t0 + 15 >= tiles.first);
-            int page = 0;
-            if (any) page = checked(((const __attribute__((address_space(4))) int32_t*)trow)[__builtin_amdgcn_readfirstlane(t0 >> p.log2_page)]);
-            const int64_t off = (int64_t)__builtin_amdgcn_readfirstlane(page) * p.page_stride + (int64_t)((t0 & page_mask) * D);
+            const int page = __builtin_amdgcn_readfirstlane(checked(page_ahead));
+            page_ahead = page_of(step + 1);
+            const int64_t off = (int64_t)page * p.page_stride + (int64_t)((t0 & page_mask) * D);
             const uint16_t *ks = kbase + off, *vs = vbase + off;
             unrolled<kLoads>([&](auto j) {
                 dma16_at<j * 1024>(ks, key_off[j], kdst);
@@ -859,7 +882,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int t = t0 + j * kTokensPerLoad + in;
-                const int page = used(t) ? checked(trow[t >> p.log2_page]) : 0;
+                const int page = checked(trow[(used(t) ? t : safe) >> p.log2_page]);
                 const int64_t off = (int64_t)page * p.page_stride + (int64_t)(t & page_mask) * D;
                 dma16(kbase + off + (key_off[j] / 2 - in * D), kdst + j * 1024);
                 dma16(vbase + off + (value_off / 2 - in * D), kdst + kTileBytes + j * 1024);
@@ -873,8 +896,8 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
     Softmax sm;
-    if (tid < kEdges) sh_partly[tid] = 0;
-    if (tid == 0) sh_bad = 0;
+    if (tid < kEdges) sh.partly[tid] = 0;
+    if (tid == 0) sh.bad = 0;
     int edges = 0;
 
     // LDS addresses in buffer 0.  A key piece's place depends on the piece and the
@@ -895,7 +918,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
     // noted; what was not finite is added at the end to the rows that see it.
     auto clean = [&](int t0, uint32_t at) {
         const int edge = min(edges++, kEdges - 1);
-        if (tid == 0) sh_edge[edge] = t0;
+        if (tid == 0) sh.edge[edge] = t0;
 #pragma unroll 1
         for (int x = tid; x < kTileTokens * kPieces; x += kThreads) {
             const int t = t0 + x / kPieces;
@@ -911,15 +934,15 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
             }
             if (same) continue;
             lds_write(at + x * 16, f);
-            if (any) atomicOr(&sh_partly[edge], 1ull << (x / kPieces));
+            if (any) atomicOr(&sh.partly[edge], 1ull << (x / kPieces));
         }
         lds_barrier();
     };
     auto add_others = [&] {
         for (int e = 0; e < min(edges, kEdges); ++e) {
-            uint64_t tokens = sh_partly[e];
+            uint64_t tokens = sh.partly[e];
             while (tokens) {
-                const int t = sh_edge[e] + __builtin_ctzll(tokens);
+                const int t = sh.edge[e] + __builtin_ctzll(tokens);
                 tokens &= tokens - 1;
                 const uint16_t* src = vbase + (int64_t)checked(trow[t >> p.log2_page]) * p.page_stride + (int64_t)(t & page_mask) * D;
                 if (!sees(p, place, t)) continue;
@@ -947,6 +970,8 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
         const bool all = tl <= lo && (tl < p.sinks || t0 > hi - p.window);  // every row sees every token
         if (!all) clean(t0, lds0 + kTileBytes + at);
 
+        // A tile that none of the wave's rows sees.
+        if (idle || t0 > whi || (t0 >= p.sinks && tl <= wlo - p.window)) continue;
         float16v st[2];
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
@@ -966,7 +991,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
-        if (!all) {
+        if (!(tl <= wlo && (tl < p.sinks || t0 > whi - p.window))) {
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
@@ -1014,9 +1039,9 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
 
     float l = pair_sum<true>(sm.l);
     // A page outside the cache, met by any wave: the sum of every row is NaN.
-    if (bad) sh_bad = 1;
+    if (bad) sh.bad = 1;
     lds_barrier();
-    if (sh_bad) l = NAN;
+    if (sh.bad) l = NAN;
     add_others();
     if (!row_ok) return;
     if (p.splits == 1) {
@@ -1032,6 +1057,25 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
                     float4v{o[dt][r4 * 4], o[dt][r4 * 4 + 1], o[dt][r4 * 4 + 2], o[dt][r4 * 4 + 3]};
         if (h == 0) p.tile_ml[slot] = make_float2(sm.m, l);
     }
+}
+
+template <typename T, int D, bool WHOLE>
+__global__ __launch_bounds__(kThreads, 2) void tile_kernel(const Params p) {
+    __shared__ __align__(16) TileShared<D> sh;
+    tile_body<T, D, WHOLE>(p, blockIdx.x, sh);
+}
+
+// A mixed batch in one launch: row tiles, then units of few rows.  Neither waits
+// for the other, and the units, which are bound by memory, run beside the row
+// tiles.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void mixed_kernel(const Params p, int tile_blocks) {
+    __shared__ __align__(16) union {
+        TileShared<D> tile;
+        FewShared<D, kWaves> few;
+    } sh;
+    if ((int)blockIdx.x < tile_blocks) tile_body<T, D, true>(p, blockIdx.x, sh.tile);
+    else few_body<T, D, true, kWaves>(p, blockIdx.x - tile_blocks, sh.few);
 }
 
 // One workgroup per (token, query head) of the sequences that tile_kernel took.
@@ -1124,29 +1168,31 @@ wq_status check_sizes(const char* fn, int64_t seqs, int64_t tokens, int64_t max_
     WQ_TRY(in_range(fn, "window", window, 0, (int64_t)1 << 30));
     WQ_TRY(in_range(fn, "sinks", sinks, 0, (int64_t)1 << 30));
     const Plan pl = plan_of(seqs, tokens, max_query, hq, hkv, dim, max_len, window, sinks);
-    if (pl.units * hkv > INT32_MAX || seqs * pl.few_slots * hkv > INT32_MAX || pl.row_tiles * pl.splits * hkv > INT32_MAX || tokens * hq > INT32_MAX)
+    if (pl.units * hkv > INT32_MAX || seqs * pl.few_slots * hkv > INT32_MAX || pl.row_tiles * pl.splits * hkv + pl.units * hkv > INT32_MAX || tokens * hq > INT32_MAX)
         return err(WQ_ERR_INVALID_ARG, "%s: too many workgroups for one launch", fn);
     return WQ_OK;
 }
 
 template <typename T, int D>
 hipError_t launch(const Params& p, const Plan& pl, hipStream_t stream) {
-    if (pl.tiles) {
-        const dim3 grid((unsigned)(pl.row_tiles * pl.splits * p.hkv));
-        if (p.log2_page >= 4) hipLaunchKernelGGL((tile_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, p);
-        else hipLaunchKernelGGL((tile_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, p);
-        if (pl.splits > 1) hipLaunchKernelGGL((tile_merge_kernel<T, D>), dim3((unsigned)(p.num_tokens * p.hq)), dim3(kThreads), 0, stream, p);
+    const int64_t tile_blocks = pl.tiles ? pl.row_tiles * pl.splits * p.hkv : 0, few_blocks = pl.few ? (int64_t)p.units * p.hkv : 0;
+    const dim3 tiles((unsigned)tile_blocks), few((unsigned)few_blocks);
+    const bool split = p.units > p.num_seqs;
+    if (pl.tiles && pl.few && p.log2_page >= 4) {
+        hipLaunchKernelGGL((mixed_kernel<T, D>), dim3((unsigned)(tile_blocks + few_blocks)), dim3(kThreads), 0, stream, p, (int)tile_blocks);
+    } else {
+        if (pl.tiles && p.log2_page >= 4) hipLaunchKernelGGL((tile_kernel<T, D, true>), tiles, dim3(kThreads), 0, stream, p);
+        else if (pl.tiles) hipLaunchKernelGGL((tile_kernel<T, D, false>), tiles, dim3(kThreads), 0, stream, p);
+        if (pl.few) {
+            const bool whole = p.log2_page >= 3;
+            if (whole && split) hipLaunchKernelGGL((few_kernel<T, D, true, 4>), few, dim3(256), 0, stream, p);
+            else if (whole) hipLaunchKernelGGL((few_kernel<T, D, true, 8>), few, dim3(512), 0, stream, p);
+            else if (split) hipLaunchKernelGGL((few_kernel<T, D, false, 4>), few, dim3(256), 0, stream, p);
+            else hipLaunchKernelGGL((few_kernel<T, D, false, 8>), few, dim3(512), 0, stream, p);
+        }
     }
-    if (pl.few) {
-        const dim3 grid((unsigned)(p.units * p.hkv));
-        const bool whole = p.log2_page >= 3, split = p.units > p.num_seqs;
-        if (whole && split) hipLaunchKernelGGL((few_kernel<T, D, true, 4>), grid, dim3(256), 0, stream, p);
-        else if (whole) hipLaunchKernelGGL((few_kernel<T, D, true, 8>), grid, dim3(512), 0, stream, p);
-        else if (split) hipLaunchKernelGGL((few_kernel<T, D, false, 4>), grid, dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((few_kernel<T, D, false, 8>), grid, dim3(512), 0, stream, p);
-        if (p.units > p.num_seqs)
-            hipLaunchKernelGGL((few_merge_kernel<T, D>), dim3((unsigned)(p.num_seqs * p.few_slots * p.hkv)), dim3(kThreads), 0, stream, p);
-    }
+    if (pl.tiles && pl.splits > 1) hipLaunchKernelGGL((tile_merge_kernel<T, D>), dim3((unsigned)(p.num_tokens * p.hq)), dim3(kThreads), 0, stream, p);
+    if (pl.few && split) hipLaunchKernelGGL((few_merge_kernel<T, D>), dim3((unsigned)(p.num_seqs * p.few_slots * p.hkv)), dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
