@@ -129,6 +129,29 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
         if (c.frequency) r.frequency = c.frequency[row];
         if (c.presence) r.presence = c.presence[row];
     }
+    // The first vectors and their mask words are on their way while the history is
+    // counted.
+    typedef T Vec __attribute__((ext_vector_type(kPer)));
+    constexpr int kUnroll = 4;
+    const int vectors = VECTOR ? (end - from) / kPer : 0;
+    const int words = (vocab + 31) >> 5;
+    struct Batch {
+        Vec in[kUnroll];
+        uint32_t lo[kUnroll], hi[kUnroll];
+    } batch;
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j) {
+            const int w = from + min(i0 + j * kThreads, vectors - 1) * kPer;
+            batch.in[j] = __builtin_nontemporal_load(gbl(reinterpret_cast<const Vec*>(x + w)));
+            if (mask) {
+                batch.lo[j] = mask[w >> 5];
+                batch.hi[j] = mask[min((w >> 5) + 1, words - 1)];
+            }
+        }
+    };
+    if (vectors > 0) load(tid);
+
     if constexpr (HISTORY || BIAS) {
         const int entries = (p.tile + kPer) * (HISTORY + BIAS);
         for (int i = tid * 4; i < entries; i += kThreads * 4) *reinterpret_cast<u32x4*>(smem + i) = u32x4{0, 0, 0, 0};
@@ -145,20 +168,26 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
                 else atomicAdd(&uses[w - base], 1u);
             }
         };
-        // Four words at a time from the first 16-byte boundary on.
+        // Four words at a time from the first 16-byte boundary on, several loads in
+        // flight.
         const int lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(h) & 15)) & 15) / 4);
         if (tid < lead) use(tid, h[tid]);
-        for (int i = lead + tid * 4; i < n; i += kThreads * 4) {
-            if (i + 4 <= n) {
-                const int4v w = *reinterpret_cast<const int4v*>(h + i);
-                use(i, w.x);
-                use(i + 1, w.y);
-                use(i + 2, w.z);
-                use(i + 3, w.w);
-            } else {
-                for (int j = i; j < n; ++j) use(j, h[j]);
+        const int whole = (n - lead) / 4;
+        constexpr int kAhead = 4;
+        for (int i0 = tid; i0 < whole; i0 += kThreads * kAhead) {
+            int4v w[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) w[j] = *gbl(reinterpret_cast<const int4v*>(h + lead) + min(i0 + j * kThreads, whole - 1));
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int i = i0 + j * kThreads;
+                if (i >= whole) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) use(lead + 4 * i + e, w[j][e]);
             }
         }
+        const int rest = lead + 4 * whole + tid;
+        if (rest < n) use(rest, h[rest]);
     }
     if constexpr (BIAS) {
         const int32_t* ids = c.bias_ids + row * c.bias_size;
@@ -189,31 +218,17 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
     if constexpr (!VECTOR) {
         for (int w = begin + tid; w < end; w += kThreads) one(w);
     } else {
-        typedef T Vec __attribute__((ext_vector_type(kPer)));
         if (blockIdx.x == 0 && tid < from) one(tid);
-        const int vectors = (end - from) / kPer;
-        constexpr int kUnroll = 4;
-        const int words = (vocab + 31) >> 5;
         for (int i0 = tid; i0 < vectors; i0 += kThreads * kUnroll) {
-            Vec in[kUnroll];
-            uint32_t ok[kUnroll];
-#pragma unroll
-            for (int j = 0; j < kUnroll; ++j) {
-                const int i = min(i0 + j * kThreads, vectors - 1), w = from + i * kPer;
-                in[j] = *gbl(reinterpret_cast<const Vec*>(x + w));
-                ok[j] = ~0u;
-                if (mask) {
-                    const uint32_t lo = mask[w >> 5], hi = mask[min((w >> 5) + 1, words - 1)];
-                    ok[j] = __builtin_amdgcn_alignbit(hi, lo, w & 31);
-                }
-            }
+            if (i0 != tid) load(i0);
 #pragma unroll
             for (int j = 0; j < kUnroll; ++j) {
                 const int i = i0 + j * kThreads, w = from + i * kPer;
                 if (i >= vectors) break;
+                const uint32_t ok = mask ? __builtin_amdgcn_alignbit(batch.hi[j], batch.lo[j], w & 31) : ~0u;
                 float v[kPer];
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) v[e] = (float)in[j][e];
+                for (int e = 0; e < kPer; ++e) v[e] = (float)batch.in[j][e];
                 if constexpr (HISTORY || BIAS) {
                     u32x4 used[kPer / 4] = {}, named[kPer / 4] = {};
                     u32x4 any = {0, 0, 0, 0};
@@ -230,11 +245,11 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
                 Vec out;
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
-                    const bool allowed = ok[j] >> e & 1;
+                    const bool allowed = ok >> e & 1;
                     take(v[e], w + e, allowed);
                     out[e] = (T)(allowed ? v[e] : -INFINITY);
                 }
-                *gbl(reinterpret_cast<Vec*>(y + w)) = out;
+                __builtin_nontemporal_store(out, gbl(reinterpret_cast<Vec*>(y + w)));
             }
         }
         const int rest = from + vectors * kPer + tid;
