@@ -4,8 +4,8 @@
 // The logits are read once and written once, which is what bounds large
 // batches.  A workgroup takes a tile of one row's words.  What it has to know of
 // the row's history is how often each word of its tile occurs, so it scans the
-// history once (a few thousand words, from L2) into counters in LDS, adds the
-// positions of listed biases beside them, and then streams its tile: 16 bytes
+// history once (a few thousand words, from L2) into counters in LDS, marks the
+// listed biases there, and then streams its tile: 16 bytes
 // per lane and load, whatever word the row starts at, as long as input and
 // output rows lie alike.  The best word of each tile goes to the workspace and
 // pick_kernel takes the best of a row's.  Integer LDS atomics are the only
@@ -32,7 +32,10 @@ using namespace host;
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kPickThreads = 64;
-constexpr uint32_t kPrompt = 0x80000000u;  // the word occurs in the prompt; below it the times it was generated
+// A word's counter: the times it was generated, and whether it occurs in the
+// prompt and in the bias list.
+constexpr uint32_t kPrompt = 0x80000000u, kListed = 0x40000000u, kTimes = kListed - 1;
+constexpr int kTileBias = 256;  // biases of one tile that are kept in LDS
 constexpr int kMinTile = 2048, kMaxTile = 8192;
 
 typedef int int4v __attribute__((ext_vector_type(4)));
@@ -80,21 +83,39 @@ __device__ __forceinline__ void best_of_wave(float& v, int& w) {
 
 struct Row {
     float repetition, frequency, presence;
-    const float* bias;  // bias value of list position i
+    // The row's bias list, and the part of it in this tile: (word, position).
+    const int32_t* ids;
+    const float* values;
+    int listed;
+    const int2* tile_bias;
+    const int* tile_listed;
 };
 
-// A word's value.  `uses`: the counter of its history; `listed`: its position
-// in the bias list plus one, or 0.
-__device__ __forceinline__ float adjusted(float x, uint32_t uses, uint32_t listed, const Row& r) {
+// The bias of a word that the row lists: that of its last position.
+__device__ __forceinline__ float bias_of(int w, const Row& r) {
+    int at = -1;
+    const int n = *r.tile_listed;
+    if (n <= kTileBias) {
+        for (int i = 0; i < n; ++i)
+            if (r.tile_bias[i].x == w) at = max(at, r.tile_bias[i].y);
+    } else {
+        for (int i = 0; i < r.listed; ++i)
+            if (r.ids[i] == w) at = i;
+    }
+    return r.values[at];
+}
+
+// A word's value, `uses` being its counter.
+__device__ __forceinline__ float adjusted(float x, uint32_t uses, int w, const Row& r) {
 #pragma clang fp contract(off)
-    if (uses) {
+    if (uses & ~kListed) {
         x = x > 0.0f ? x / r.repetition : x * r.repetition;
-        const uint32_t c = uses & ~kPrompt;
+        const uint32_t c = uses & kTimes;
         const float taken = r.frequency * (float)c;
         x = x - taken;
         if (c) x = x - r.presence;
     }
-    if (listed) x = x + r.bias[listed - 1];
+    if (uses & kListed) x = x + bias_of(w, r);
     return x;
 }
 
@@ -104,8 +125,10 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
     constexpr int kPer = Type<T>::kPer;
     __shared__ float sh_v[kWaves];
     __shared__ int sh_w[kWaves];
-    uint32_t* uses = smem;                                   // [tile + kPer] where HISTORY
-    uint32_t* listed = smem + (HISTORY ? p.tile + kPer : 0);  // [tile + kPer] where BIAS
+    __shared__ int2 sh_bias[BIAS ? kTileBias : 1];
+    __shared__ int sh_listed;
+    constexpr bool COUNTS = HISTORY || BIAS;
+    uint32_t* uses = smem;  // [tile + kPer] counters, where there are any
     const wq_logits_call& c = p.c;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.y;
@@ -123,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
     const int from = VECTOR && blockIdx.x == 0 ? min(head, end) : begin;  // words from here on come in vectors
     const int base = VECTOR ? from - kPer : begin;
 
-    Row r{1.0f, 0.0f, 0.0f, nullptr};
+    Row r{1.0f, 0.0f, 0.0f, nullptr, nullptr, 0, sh_bias, &sh_listed};
     if constexpr (HISTORY) {
         if (c.repetition) r.repetition = c.repetition[row];
         if (c.frequency) r.frequency = c.frequency[row];
@@ -152,8 +175,9 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
     };
     if (vectors > 0) load(tid);
 
-    if constexpr (HISTORY || BIAS) {
-        const int entries = (p.tile + kPer) * (HISTORY + BIAS);
+    if constexpr (COUNTS) {
+        const int entries = p.tile + kPer;
+        if (BIAS && tid == 0) sh_listed = 0;
         for (int i = tid * 4; i < entries; i += kThreads * 4) *reinterpret_cast<u32x4*>(smem + i) = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
@@ -190,16 +214,20 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
         if (rest < n) use(rest, h[rest]);
     }
     if constexpr (BIAS) {
-        const int32_t* ids = c.bias_ids + row * c.bias_size;
-        r.bias = c.bias_values + row * c.bias_size;
-        int n = (int)c.bias_size;
-        if (c.bias_lens) n = min(max(c.bias_lens[row], 0), n);
-        for (int i = tid; i < n; i += kThreads) {
-            const int w = ids[i];
-            if (w >= begin && w < end) atomicMax(&listed[w - base], (uint32_t)i + 1u);
+        r.ids = c.bias_ids + row * c.bias_size;
+        r.values = c.bias_values + row * c.bias_size;
+        r.listed = (int)c.bias_size;
+        if (c.bias_lens) r.listed = min(max(c.bias_lens[row], 0), r.listed);
+        for (int i = tid; i < r.listed; i += kThreads) {
+            const int w = r.ids[i];
+            if (w >= begin && w < end) {
+                atomicOr(&uses[w - base], kListed);
+                const int at = atomicAdd(&sh_listed, 1);
+                if (at < kTileBias) sh_bias[at] = make_int2(w, i);
+            }
         }
     }
-    if constexpr (HISTORY || BIAS) __syncthreads();
+    if constexpr (COUNTS) __syncthreads();
 
     float top = -INFINITY;
     int word = -1;
@@ -211,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
     };
     auto one = [&](int w) {
         const bool allowed = !mask || (mask[w >> 5] >> (w & 31) & 1);
-        const float v = adjusted((float)x[w], HISTORY ? uses[w - base] : 0, BIAS ? listed[w - base] : 0, r);
+        const float v = adjusted((float)x[w], COUNTS ? uses[w - base] : 0, w, r);
         y[w] = (T)(allowed ? v : -INFINITY);
         take(v, w, allowed);
     };
@@ -229,17 +257,14 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const Params p) {
                 float v[kPer];
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) v[e] = (float)batch.in[j][e];
-                if constexpr (HISTORY || BIAS) {
-                    u32x4 used[kPer / 4] = {}, named[kPer / 4] = {};
+                if constexpr (COUNTS) {
+                    u32x4 used[kPer / 4];
                     u32x4 any = {0, 0, 0, 0};
 #pragma unroll
-                    for (int e = 0; e < kPer / 4; ++e) {
-                        if constexpr (HISTORY) any |= used[e] = *reinterpret_cast<const u32x4*>(uses + (w - base) + 4 * e);
-                        if constexpr (BIAS) any |= named[e] = *reinterpret_cast<const u32x4*>(listed + (w - base) + 4 * e);
-                    }
+                    for (int e = 0; e < kPer / 4; ++e) any |= used[e] = *reinterpret_cast<const u32x4*>(uses + (w - base) + 4 * e);
                     if (any.x | any.y | any.z | any.w) {
 #pragma unroll
-                        for (int e = 0; e < kPer; ++e) v[e] = adjusted(v[e], used[e / 4][e % 4], named[e / 4][e % 4], r);
+                        for (int e = 0; e < kPer; ++e) v[e] = adjusted(v[e], used[e / 4][e % 4], w + e, r);
                     }
                 }
                 Vec out;
@@ -311,7 +336,7 @@ wq_status check_sizes(const char* fn, int64_t rows, int64_t vocab, int64_t dtype
 template <typename T, bool HISTORY, bool BIAS>
 void launch_as(const Params& p, bool vector, hipStream_t stream) {
     const dim3 grid((unsigned)p.tiles, (unsigned)p.c.rows);
-    const size_t lds = (size_t)(HISTORY + BIAS) * (p.tile + Type<T>::kPer) * 4;
+    const size_t lds = HISTORY || BIAS ? (size_t)(p.tile + Type<T>::kPer) * 4 : 0;
     if (vector) hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, true>), grid, dim3(kThreads), lds, stream, p);
     else hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, false>), grid, dim3(kThreads), lds, stream, p);
 }
