@@ -79,6 +79,62 @@ __device__ __forceinline__ void best_of_wave(float& v, int& w) {
     }
 }
 
+// The words of 16 bytes of logits with those masked that `ok` does not allow,
+// and the largest value left (NaN left out).
+template <typename T>
+__device__ __forceinline__ float mask_and_max(u32x4& w, uint32_t ok) {
+    float m = -INFINITY;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            const uint32_t v = ok >> d & 1 ? w[d] : 0xFF800000u;
+            w[d] = v;
+            m = fmaxf(m, __builtin_bit_cast(float, v));
+        }
+    } else {
+        constexpr uint32_t kLowest = std::is_same_v<T, _Float16> ? 0xFC00FC00u : 0xFF80FF80u;  // two of -infinity
+        dev::half2v pair = dev::as_h2(0xFC00FC00u);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            const uint32_t lo = (uint32_t)((int)(ok << (31 - 2 * d)) >> 31), hi = (uint32_t)((int)(ok << (30 - 2 * d)) >> 31);
+            const uint32_t keep = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+            w[d] = (w[d] & keep) | (kLowest & ~keep);
+            if constexpr (std::is_same_v<T, _Float16>) {
+                pair = __builtin_elementwise_max(pair, dev::as_h2(w[d]));
+            } else {
+                m = fmaxf(m, __builtin_bit_cast(float, w[d] << 16));
+                m = fmaxf(m, __builtin_bit_cast(float, w[d] & 0xFFFF0000u));
+            }
+        }
+        if constexpr (std::is_same_v<T, _Float16>) m = fmaxf((float)pair.x, (float)pair.y);
+    }
+    return m;
+}
+
+// Element e of 16 bytes of logits.
+template <typename T>
+__device__ __forceinline__ T element(const u32x4 w, int e) {
+    const int d = sizeof(T) == 4 ? e : e / 2;
+    const uint32_t v = d == 0 ? w.x : d == 1 ? w.y : d == 2 ? w.z : w.w;
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, v);
+    else return __builtin_bit_cast(T, (uint16_t)(v >> (16 * (e & 1))));
+}
+template <typename T>
+__device__ __forceinline__ void set_element(u32x4& w, int e, T x) {
+    const int d = sizeof(T) == 4 ? e : e / 2;
+    uint32_t bits, keep = 0;
+    if constexpr (sizeof(T) == 4) {
+        bits = __builtin_bit_cast(uint32_t, x);
+    } else {
+        bits = (uint32_t)__builtin_bit_cast(uint16_t, x) << (16 * (e & 1));
+        keep = e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+    }
+    w.x = d == 0 ? (w.x & keep) | bits : w.x;
+    w.y = d == 1 ? (w.y & keep) | bits : w.y;
+    w.z = d == 2 ? (w.z & keep) | bits : w.z;
+    w.w = d == 3 ? (w.w & keep) | bits : w.w;
+}
+
 struct Row {
     float repetition, frequency, presence;
     // The row's bias list, and the part of it in this tile: (word, position).
@@ -228,13 +284,14 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const Params p) {
     }
     if constexpr (COUNTS) __syncthreads();
 
+    // The best word so far, or the first word of the vector `best` that holds it.
     float top = -INFINITY;
     int word = -1;
+    Vec best = {};
+    uint32_t best_ok = 0;
+    // (Words come in any order.)
     auto take = [&](float v, int w, bool allowed) {
-        if (allowed && (v > top || (word < 0 && v == v))) {
-            top = v;
-            word = w;
-        }
+        if (allowed && v == v) better(top, word, v, w);
     };
     auto one = [&](int w) {
         const bool allowed = !mask || (mask[w >> 5] >> (w & 31) & 1);
@@ -245,7 +302,6 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const Params p) {
     if constexpr (!VECTOR) {
         for (int w = begin + tid; w < end; w += kThreads) one(w);
     } else {
-        if (blockIdx.x == 0 && tid < from) one(tid);
         for (int i0 = tid; i0 < vectors; i0 += kThreads * kUnroll) {
             if (i0 != tid) load(i0);
 #pragma unroll
@@ -253,42 +309,88 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const Params p) {
                 const int i = i0 + j * kThreads, w = from + i * kPer;
                 if (i >= vectors) break;
                 const uint32_t ok = mask ? __builtin_amdgcn_alignbit(batch.hi[j], batch.lo[j], w & 31) : ~0u;
-                float v[kPer];
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) v[e] = (float)batch.in[j][e];
+                u32x4 bits = __builtin_bit_cast(u32x4, batch.in[j]);
+                uint32_t changed = 0;  // words that the history or the bias list changes
                 if constexpr (COUNTS) {
                     u32x4 used[kPer / 4];
-                    u32x4 any = {0, 0, 0, 0};
+                    uint32_t any = 0;
 #pragma unroll
-                    for (int e = 0; e < kPer / 4; ++e) any |= used[e] = *reinterpret_cast<const u32x4*>(uses + (w - base) + 4 * e);
-                    if (any.x | any.y | any.z | any.w) {
+                    for (int e = 0; e < kPer / 4; ++e) {
+                        used[e] = *reinterpret_cast<const u32x4*>(uses + (w - base) + 4 * e);
+                        any |= used[e].x | used[e].y | used[e].z | used[e].w;
+                    }
+                    if (any) {
 #pragma unroll
-                        for (int e = 0; e < kPer; ++e) v[e] = adjusted(v[e], used[e / 4][e % 4], w + e, r);
+                        for (int e = 0; e < kPer; ++e) changed |= used[e / 4][e % 4] ? 1u << e : 0u;
                     }
                 }
-                Vec out;
+                // The others stay as they are.
+                float m = mask_and_max<T>(bits, ok & ~changed);
+                // Few vectors have any, and those seldom more than one, which is taken
+                // by itself; where some lane has several (common words lie together),
+                // all eight are formed at once.
+                if (__builtin_amdgcn_ballot_w64((changed & (changed - 1)) != 0)) {
+                    if (changed) {
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) {
-                    const bool allowed = ok >> e & 1;
-                    take(v[e], w + e, allowed);
-                    out[e] = (T)(allowed ? v[e] : -INFINITY);
+                        for (int e = 0; e < kPer; ++e) {
+                            if (!(changed & ok & 1u << e)) continue;
+                            const float v = adjusted((float)batch.in[j][e], uses[w - base + e], w + e, r);
+                            m = fmaxf(m, v);
+                            set_element<T>(bits, e, (T)v);
+                        }
+                    }
+                } else if (changed & ok) {
+                    const int e = __builtin_ctz(changed);
+                    const float v = adjusted((float)element<T>(__builtin_bit_cast(u32x4, batch.in[j]), e), uses[w - base + e], w + e, r);
+                    m = fmaxf(m, v);
+                    set_element<T>(bits, e, (T)v);
                 }
-                __builtin_nontemporal_store(out, gbl(reinterpret_cast<Vec*>(y + w)));
+                if (m > top) {
+                    top = m;
+                    word = w;
+                    best = batch.in[j];
+                    best_ok = ok;
+                }
+                __builtin_nontemporal_store(bits, gbl(reinterpret_cast<u32x4*>(y + w)));
             }
         }
+        if (blockIdx.x == 0 && tid < from) one(tid);
         const int rest = from + vectors * kPer + tid;
         if (rest < end) one(rest);
     }
     if (!c.token) return;
-    best_of_wave<64>(top, word);
-    if ((tid & 63) == 0) {
-        sh_v[tid >> 6] = top;
-        sh_w[tid >> 6] = word;
-    }
-    __syncthreads();
-    if (tid == 0) {
+    auto best_of_block = [&] {
+        best_of_wave<64>(top, word);
+        if ((tid & 63) == 0) {
+            sh_v[tid >> 6] = top;
+            sh_w[tid >> 6] = word;
+        }
+        __syncthreads();
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) better(top, word, sh_v[i], sh_w[i]);
+        for (int i = 0; i < kWaves; ++i) better(top, word, sh_v[i], sh_w[i]);
+    };
+    const float my_top = top;
+    const int my_word = word;
+    best_of_block();
+    bool mine = word >= 0 && my_word == word;
+    if (mine && best_ok && my_word >= from && my_word < from + vectors * kPer) {
+        // Which of the vector's words it is.
+        for (int e = kPer - 1; e >= 0; --e)
+            if (best_ok >> e & 1) {
+                const float v = COUNTS ? adjusted((float)best[e], uses[my_word - base + e], my_word + e, r) : (float)best[e];
+                if (v == my_top) word = my_word + e;
+            }
+    }
+    if (word < 0) {
+        // Nothing above -infinity: the first allowed word that is not NaN, from what
+        // was written.
+        __syncthreads();
+        for (int w = begin + tid; w < end && word < 0; w += kThreads)
+            if (!mask || (mask[w >> 5] >> (w & 31) & 1)) take((float)y[w], w, true);
+        best_of_block();
+        mine = tid == 0;
+    }
+    if (mine) {
         if (p.tiles == 1) {
             c.token[row] = word;
         } else {
