@@ -160,14 +160,14 @@ def _check(status: int) -> None:
 # pointers and the stream are passed as integers (the declared argument types
 # turn them into C values).
 
-_torch = None
+_torch = _Tensor = None
 _WORDS = _HALVES = _FLOATS = _INTS = _BYTES = ()
 _DTYPES = {}  # WQ_DTYPE_* of include/wq_logits.h
 _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _DTYPES, _raw_stream
+    global _torch, _Tensor, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _DTYPES, _raw_stream
     import torch
 
     _WORDS = (torch.int32, torch.uint32)
@@ -178,12 +178,16 @@ def _load_torch():
     _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
     # The current stream's handle without building a Stream object.
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _Tensor = torch.Tensor
     _torch = torch
     return torch
 
 
 def _dev_tensor(t, name, dtypes, shape):
     """The device address of `t` after the checks that every argument gets."""
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype in dtypes and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    # Something is wrong with it: say what.
     if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
@@ -192,9 +196,7 @@ def _dev_tensor(t, name, dtypes, shape):
         raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous (row-major)")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous (row-major)")
 
 
 def _stream(stream, t):
@@ -408,66 +410,69 @@ def window_attention(q, k_cache, v_cache, block_table, seq_lens, out, scale: flo
     apart (slices of a wider array).  `workspace` is from window_workspace
     (allocated here when omitted)."""
     _torch or _load_torch()
-    num_pages, hkv, page, d = _cache_dims(k_cache, "k_cache")
-    kind = k_cache.dtype
-    if q.dim() != 3 or block_table.dim() != 2:
+    shape, cached, rows = q.shape, k_cache.shape, block_table.shape
+    if len(shape) != 3 or len(rows) != 2:
         raise ValueError("q must be [T, HQ, D] and block_table [S, max_pages]")
-    if kind not in _DTYPES:
+    num_pages, hkv, page, d = cached if len(cached) == 4 else _cache_dims(k_cache, "k_cache")
+    kind = k_cache.dtype
+    if kind not in _DTYPES or k_cache.element_size() != 2:
+        _cache_dims(k_cache, "k_cache")
         raise TypeError(f"the caches must be fp16 or bf16 (got {kind})")
-    shape = q.shape
-    num_seqs, max_pages = block_table.shape
-    if shape[2] != d:
-        raise ValueError(f"q has head_dim {shape[2]}, the caches {d}")
+    tokens, hq, dim = shape
+    if dim != d:
+        raise ValueError(f"q has head_dim {dim}, the caches {d}")
+    num_seqs, max_pages = rows
+    kinds = (kind,)
     pq, qs = _rows_tensor(q, "q", kind, shape)
     po, os_ = _rows_tensor(out, "out", kind, shape)
-    pk = _dev_tensor(k_cache, "k_cache", (kind,), k_cache.shape)
-    pv = _dev_tensor(v_cache, "v_cache", (kind,), k_cache.shape)
-    pt = _dev_tensor(block_table, "block_table", _INTS, (num_seqs, max_pages))
+    pk = _dev_tensor(k_cache, "k_cache", kinds, cached)
+    pv = _dev_tensor(v_cache, "v_cache", kinds, cached)
+    pt = _dev_tensor(block_table, "block_table", _INTS, rows)
     pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
     ps = None if q_starts is None else _dev_tensor(q_starts, "q_starts", _INTS, (num_seqs + 1,))
     if workspace is None:
         workspace = window_workspace(q, hkv, num_seqs, max_seq_len, window, sinks, max_query_len)
     pw, nw = _workspace(workspace, q)
-    _check((_lib or lib()).wq_window_attention(pq, pk, pv, pt, pl, ps, po, num_seqs, shape[0], max_query_len, shape[1], hkv, d, qs, os_, page,
+    _check((_lib or lib()).wq_window_attention(pq, pk, pv, pt, pl, ps, po, num_seqs, tokens, max_query_len, hq, hkv, d, qs, os_, page,
                                                num_pages, max_pages, max_seq_len, window, sinks, float(scale), _DTYPES[kind], pw, nw,
                                                _stream(stream, q)))
 
 
 # ------------------------------------------------------- paged cache upkeep
 
-def _rows_tensor(t, name, dtype, shape, align=8):
+def _rows_tensor(t, name, dtype, shape):
     """Address and row stride of `t` [rows, heads, dim], whose rows may lie
     apart (a slice of a wider array) but are contiguous in themselves."""
-    if not isinstance(t, _torch.Tensor):
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype is dtype and t.shape == shape:
+        stride, head, one = t.stride()
+        if (one == 1 or shape[2] == 1) and (head == shape[2] or shape[1] == 1):
+            # (One row's stride says nothing.)
+            return t.data_ptr(), stride if shape[0] > 1 else shape[1] * shape[2]
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor (got {t.device})")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    stride, head, one = t.stride()
-    if t.shape[0] == 1:
-        stride = (t.shape[1] * t.shape[2] + align - 1) // align * align
-    if (one != 1 and t.shape[2] > 1) or (head != t.shape[2] and t.shape[1] > 1):
-        raise ValueError(f"the rows of {name} must be contiguous")
-    return t.data_ptr(), stride
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _workspace(workspace, t):
     if workspace is None:
         return None, 0
-    if workspace.device != t.device or workspace.dtype not in _BYTES or not workspace.is_contiguous():
+    if not workspace.is_cuda or workspace.get_device() != t.get_device() or workspace.dtype not in _BYTES or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous uint8 tensor on the device of the other arguments")
     return workspace.data_ptr(), workspace.numel()
 
 
 def _cache_dims(cache, name):
-    if cache.dim() != 4:
+    shape = cache.shape
+    if len(shape) != 4:
         raise ValueError(f"{name} must be [pages, HKV, P, D]")
     if cache.element_size() != 2:
         raise TypeError(f"{name} must hold 16-bit values (got {cache.dtype})")
-    return cache.shape
+    return shape
 
 
 def cache_append(k, v, k_cache, v_cache, block_table, seq_lens, q_starts=None, stream=None) -> None:
@@ -478,17 +483,19 @@ def cache_append(k, v, k_cache, v_cache, block_table, seq_lens, q_starts=None, s
     q_starts is None.  Rows of k and v may lie apart (slices of the QKV
     projection's output)."""
     _torch or _load_torch()
-    num_pages, hkv, page, d = _cache_dims(k_cache, "k_cache")
+    num_pages, hkv, page, d = cached = _cache_dims(k_cache, "k_cache")
     kind = k_cache.dtype
-    if block_table.dim() != 2 or k.dim() != 3:
+    shape, rows = k.shape, block_table.shape
+    if len(rows) != 2 or len(shape) != 3:
         raise ValueError("k must be [T, HKV, D] and block_table [S, max_pages]")
-    num_seqs, max_pages = block_table.shape
-    shape = (k.shape[0], hkv, d)
+    num_seqs, max_pages = rows
+    if shape[1] != hkv or shape[2] != d:
+        raise ValueError(f"k has shape {tuple(shape)}, the caches {hkv} heads of {d}")
     pk, ks = _rows_tensor(k, "k", kind, shape)
     pv, vs = _rows_tensor(v, "v", kind, shape)
-    pkc = _dev_tensor(k_cache, "k_cache", (kind,), k_cache.shape)
-    pvc = _dev_tensor(v_cache, "v_cache", (kind,), k_cache.shape)
-    pt = _dev_tensor(block_table, "block_table", _INTS, (num_seqs, max_pages))
+    pkc = _dev_tensor(k_cache, "k_cache", (kind,), cached)
+    pvc = _dev_tensor(v_cache, "v_cache", (kind,), cached)
+    pt = _dev_tensor(block_table, "block_table", _INTS, rows)
     pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
     ps = None if q_starts is None else _dev_tensor(q_starts, "q_starts", _INTS, (num_seqs + 1,))
     if shape[0] == 0:
@@ -544,10 +551,10 @@ def cache_copy_pages(caches: CacheSet, src, dst, stream=None) -> None:
 
 def _pool(block_table, refs):
     _torch or _load_torch()
-    if block_table.dim() != 2 or refs.dim() != 1:
+    rows, pages = block_table.shape, refs.shape
+    if len(rows) != 2 or len(pages) != 1:
         raise ValueError("block_table must be [S, max_pages] and refs [pages]")
-    return (_dev_tensor(block_table, "block_table", _INTS, block_table.shape), _dev_tensor(refs, "refs", _INTS, refs.shape),
-            block_table.shape[0], block_table.shape[1], refs.shape[0])
+    return (_dev_tensor(block_table, "block_table", _INTS, rows), _dev_tensor(refs, "refs", _INTS, pages), rows[0], rows[1], pages[0])
 
 
 def cache_reserve(block_table, refs, old_lens, new_lens, page_size: int, shortfall, workspace=None, stream=None) -> None:
@@ -622,16 +629,16 @@ def logits_workspace(logits):
 
 def _row_stride(t, name, shape):
     """Address and row stride of a device tensor whose rows may lie apart."""
-    if not isinstance(t, _torch.Tensor):
+    if isinstance(t, _Tensor) and t.is_cuda and t.shape == shape:
+        stride, one = t.stride()
+        if one == 1 or shape[1] == 1:
+            return t.data_ptr(), stride if shape[0] > 1 else shape[1]
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor (got {t.device})")
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    stride, one = t.stride()
-    if one != 1 and shape[1] > 1:
-        raise ValueError(f"the rows of {name} must be contiguous")
-    return t.data_ptr(), stride if shape[0] > 1 else max(stride, shape[1])
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def process_logits(logits, out, token=None, mask=None, history=None, history_lens=None, prompt_lens=None, repetition=None,
