@@ -124,7 +124,7 @@ struct Params {
     int32_t splits;
     float* tile_acc;   // [token][q head][splits][head_dim]
     float2* tile_ml;
-    int32_t tiles_too; // tile_kernel runs as well
+    int32_t few_rows;  // sequences of up to so many rows are few_kernel's, all others tile_kernel's
 };
 
 // ------------------------------------------------------------- sequences
@@ -132,7 +132,7 @@ struct Params {
 struct Seq {
     int first, n, len;  // first row of q, new tokens, tokens
     bool bad;           // its outputs are NaN
-    __device__ __forceinline__ bool few(const Params& p) const { return n * p.group <= kFewRows || !p.tiles_too; }
+    __device__ __forceinline__ bool few(const Params& p) const { return n * p.group <= p.few_rows; }
 };
 
 __device__ __forceinline__ Seq seq_of(const Params& p, int s) {
@@ -743,7 +743,8 @@ __device__ __forceinline__ bool find_tile(const Params& p, int tile, RowTile& ou
         int n = 0;
         if (s0 + lane < p.num_seqs) {
             const Seq q = seq_of(p, s0 + lane);
-            n = q.few(p) ? 0 : (q.n * p.group + kTileRows - 1) / kTileRows;
+            // (An invalid one may have more rows than the launch has tiles for: one writes its NaN.)
+            n = q.few(p) ? 0 : q.bad ? min(q.n, 1) : (q.n * p.group + kTileRows - 1) / kTileRows;
         }
         const int inc = inclusive_scan(n);
         const uint64_t owner = __builtin_amdgcn_ballot_w64(tile >= inc - n && tile < inc);
@@ -810,7 +811,7 @@ __device__ __forceinline__ void tile_body(const Params& p, int block, TileShared
     const int s = rt.s, row0 = rt.row0, rows = rt.rows, all_rows = q.n * p.group;
     if (q.bad) {
         if (split == 0)
-            for (int x = tid; x < rows * D; x += kThreads) out_row(p, q, kvh, row0 + x / D, D)[x % D] = Type<T>::kNaN;
+            for (int64_t x = tid; x < (int64_t)all_rows * D; x += kThreads) out_row(p, q, kvh, (int)(x / D), D)[x % D] = Type<T>::kNaN;
         return;
     }
     const int lo = q.len - q.n + row0 / p.group, hi = q.len - q.n + (row0 + rows - 1) / p.group;  // positions of the rows
@@ -1300,7 +1301,8 @@ wq_status wq_window_attention(const uint16_t* q, const uint16_t* k_cache, const 
     p.splits = (int32_t)pl.splits;
     p.tile_acc = reinterpret_cast<float*>(ws + pl.tile_acc);
     p.tile_ml = reinterpret_cast<float2*>(ws + pl.tile_ml);
-    p.tiles_too = pl.tiles;
+    // (With one sequence, whose n may be below num_tokens, only one kernel is launched.)
+    p.few_rows = !pl.tiles ? INT32_MAX : pl.few ? kFewRows : 0;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     hipError_t e;

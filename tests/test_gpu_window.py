@@ -347,3 +347,36 @@ def test_in_a_graph_on_another_stream():
             call()
             assert torch.equal(got, out)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("tokens,splits", [(17, False), (200, True)])
+def test_one_sequence_with_fewer_new_tokens_than_rows(tokens, splits):
+    """A buffer of rows that is not full: the sequence's rows are computed, few or many, and the rest is not written."""
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    lens = 4000 if splits else 300
+    for news in (1, 2, 4, 16, 17):
+        c = Case(41, "float16", [lens], [news], 2, 4, 64, 16, 5000, 4)
+        q = torch.cat([c.q, torch.zeros((tokens - news, 8, 64), dtype=c.kind, device="cuda")])
+        out = torch.full_like(q, 7.0)
+        wq.window_attention(q, c.k, c.v, ints(c.table), ints(c.lens), out, c.scale, lens, 5000, sinks=4, q_starts=ints([0, news]), max_query_len=tokens)
+        c.check(out[:news])
+        assert bool((out[news:] == 7.0).all())
+
+
+def test_a_sequence_beyond_the_query_bound_is_nan_in_every_row():
+    """Its rows are more than the launch has tiles for; the sequences after it keep theirs."""
+    import torch
+
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    c = Case(43, "float16", [900, 100, 60], [900, 100, 30], 1, 4, 64, 16, 2000, 0)
+    clean = c.run()
+    out = torch.full((1030, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+    wq.window_attention(c.q, c.k, c.v, ints(c.table), ints(c.lens), out, c.scale, 900, 2000, q_starts=ints(c.starts), max_query_len=100)
+    assert bool(torch.isnan(out[:900]).all())
+    c.check(torch.cat([clean[:900], out[900:]]))
