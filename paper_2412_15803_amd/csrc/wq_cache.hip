@@ -156,6 +156,7 @@ struct Survey {
     const int32_t* src;
     const int32_t* dst;
     int32_t num_seqs;
+    int32_t* length;  // [items] of each fork's source, -1: skipped
 };
 
 // Table entries [lo, hi) in which a growing sequence may lack pages.
@@ -225,14 +226,18 @@ __global__ __launch_bounds__(kThreads) void survey_kernel(const Survey p) {
     } else if constexpr (WHAT == kFork) {
         const int i = g * kGroupForks + threadIdx.x;
         bool need = false;
-        int s, d, len;
+        int s, d, len, length = -1;
         if (i < p.items && fork_of(p, i, s, d, len)) {
+            length = len;
             if (len & ((1 << p.log2_page) - 1)) {
                 const int tail = p.table[(int64_t)s * p.max_pages + (len >> p.log2_page)];
                 need = (uint32_t)tail < (uint32_t)p.num_pages;
             }
         }
-        if (i < p.items) p.need[i] = need;
+        if (i < p.items) {
+            p.need[i] = need;
+            p.length[i] = length;
+        }
         const uint64_t m = __builtin_amdgcn_ballot_w64(need);
         if (lane == 0) sums[wave] = __popcll(m);
         __syncthreads();
@@ -390,15 +395,17 @@ __global__ void zero_kernel(int32_t* word) {
 }
 
 // Workgroups (i, y): fork i, caches y, y + gridDim.y, ...  Those with y = 0
-// write the row as well.
+// write the row as well.  Lengths are those that the survey found, so that all
+// of a fork's workgroups go by the same one, also where a sequence is in both lists.
 __global__ __launch_bounds__(kThreads) void fork_kernel(const Fork p, const Arrays arrays) {
     __shared__ int shared_page;
     const Pool pool{p.s.bits, p.s.counts, p.s.blocks};
     const int i = blockIdx.x, g = i / kGroupForks, lane = lane_id();
     const int missing = sum_of(p.s.group, p.groups) - sum_of(pool.counts, pool.blocks);
     if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.shortfall = max(missing, 0);
-    int s, d, len;
-    if (missing > 0 || !fork_of(p.s, i, s, d, len)) return;
+    const int len = p.s.length[i];
+    if (missing > 0 || len < 0) return;
+    const int s = p.s.src[i], d = p.s.dst[i];
     const int page_size = 1 << p.s.log2_page, full = len >> p.s.log2_page, part = len & (page_size - 1);
     const bool need = p.s.need[i] != 0;
     const int32_t* from = p.table + (int64_t)s * p.s.max_pages;
@@ -572,10 +579,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const Append p) {
 constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 
-// The workspace, in 16-byte steps: counts, bits, needs, group sums, then
+// The workspace, in 16-byte steps: counts, bits, needs, lengths, group sums, then
 // compact's map and moves (a move's count first).
 struct Layout {
-    int64_t blocks, counts, bits, need, group, map, moves, total;
+    int64_t blocks, counts, bits, need, length, group, map, moves, total;
 };
 Layout layout_of(int64_t num_pages, int64_t num_seqs) {
     Layout l{};
@@ -589,6 +596,7 @@ Layout layout_of(int64_t num_pages, int64_t num_seqs) {
     l.counts = take(4 * l.blocks);
     l.bits = take(4 * l.blocks * kBlockWords);
     l.need = take(4 * num_seqs);
+    l.length = take(4 * num_seqs);
     l.group = take(4 * ceil_div(num_seqs, kGroupSeqs));
     l.map = take(4 * num_pages);
     l.moves = take(16 + 8 * num_pages);
@@ -662,6 +670,7 @@ Survey survey_of(const int32_t* refs, int64_t num_pages, void* ws, const Layout&
     s.counts = at<int32_t>(ws, l.counts);
     s.blocks = (int32_t)l.blocks;
     s.need = at<int32_t>(ws, l.need);
+    s.length = at<int32_t>(ws, l.length);
     s.group = at<int32_t>(ws, l.group);
     return s;
 }

@@ -335,3 +335,17 @@ def test_upkeep_in_a_graph_and_on_another_stream():
             assert gt.tolist() == table and gr.tolist() == refs and gl.tolist() == lens, replay
             assert np.array_equal(bits(gk), kc) and np.array_equal(bits(gv), vc)
     torch.cuda.synchronize()
+
+
+def test_a_sequence_forked_to_and_from_keeps_to_the_lengths_before_the_call():
+    """Not allowed, so its pages hold either content, but lengths and counts of every fork are those of the lists' start."""
+    from paper_2412_15803_amd import wq
+
+    require_gpu()
+    rng = np.random.default_rng(5)
+    g = [to_gpu(halves(rng, (8, 1, 4, 8))) for _ in range(3)]
+    for _ in range(5):
+        gt, gr, gl, gs = dev([[0, 1], [2, 3], [-1, -1]]), dev([1, 1, 1, 1, 0, 0, 0, 0]), dev([8, 6, 0]), dev([9])
+        wq.cache_fork(wq.cache_set(g), gt, gr, gl, dev([0, 1]), dev([1, 2]), gs)
+        assert gs.item() == 0 and gl.tolist() == [8, 8, 6] and gt.tolist()[1] == [0, 1] and gt.tolist()[2][1] == 4
+        assert gr.tolist()[4:] == [1, 0, 0, 0]
