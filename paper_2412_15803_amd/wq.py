@@ -431,7 +431,8 @@ def window_attention(q, k_cache, v_cache, block_table, seq_lens, out, scale: flo
     pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
     ps = None if q_starts is None else _dev_tensor(q_starts, "q_starts", _INTS, (num_seqs + 1,))
     if workspace is None:
-        workspace = window_workspace(q, hkv, num_seqs, max_seq_len, window, sinks, max_query_len)
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = window_workspace(q, hkv, num_seqs, max_seq_len, window, sinks, max_query_len)
     pw, nw = _workspace(workspace, q)
     _check((_lib or lib()).wq_window_attention(pq, pk, pv, pt, pl, ps, po, num_seqs, tokens, max_query_len, hq, hkv, d, qs, os_, page,
                                                num_pages, max_pages, max_seq_len, window, sinks, float(scale), _DTYPES[kind], pw, nw,
@@ -566,7 +567,8 @@ def cache_reserve(block_table, refs, old_lens, new_lens, page_size: int, shortfa
     pn = _dev_tensor(new_lens, "new_lens", _INTS, (num_seqs,))
     pf = _dev_tensor(shortfall, "shortfall", _INTS, (1,))
     if workspace is None:
-        workspace = page_workspace(num_pages, num_seqs, refs.device)
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = page_workspace(num_pages, num_seqs, refs.device)
     pw, nw = _workspace(workspace, refs)
     _check((_lib or lib()).wq_cache_reserve(pt, pr, po, pn, num_seqs, page_size, num_pages, max_pages, pf, pw, nw, _stream(stream, refs)))
 
@@ -594,7 +596,8 @@ def cache_fork(caches: CacheSet, block_table, refs, seq_lens, src, dst, shortfal
     pd = _dev_tensor(dst, "dst", _INTS, (n,))
     pf = _dev_tensor(shortfall, "shortfall", _INTS, (1,))
     if workspace is None:
-        workspace = page_workspace(num_pages, num_seqs, refs.device)
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = page_workspace(num_pages, num_seqs, refs.device)
     pw, nw = _workspace(workspace, refs)
     _check((_lib or lib()).wq_cache_fork(caches.array, len(caches.array), pt, pr, pl, ps, pd, n, num_seqs, caches.kv_heads, caches.head_dim,
                                          caches.page, num_pages, max_pages, pf, pw, nw, _stream(stream, refs)))
@@ -611,7 +614,8 @@ def cache_compact(caches: CacheSet, block_table, refs, new_table, new_refs, live
     pnr = _dev_tensor(new_refs, "new_refs", _INTS, refs.shape)
     pl = _dev_tensor(live, "live", _INTS, (1,))
     if workspace is None:
-        workspace = page_workspace(num_pages, num_seqs, refs.device)
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = page_workspace(num_pages, num_seqs, refs.device)
     pw, nw = _workspace(workspace, refs)
     _check((_lib or lib()).wq_cache_compact(caches.array, len(caches.array), caches.page_bytes, pt, pr, pnt, pnr, pl, num_seqs, num_pages,
                                             max_pages, pw, nw, _stream(stream, refs)))
@@ -692,7 +696,8 @@ def process_logits(logits, out, token=None, mask=None, history=None, history_len
     if bias_lens is not None:
         pbl = _dev_tensor(bias_lens, "bias_lens", _INTS, one)
     if workspace is None and token is not None:
-        workspace = logits_workspace(logits)
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = logits_workspace(logits)
     pw, nw = _workspace(workspace, logits)
     call = WqLogitsCall(px, py, pt, pm or None, ph, phl, ppl, pr, pf, pp, pbi, pbv, pbl, rows, vocab, xs, ys, ms, hs, bs, kind)
     _check((_lib or lib()).wq_process_logits(ctypes.addressof(call), pw, nw, _stream(stream, logits)))

@@ -380,3 +380,22 @@ def test_a_sequence_beyond_the_query_bound_is_nan_in_every_row():
     wq.window_attention(c.q, c.k, c.v, ints(c.table), ints(c.lens), out, c.scale, 900, 2000, q_starts=ints(c.starts), max_query_len=100)
     assert bool(torch.isnan(out[:900]).all())
     c.check(torch.cat([clean[:900], out[900:]]))
+
+
+def test_without_a_workspace_on_another_stream():
+    """The memory of a workspace made in the call belongs to the stream that the call is queued on."""
+    import torch
+
+    require_gpu()
+    c = Case(47, "float16", [3000, 2500], [1, 1], 2, 4, 64, 16, 4000, 0)
+    want = c.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(20):
+        out = torch.empty_like(want)
+        side.wait_stream(torch.cuda.current_stream())
+        c.run(out=out, stream=side)
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
