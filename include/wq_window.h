@@ -28,7 +28,8 @@
  * Numerics: products of 16-bit values are exact, scores, softmax and sums are
  * fp32; the weights exp(a - m) are rounded once to the values' type for the
  * matrix cores that multiply them by V (relative error 2^-11, bfloat16 2^-8
- * each), and the output once.  Per element the result is within
+ * each; where a sequence's new tokens have at most 16 rows per kv head, n_s * G,
+ * a weight's rounding error is multiplied as well), and the output once.  Per element the result is within
  * e * sum_t w_t |V_t[d]| + 1e-6 of the exact value, e = 3e-3 for binary16 and
  * 2e-2 for bfloat16, when scale * sum_d |q[d] K_t[d]| <= 60 for every token.
  * Infinities and NaN in a cached token, or in the unused part of a page, reach

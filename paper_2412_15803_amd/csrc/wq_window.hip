@@ -44,6 +44,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
@@ -503,7 +504,7 @@ __device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D
             }
             load_keys(t1, pg);
             // Every row sees every token of the step, or some are masked.
-                                const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
+            const bool all = t0 + kFewTokens - 1 <= lo && (t0 + kFewTokens - 1 < p.sinks || t0 > last - p.window);
             if (!all) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -528,22 +529,42 @@ __device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D
                 for (int m = 0; m < kVw; ++m) o[m] *= f;
             }
             const float base = sm.base(p.c);
-            Vec8 pf;
+            // A weight is two values of the type, its rounding and what that leaves: memory
+            // bounds this kernel, so the second product costs little (48 sequences 98.0 ->
+            // 98.7 us), and the output's own rounding is then its largest error (fp16, 512
+            // tokens: 3.1e-4 -> 2.0e-4 of the output's norm).
+            Vec8 pf, rest;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
                 sm.l += w;
                 pf[j] = static_cast<T>(w);
+                rest[j] = static_cast<T>(w - static_cast<float>(pf[j]));
             }
             // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
+            u32x4 vf[kVw];
+            ushort2v top = {0, 0};
 #pragma unroll
-            for (int m = 0; m < kVw; ++m) {
-                u32x4 vf;
+            for (int m = 0; m < kVw; ++m)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    vf[j] = __builtin_amdgcn_perm(v[2 * j + 1][m / 2], v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
-                o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf), pf, o[m]);
+                    vf[m][j] = __builtin_amdgcn_perm(v[2 * j + 1][m / 2], v[2 * j][m / 2], m & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int m = 0; m < kVw; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2v, vf[m][j] & 0x7FFF7FFFu));
+#pragma unroll
+            for (int m = 0; m < kVw; ++m) o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf[m]), pf, o[m]);
+            // What is not finite takes part in the first product only: `rest` may be 0 or
+            // below.
+            if (__builtin_amdgcn_ballot_w64(max(top.x, top.y) >= Type<T>::kExponent)) {
+#pragma unroll
+                for (int m = 0; m < kVw; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) vf[m][j] = finite_part<T>(vf[m][j]);
             }
+#pragma unroll
+            for (int m = 0; m < kVw; ++m) o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf[m]), rest, o[m]);
             load_values(t1, pg);
             if (t1 < 0) break;
             pg = after;
