@@ -61,12 +61,15 @@ __device__ __forceinline__ int count_below(uint64_t mask) {
 }
 __device__ __forceinline__ int from_lane(int v, int lane) { return __builtin_amdgcn_ds_bpermute(lane * 4, v); }
 
-// Sum of a[0 .. n) over a wave; the lanes take turns.
-__device__ __forceinline__ int sum_of(const int32_t* a, int n) {
-    int v = 0;
-    for (int i = lane_id(); i < n; i += 64) v += a[i];
+// Sum of a[0 .. n) over a wave; the lanes take turns.  Their first values can be
+// asked for ahead.
+__device__ __forceinline__ int first_of(const int32_t* a, int n) { return lane_id() < n ? a[lane_id()] : 0; }
+__device__ __forceinline__ int sum_of(const int32_t* a, int n, int first) {
+    int v = first;
+    for (int i = lane_id() + 64; i < n; i += 64) v += a[i];
     return wave_sum(v);
 }
+__device__ __forceinline__ int sum_of(const int32_t* a, int n) { return sum_of(a, n, first_of(a, n)); }
 
 // ------------------------------------------------------------- free pages
 
@@ -401,18 +404,23 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(const Fork p, const Arra
     __shared__ int shared_page;
     const Pool pool{p.s.bits, p.s.counts, p.s.blocks};
     const int i = blockIdx.x, g = i / kGroupForks, lane = lane_id();
-    const int missing = sum_of(p.s.group, p.groups) - sum_of(pool.counts, pool.blocks);
-    if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.shortfall = max(missing, 0);
-    const int len = p.s.length[i];
-    if (missing > 0 || len < 0) return;
-    const int s = p.s.src[i], d = p.s.dst[i];
-    const int page_size = 1 << p.s.log2_page, full = len >> p.s.log2_page, part = len & (page_size - 1);
+    // What waits for no other load comes first: one round trip instead of five (36
+    // forks, 32 caches: 19.8 -> 19.3 us).
+    const int32_t* needs = p.s.need + g * kGroupForks;
+    const int len = p.s.length[i], s = p.s.src[i], d = p.s.dst[i];
     const bool need = p.s.need[i] != 0;
+    const int wanted = first_of(p.s.group, p.groups), there = first_of(pool.counts, pool.blocks);
+    const int before = first_of(p.s.group, g), ahead = first_of(needs, i - g * kGroupForks);
+    const int missing = sum_of(p.s.group, p.groups, wanted) - sum_of(pool.counts, pool.blocks, there);
+    if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.shortfall = max(missing, 0);
+    if (missing > 0 || len < 0) return;
+    const int page_size = 1 << p.s.log2_page, full = len >> p.s.log2_page, part = len & (page_size - 1);
     const int32_t* from = p.table + (int64_t)s * p.s.max_pages;
+    const int tail = need ? from[full] : -1;
     int page = -1;
     if (need) {
         if (threadIdx.x < 64) {
-            const int rank = sum_of(p.s.group, g) + sum_of(p.s.need + g * kGroupForks, i - g * kGroupForks);
+            const int rank = sum_of(p.s.group, g, before) + sum_of(needs, i - g * kGroupForks, ahead);
             const int found = select(pool, lane == 0 ? rank : -1);
             if (lane == 0) shared_page = found;
         }
@@ -437,7 +445,6 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(const Fork p, const Arra
         }
     }
     if (page < 0) return;
-    const int tail = from[full];
     if ((uint32_t)tail >= (uint32_t)p.s.num_pages) return;
     const int per_token = p.head_dim / 8;
     const int run = part * per_token;  // pieces of one kv head, contiguous
