@@ -157,8 +157,10 @@ struct Tiles {
     int first;       // no token below it is in the window of the first
     int start;       // first, down to a multiple of TOKENS
     int sink_tiles, count;
+    // A window of 0 holds no token: `first` is then the start of the tile after hi's, so
+    // that no aligned group of tokens up to hi's reaches it.
     __device__ __forceinline__ Tiles(const Params& p, int lo, int hi) {
-        first = max(0, lo - p.window + 1);
+        first = p.window > 0 ? max(0, lo - p.window + 1) : (hi + TOKENS) & ~(TOKENS - 1);
         start = first & ~(TOKENS - 1);
         sink_tiles = (min(p.sinks, start) + TOKENS - 1) / TOKENS;
         count = p.window > 0 || p.sinks > 0 ? sink_tiles + (hi - start + TOKENS) / TOKENS : 0;
