@@ -26,12 +26,19 @@
  * anything, so freed pages need no page behind them.
  *
  * Numerics: products of 16-bit values are exact, scores, softmax and sums are
- * fp32; the weights exp(a - m) are rounded once to the values' type for the
- * matrix cores that multiply them by V (relative error 2^-11, bfloat16 2^-8
- * each; where a sequence's new tokens have at most 16 rows per kv head, n_s * G,
- * a weight's rounding error is multiplied as well), and the output once.  Per element the result is within
- * e * sum_t w_t |V_t[d]| + 1e-6 of the exact value, e = 3e-3 for binary16 and
- * 2e-2 for bfloat16, when scale * sum_d |q[d] K_t[d]| <= 60 for every token.
+ * fp32; the weights exp(a - m) are rounded to the values' type for the matrix
+ * cores that multiply them by V, and the output once.  A sequence whose new tokens
+ * have at most 16 rows per kv head (n_s * G; unless it is the only one of a call
+ * with max_query_len * G above 16) has what a weight's rounding took multiplied as
+ * well; in the others a weight is rounded once, by a relative 2^-11 (bfloat16:
+ * 2^-8) or, in binary16, by up to 2^-32 of the row's largest weight.  Per element
+ * the result is within
+ *
+ *     e * sum_t w_t |V_t[d]| + f * sum_{t in V(p)} |V_t[d]| + 1e-6
+ *
+ * of the exact value, e = 3e-3 for binary16 and 2e-2 for bfloat16, f = 2^-32 for
+ * binary16, 2^-43 up to those 16 rows, and 0 for bfloat16, when
+ * scale * sum_d |q[d] K_t[d]| <= 60 for every token.
  * Infinities and NaN in a cached token, or in the unused part of a page, reach
  * only outputs whose query sees that token.
  *

@@ -64,6 +64,8 @@ struct Type<_Float16> {
     typedef _Float16 Vec8 __attribute__((ext_vector_type(8)));
     static constexpr uint16_t kNaN = 0x7E00;
     static constexpr uint32_t kExponent = 0x7C00;
+    static constexpr float kLift = 7.0f;     // see Softmax
+    static constexpr float kFine = 2048.0f;  // see few_body
     static __device__ __forceinline__ float4v mfma16(Vec8 a, Vec8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ float16v mfma32(Vec8 a, Vec8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
@@ -72,6 +74,7 @@ struct Type<__bf16> {
     typedef __bf16 Vec8 __attribute__((ext_vector_type(8)));
     static constexpr uint16_t kNaN = 0x7FC0;
     static constexpr uint32_t kExponent = 0x7F80;
+    static constexpr float kLift = 0.0f, kFine = 1.0f;  // it has the range of fp32
     static __device__ __forceinline__ float4v mfma16(Vec8 a, Vec8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ float16v mfma32(Vec8 a, Vec8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
@@ -222,11 +225,15 @@ __device__ __forceinline__ float pair_sum(float x) {
     return a + b;
 }
 
-// Softmax.  m is the reference that a row's weights 2^(c s - c m) are formed
+// Softmax.  m is the reference that a row's weights 2^(c s - c m + kLift) are formed
 // against, l this lane's share of their sum.  m follows the row's largest score
 // only when that passes it by more than kRescale in log2 units, so a wave
-// rarely has to rescale its accumulators; weights then reach at most 2^8, within
-// range of both 16-bit types, and their sums are fp32.
+// rarely has to rescale its accumulators; weights then reach at most 2^(8 + kLift),
+// and their sums are fp32.  The lift, which is the same in every part of a row and so
+// leaves the quotient, puts binary16's weights at the top of its range (2^15 <
+// 65504): below 2^-14 that type is off by up to 2^-25 however small the weight,
+// 2^-32 of the row's largest with the lift, 2^-25 without.
+template <typename T>
 struct Softmax {
     float m = -INFINITY, l = 0.0f;
     // Given the row's largest new score: whether any row of the wave needs a new
@@ -240,8 +247,8 @@ struct Softmax {
         l *= factor;
         return true;
     }
-    // c m, or 0 while nothing is visible (every weight is then 2^-inf = 0).
-    __device__ __forceinline__ float base(float c) const { return m == -INFINITY ? 0.0f : m * c; }
+    // kLift - c m, or 0 while nothing is visible (every weight is then 2^-inf = 0).
+    __device__ __forceinline__ float shift(float c) const { return m == -INFINITY ? 0.0f : fmaf(m, -c, Type<T>::kLift); }
 };
 
 // ------------------------------------------------------ few rows: the split
@@ -479,10 +486,13 @@ __device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D
         }
     };
 
-    Softmax sm;
-    float4v o[kVw];
+    Softmax<T> sm;
+    // Sums of values times weights, and (times kFine) of values times what rounding took
+    // from the weights.
+    constexpr bool kApart = Type<T>::kFine != 1.0f;
+    float4v o[kVw], fine[kApart ? kVw : 1];
 #pragma unroll
-    for (int m = 0; m < kVw; ++m) o[m] = float4v{0, 0, 0, 0};
+    for (int m = 0; m < kVw; ++m) o[m] = fine[kApart ? m : 0] = float4v{0, 0, 0, 0};
 
     // Waves take steps in turn.
     const int lo = q.len - q.n;
@@ -528,20 +538,27 @@ __device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D
             float f;
             if (sm.advance(mx, p.c, f)) {
 #pragma unroll
-                for (int m = 0; m < kVw; ++m) o[m] *= f;
+                for (int m = 0; m < kVw; ++m) {
+                    o[m] *= f;
+                    if constexpr (kApart) fine[m] *= f;
+                }
             }
-            const float base = sm.base(p.c);
+            const float shift = sm.shift(p.c);
             // A weight is two values of the type, its rounding and what that leaves: memory
             // bounds this kernel, so the second product costs little (48 sequences 98.0 ->
             // 98.7 us), and the output's own rounding is then its largest error (fp16, 512
-            // tokens: 3.1e-4 -> 2.0e-4 of the output's norm).
+            // tokens: 3.1e-4 -> 2.0e-4 of the output's norm).  What rounding leaves of a weight
+            // of 2^15 is at most 2^4 in binary16, and is multiplied by 2^11, so that it too
+            // reaches down as far as the type allows (2^-36 in place of 2^-25); sums of their own
+            // take 20 to 32 registers (head_dim 64: 16 sequences of up to 20000 tokens 59.8 -> 61.4
+            // us, 200 of up to 2004 42.9 -> 43.3; head_dim 128 within 1%).
             Vec8 pf, rest;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, -base));
+                const float w = exp2_(fmaf(st[j / 4][j % 4], p.c, shift));
                 sm.l += w;
                 pf[j] = static_cast<T>(w);
-                rest[j] = static_cast<T>(w - static_cast<float>(pf[j]));
+                rest[j] = static_cast<T>((w - static_cast<float>(pf[j])) * Type<T>::kFine);
             }
             // V^T: the 8 tokens x kVw dims that a lane holds, turned 2 x 2 at a time.
             u32x4 vf[kVw];
@@ -566,7 +583,10 @@ __device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D
                     for (int j = 0; j < 4; ++j) vf[m][j] = finite_part<T>(vf[m][j]);
             }
 #pragma unroll
-            for (int m = 0; m < kVw; ++m) o[m] = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf[m]), rest, o[m]);
+            for (int m = 0; m < kVw; ++m) {
+                float4v& sum = kApart ? fine[m] : o[m];
+                sum = Type<T>::mfma16(__builtin_bit_cast(Vec8, vf[m]), rest, sum);
+            }
             load_values(t1, pg);
             if (t1 < 0) break;
             pg = after;
@@ -577,6 +597,10 @@ __device__ __forceinline__ void few_body(const Params& p, int block, FewShared<D
 
     // The waves' states are joined through LDS.  A wave that met a page outside
     // the cache leaves a NaN sum.
+    if constexpr (kApart) {
+#pragma unroll
+        for (int m = 0; m < kVw; ++m) o[m] += fine[m] * (1.0f / Type<T>::kFine);
+    }
     float l = pair_sum<true>(pair_sum<false>(sm.l));
     if (__builtin_amdgcn_ballot_w64(bad != 0)) l = NAN;
     if (g == 0) {
@@ -919,7 +943,7 @@ __device__ __forceinline__ void tile_body(const Params& p, int block, TileShared
     for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
-    Softmax sm;
+    Softmax<T> sm;
     if (tid < kEdges) sh.partly[tid] = 0;
     if (tid == 0) sh.bad = 0;
     int edges = 0;
@@ -1033,13 +1057,18 @@ __device__ __forceinline__ void tile_body(const Params& p, int block, TileShared
 #pragma unroll
             for (int dt = 0; dt < kDt; ++dt) o[dt] *= f;
         }
-        const float base = sm.base(p.c);
+        const float shift = sm.shift(p.c);
+        // Weights are rounded once to the values' type (their sum is of the unrounded ones):
+        // against fp32 weights a prompt's error grows from 1.9e-4 to 2.5e-4 of the output's norm
+        // in binary16, from 1.6e-3 to 2.0e-3 in bfloat16.  Multiplying what rounding takes, as
+        // few_body does, would make the products of this kernel, which they bound, half as many
+        // again.
         Vec8 pf[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float w = exp2_(fmaf(st[x / 2][(x & 1) * 8 + j], p.c, -base));
+                const float w = exp2_(fmaf(st[x / 2][(x & 1) * 8 + j], p.c, shift));
                 sm.l += w;
                 pf[x][j] = static_cast<T>(w);
             }
