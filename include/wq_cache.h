@@ -96,7 +96,7 @@ wq_status wq_page_workspace_size(int64_t num_pages, int64_t num_seqs, size_t* by
  * no page gets the lowest free page left, with a reference count of 1.  Lengths
  * below 0 count as 0, those beyond the table's row as the row's end.
  *   shortfall  int32 on the device, written: 0, or how many pages too few are
- *              free; then nothing else has been changed.
+ *              free (at most INT32_MAX); then nothing else has been changed.
  *   workspace  of at least the bytes that wq_page_workspace_size reports,
  *              16-byte aligned, owned by the caller, used only while the
  *              work queued by this call runs (calls on one stream may share it).

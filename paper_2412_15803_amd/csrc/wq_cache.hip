@@ -70,6 +70,12 @@ __device__ __forceinline__ int sum_of(const int32_t* a, int n, int first) {
     return wave_sum(v);
 }
 __device__ __forceinline__ int sum_of(const int32_t* a, int n) { return sum_of(a, n, first_of(a, n)); }
+// The same of up to 2^16 values of 0 .. 2^28, whose sum may pass 32 bits.
+__device__ __forceinline__ int64_t long_sum_of(const int32_t* a, int n) {
+    int64_t v = first_of(a, n);
+    for (int i = lane_id() + 64; i < n; i += 64) v += a[i];
+    return ((int64_t)wave_sum((int)(v >> 24)) << 24) + wave_sum((int)(v & 0xFFFFFF));
+}
 
 // ------------------------------------------------------------- free pages
 
@@ -265,8 +271,9 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(const Reserve p) {
     const Pool pool{p.s.bits, p.s.counts, p.s.blocks};
     const int need = p.s.need[s];
     if (need == 0 && s != 0) return;
-    const int missing = sum_of(p.s.group, p.groups) - sum_of(pool.counts, pool.blocks);
-    if (s == 0 && threadIdx.x == 0) *p.shortfall = max(missing, 0);
+    // (Tables may want more pages than 32 bits count: 2^16 rows of 2^24 entries.)
+    const int64_t missing = long_sum_of(p.s.group, p.groups) - sum_of(pool.counts, pool.blocks);
+    if (s == 0 && threadIdx.x == 0) *p.shortfall = (int32_t)min<int64_t>(max<int64_t>(missing, 0), INT32_MAX);
     if (missing > 0 || need == 0) return;
     int rank = sum_of(p.s.group, g) + sum_of(p.s.need + g * kGroupSeqs, s - g * kGroupSeqs);
     int lo, hi;
