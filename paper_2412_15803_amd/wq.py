@@ -318,7 +318,8 @@ def paged_attention(q, k_cache, v_cache, block_table, seq_lens, out, scale: floa
     pl = _dev_tensor(seq_lens, "seq_lens", _INTS, (num_seqs,))
     po = _dev_tensor(out, "out", _HALVES, (num_seqs, hq, d))
     if workspace is None:
-        workspace = paged_workspace(q, max_seq_len, hkv)
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = paged_workspace(q, max_seq_len, hkv)
     if workspace is not None:
         if workspace.device != q.device or workspace.dtype not in _BYTES or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 tensor on the device of q")
