@@ -88,6 +88,7 @@ class Cache:
         ints = dict(dtype=torch.int32, device=model.device)
         self.table, self.refs = torch.full((slots, width), -1, **ints), torch.zeros(pages, **ints)
         self.lens, self.shortfall, self.live = torch.zeros(slots, **ints), torch.zeros(1, **ints), torch.zeros(1, **ints)
+        self.lacked = torch.zeros(1, **ints)  # the largest shortfall so far
         self.workspace = wq.page_workspace(pages, slots, model.device)
 
     def layer(self, i):
@@ -95,6 +96,7 @@ class Cache:
 
     def reserve(self, new_lens):
         wq.cache_reserve(self.table, self.refs, self.lens, new_lens, self.page, self.shortfall, workspace=self.workspace)
+        torch.maximum(self.lacked, self.shortfall, out=self.lacked)
 
     def slide(self, seqs):
         """Give back what the window of the listed sequences has left behind."""
@@ -106,6 +108,13 @@ class Cache:
 
     def fork(self, src, dst):
         wq.cache_fork(self.set, self.table, self.refs, self.lens, src, dst, self.shortfall, workspace=self.workspace)
+        torch.maximum(self.lacked, self.shortfall, out=self.lacked)
+
+    def check(self):
+        """Raise if the pool was ever too small (waits for the device)."""
+        lacked = int(self.lacked)
+        if lacked:
+            raise RuntimeError(f"the pool of {self.refs.numel()} pages was {lacked} too small")
 
     def compact(self):
         wq.cache_compact(self.set, self.table, self.refs, self.table, self.refs, self.live, workspace=self.workspace)
@@ -115,7 +124,8 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
              pages=None, room=0):
     """Token histories [len(prompts) * samples] of `steps` generated words each,
     the last step's logits, and the cache.  allowed: a mask as process_logits
-    takes it, one row; room: words that the cache can take after the last."""
+    takes it, one row; room: words that the cache can take after the last.
+    Raises when the pool of `pages` is too small."""
     device = model.device
     ints = dict(dtype=torch.int32, device=device)
     n, slots = len(prompts), len(prompts) * samples
@@ -145,6 +155,7 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
         source = torch.cat([torch.arange(n, device=device), src.long()])
     else:
         source = torch.arange(n, device=device)
+    cache.check()
     history, prompt_lens = history[source].contiguous(), history_lens[source].contiguous()
     history_lens = prompt_lens.clone()
     logits = logits[starts[1:n + 1].long() - 1][source].contiguous()
@@ -161,6 +172,7 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
         logits = model.forward(token, cache, history_lens, None, 1)
         cache.lens.copy_(history_lens)
         cache.slide(every)
+    cache.check()
     return history, history_lens, logits, cache
 
 
