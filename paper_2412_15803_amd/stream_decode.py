@@ -125,7 +125,7 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
     """Token histories [len(prompts) * samples] of `steps` generated words each,
     the last step's logits, and the cache.  allowed: a mask as process_logits
     takes it, one row; room: words that the cache can take after the last.
-    Raises when the pool of `pages` is too small."""
+    Raises when the pool of `pages` is too small or a step has no word to choose."""
     device = model.device
     ints = dict(dtype=torch.int32, device=device)
     n, slots = len(prompts), len(prompts) * samples
@@ -164,8 +164,10 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
         best = logits.float().topk(samples, dim=-1).indices
         logits[rows, best[rows, nth]] += 100.0
     every = torch.arange(slots, **ints)
+    lowest = torch.zeros_like(token)  # -1 where a step found no word
     for _ in range(steps):
         wq.process_logits(logits, logits, token=token, mask=mask, history=history, history_lens=history_lens, prompt_lens=prompt_lens, **penalties)
+        torch.minimum(lowest, token, out=lowest)
         history[rows, history_lens.long()] = token
         history_lens += 1
         cache.reserve(history_lens)
@@ -173,6 +175,8 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
         cache.lens.copy_(history_lens)
         cache.slide(every)
     cache.check()
+    if int(lowest.min()) < 0:
+        raise RuntimeError(f"no word was left to choose in sequences {(lowest < 0).nonzero().flatten().tolist()}")
     return history, history_lens, logits, cache
 
 

@@ -1,4 +1,5 @@
-"""The decoding example says when its pool is too small."""
+"""The decoding example says when its pool is too small and when no word is
+allowed."""
 
 from __future__ import annotations
 
@@ -35,3 +36,15 @@ def test_a_pool_that_just_fits():
     model = sd.Decoder()
     sd.generate(model, prompts_of(model), 2, 4, 1000, 0, pages=13)  # 5, 90 and 33 words: four more fit their pages
     sd.generate(model, prompts_of(model), 1, 4, 1000, 0, pages=10)
+
+
+def test_no_word_allowed():
+    import torch
+
+    from paper_2412_15803_amd import stream_decode as sd
+
+    require_gpu()
+    model = sd.Decoder()
+    allowed = torch.zeros((1, -(-model.vocab // 32)), dtype=torch.int32, device="cuda")
+    with pytest.raises(RuntimeError, match="word"):
+        sd.generate(model, prompts_of(model), 2, 4, 1000, 0, allowed=allowed)
