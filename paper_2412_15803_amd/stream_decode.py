@@ -126,6 +126,8 @@ def generate(model, prompts, samples, steps, window, sinks, page=16, allowed=Non
     the last step's logits, and the cache.  allowed: a mask as process_logits
     takes it, one row; room: words that the cache can take after the last.
     Raises when the pool of `pages` is too small or a step has no word to choose."""
+    if not prompts or not all(len(p) for p in prompts):
+        raise ValueError("there must be prompts, and a word in each")
     device = model.device
     ints = dict(dtype=torch.int32, device=device)
     n, slots = len(prompts), len(prompts) * samples
