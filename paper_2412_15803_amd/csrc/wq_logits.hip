@@ -438,11 +438,16 @@ template <typename T, bool HISTORY, bool BIAS>
 void launch_as(const Params& p, bool vector, hipStream_t stream) {
     const dim3 grid((unsigned)p.tiles, (unsigned)p.c.rows);
     const size_t lds = HISTORY || BIAS ? (size_t)(p.tile + Type<T>::kPer) * 4 : 0;
-    // 32 KB of logits are four 16-byte loads for each of 512 lanes (256 rows of
-    // 100277 fp32 words: 48.5 us with 256 lanes, 44.7 with 512).
-    const bool wide = (size_t)p.tile * sizeof(T) >= 32768;
-    if (vector && wide) hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, true, 512>), grid, dim3(512), lds, stream, p);
-    else if (vector) hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, true, 256>), grid, dim3(256), lds, stream, p);
+    // 32 KB of logits, which only the longest tiles of fp32 have, are four 16-byte loads
+    // for each of 512 lanes (256 rows of 100277 words: 48.5 us with 256 lanes, 44.7 with
+    // 512).
+    if constexpr (kMaxTile * sizeof(T) >= 32768) {
+        if (vector && p.tile == kMaxTile) {
+            hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, true, 512>), grid, dim3(512), lds, stream, p);
+            return;
+        }
+    }
+    if (vector) hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, true, 256>), grid, dim3(256), lds, stream, p);
     else hipLaunchKernelGGL((logits_kernel<T, HISTORY, BIAS, false, 256>), grid, dim3(256), lds, stream, p);
 }
 
