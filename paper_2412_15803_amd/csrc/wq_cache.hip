@@ -411,8 +411,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(const Fork p, const Arra
     __shared__ int shared_page;
     const Pool pool{p.s.bits, p.s.counts, p.s.blocks};
     const int i = blockIdx.x, g = i / kGroupForks, lane = lane_id();
-    // What waits for no other load comes first: one round trip instead of five (36
-    // forks, 32 caches: 19.8 -> 19.3 us).
+    // What waits for no other load comes first (36 forks, 32 caches: 19.8 -> 19.3 us).
     const int32_t* needs = p.s.need + g * kGroupForks;
     const int len = p.s.length[i], s = p.s.src[i], d = p.s.dst[i];
     const bool need = p.s.need[i] != 0;

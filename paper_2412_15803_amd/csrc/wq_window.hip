@@ -262,7 +262,12 @@ struct Softmax {
 // A launch lasts about r (T + kUnitCost) steps when the units fill r rounds of
 // workgroups (two to a CU).  What counts is that the longest sequences come out
 // even, so T is a whole fraction of the longest: for one round and for two, the
-// smaller such T that fits, and then the better of both.
+// smaller such T that fits, and then the better of both.  Up to 64 sequences, one to
+// a lane; the plain T beyond.  Against the plain T alone, 24/8 heads of 128: 16 sequences
+// of 4096 tokens 53.2 -> 49.4 us, 7 of 9000 52.3 -> 49.2, 20 of 5000 71.6 -> 70.5, but 33 of
+// 4096 99.0 -> 100.5 and 48 of 4096 133 -> 146; ragged ones are the same (16 of 4000 to
+// 20000: 119, 64 of up to 30000: 370).  kUnitCost from 0 to 8 changes 48 sequences of up to
+// 30000 tokens (96 to 98 us) by less than runs differ.
 constexpr int kUnitCost = 4;
 
 struct Unit {
@@ -1180,6 +1185,10 @@ Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_
     pl.few_slots = std::min<int64_t>(kFewRows, max_query * group);
     pl.units = seqs;
     pl.round = std::max<int64_t>(1, kRound / hkv);
+    // Two rounds of workgroups that take a sequence whole are not cut either.  24/8 heads
+    // of 128: 128 sequences of 3000 to 4000 tokens take 298 us whole and 319 cut, of 4000
+    // each 324 and 322.  Uneven ones lose by it: 256 of 200 to 8000 tokens 444 and 392, and
+    // 128 with one of 30000 among 200 to 1000 325 and 82 (127 of them, which are cut: 82).
     if (steps > (seqs * hkv >= kRound / 2 ? kWholeMany : kWholeFew) && seqs * hkv < 2 * kRound) {
         const int64_t want = std::max(2 * pl.round, 2 * seqs);
         pl.units = std::max(std::min(want, seqs * ceil_div(steps, kWaves)), seqs + 1);
@@ -1188,6 +1197,9 @@ Plan plan_of(int64_t seqs, int64_t tokens, int64_t max_query, int64_t hq, int64_
     pl.row_tiles = std::min(ceil_div(tokens * group, kTileRows) + seqs, seqs * ceil_div(std::min(max_query, tokens) * group, kTileRows));
     const int64_t groups = ceil_div(tokens * group, kTileRows) * hkv;
     const int64_t seen = ceil_div(std::min(max_len, sinks + window + kTileRows / group + 1), kTileTokens) + 1;
+    // Launches that fill three quarters of a round are not split: 1540 new tokens of 16384,
+    // 32/8 heads of 128 (392 workgroups), take 462 us in one part and 537 in two.  Below,
+    // 1500 (376) take 460 and 475, 1100 (280) 410 and 444: the line could lie lower.
     pl.splits = groups >= 384 ? 1 : std::max<int64_t>(1, std::min<int64_t>({ceil_div(512, groups), seen / 16, 32}));
     size_t at = 0;
     auto take = [&](int64_t bytes) {
