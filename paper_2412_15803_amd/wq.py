@@ -1,6 +1,7 @@
 """Thin ctypes binding of the C ABI in include/wq.h, include/wq_attention.h,
 include/wq_fused.h, include/wq_cache.h, include/wq_window.h,
-include/wq_logits.h and include/wq_probe.h.
+include/wq_logits.h, include/wq_mx.h, include/wq_norm.h, include/wq_sample.h
+and include/wq_probe.h.
 
 Only argument marshalling happens here: torch tensors are turned into device
 pointers and sizes, the current HIP stream is passed through, and non-OK
@@ -33,7 +34,9 @@ EXPORTED = ("wq_status_string", "wq_last_error_message", "wq_version", "wq_pack"
             "wq_paged_attention", "wq_fused_linears", "wq_fused_check", "wq_stream_read",
             "wq_cache_append", "wq_cache_copy_pages", "wq_page_workspace_size", "wq_cache_reserve", "wq_cache_free",
             "wq_cache_fork", "wq_cache_compact", "wq_process_logits_workspace_size", "wq_process_logits",
-            "wq_window_attention_workspace_size", "wq_window_attention")
+            "wq_window_attention_workspace_size", "wq_window_attention", "wq_mx_quantize", "wq_mx_dequantize",
+            "wq_mx_linear_workspace_size", "wq_mx_linear", "wq_add_rmsnorm", "wq_sample_logits_workspace_size",
+            "wq_sample_logits")
 
 # Limits of wq_decode_linears_noalloc (include/wq.h).
 NOALLOC_MAX_LINEARS = 1024
@@ -42,6 +45,11 @@ NOALLOC_SCRATCH_BYTES = 131072
 PROLOGUE_NONE = 0
 PROLOGUE_RMSNORM = 1
 PROLOGUE_SILU_MUL = 2
+
+# Element types of microscaled matrices (include/wq_mx.h).
+MX_FP4 = 4
+MX_FP8 = 8
+MX_BLOCK = 32
 
 
 class WqLinear(ctypes.Structure):
@@ -75,6 +83,17 @@ class WqLogitsCall(ctypes.Structure):
         "logits", "out", "token", "mask", "history", "history_lens", "prompt_lens", "repetition", "frequency", "presence",
         "bias_ids", "bias_values", "bias_lens")] + [(name, ctypes.c_int64) for name in (
             "rows", "vocab", "logits_stride", "out_stride", "mask_stride", "history_size", "bias_size", "dtype")]
+
+
+class WqNormCall(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("x", "residual", "weight", "total", "out", "codes", "scales")] + [
+        (name, ctypes.c_int64) for name in ("rows", "dim", "x_stride", "residual_stride", "total_stride", "out_stride", "dtype", "format")] + [
+            ("eps", ctypes.c_float)]
+
+
+class WqSampleCall(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("logits", "random", "temperature", "top_k", "top_p", "min_p", "token", "share")] + [
+        (name, ctypes.c_int64) for name in ("rows", "vocab", "logits_stride", "dtype")]
 
 
 class WQError(RuntimeError):
@@ -133,7 +152,14 @@ def lib() -> ctypes.CDLL:
             ("wq_process_logits_workspace_size", [i64, i64, i64, ctypes.POINTER(sz)]),
             ("wq_process_logits", [vp, vp, sz, vp]),
             ("wq_window_attention_workspace_size", [i64] * 9 + [ctypes.POINTER(sz)]),
-            ("wq_window_attention", [vp] * 7 + [i64] * 14 + [ctypes.c_float, i64, vp, sz, vp])):
+            ("wq_window_attention", [vp] * 7 + [i64] * 14 + [ctypes.c_float, i64, vp, sz, vp]),
+            ("wq_mx_quantize", [vp] * 3 + [i64] * 6 + [vp]),
+            ("wq_mx_dequantize", [vp] * 3 + [i64] * 5 + [vp]),
+            ("wq_mx_linear_workspace_size", [i64] * 4 + [ctypes.POINTER(sz)]),
+            ("wq_mx_linear", [vp] * 5 + [i64] * 6 + [vp, sz, vp]),
+            ("wq_add_rmsnorm", [vp, vp]),
+            ("wq_sample_logits_workspace_size", [i64] * 3 + [ctypes.POINTER(sz)]),
+            ("wq_sample_logits", [vp, vp, sz, vp])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -161,13 +187,13 @@ def _check(status: int) -> None:
 # turn them into C values).
 
 _torch = _Tensor = None
-_WORDS = _HALVES = _FLOATS = _INTS = _BYTES = ()
+_WORDS = _HALVES = _FLOATS = _INTS = _BYTES = _SCALES = ()
 _DTYPES = {}  # WQ_DTYPE_* of include/wq_logits.h
 _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _Tensor, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _DTYPES, _raw_stream
+    global _torch, _Tensor, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _SCALES, _DTYPES, _raw_stream
     import torch
 
     _WORDS = (torch.int32, torch.uint32)
@@ -175,6 +201,7 @@ def _load_torch():
     _FLOATS = (torch.float32,)
     _INTS = (torch.int32,)
     _BYTES = (torch.uint8,)
+    _SCALES = (torch.uint8, torch.float8_e8m0fnu)
     _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
     # The current stream's handle without building a Stream object.
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -702,6 +729,186 @@ def process_logits(logits, out, token=None, mask=None, history=None, history_len
     pw, nw = _workspace(workspace, logits)
     call = WqLogitsCall(px, py, pt, pm or None, ph, phl, ppl, pr, pf, pp, pbi, pbv, pbl, rows, vocab, xs, ys, ms, hs, bs, kind)
     _check((_lib or lib()).wq_process_logits(ctypes.addressof(call), pw, nw, _stream(stream, logits)))
+
+
+# ------------------------------------------------------- microscaled matrices
+#
+# A matrix [R, C] is a pair of tensors: codes uint8 [R, C / 2] (4-bit elements) or
+# float8_e4m3fn [R, C] (8-bit), and scales [R, mx_scale_stride(C)] of uint8 or
+# float8_e8m0fnu, of which the first C / 32 of a row are used.
+
+def mx_scale_stride(cols: int) -> int:
+    """Bytes of a row of scales."""
+    return -(-cols // 512) * 16
+
+
+def mx_empty(rows: int, cols: int, bits: int, device="cuda"):
+    """Room for a microscaled matrix: (codes, scales), their contents undefined."""
+    import torch
+
+    if bits not in (4, 8):
+        raise ValueError(f"bits must be 4 or 8 (got {bits})")
+    if cols % MX_BLOCK:
+        raise ValueError(f"cols must be a multiple of {MX_BLOCK} (got {cols})")
+    codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=device) if bits == 4 else \
+        torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device)
+    return codes, torch.empty((rows, mx_scale_stride(cols)), dtype=torch.float8_e8m0fnu, device=device)
+
+
+def _mx_matrix(codes, scales, names):
+    """Addresses of a microscaled matrix's codes and scales, its rows, columns and
+    element type."""
+    for t, name in zip((codes, scales), names):
+        if not isinstance(t, _Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if t.dim() != 2:
+            raise ValueError(f"{name} must be 2-D (got {t.dim()} dimensions)")
+    rows, width = codes.shape
+    if codes.dtype is _torch.uint8:
+        kinds, bits, cols = _BYTES, MX_FP4, 2 * width
+    else:
+        kinds, bits, cols = (_torch.float8_e4m3fn,), MX_FP8, width
+    pc = _dev_tensor(codes, names[0], kinds, (rows, width))
+    ps = _dev_tensor(scales, names[1], _SCALES, (rows, mx_scale_stride(cols)))
+    return pc, ps, rows, cols, bits
+
+
+def _dtype_of(t, name):
+    kind = _DTYPES.get(t.dtype) if isinstance(t, _Tensor) else None
+    if kind is None:
+        raise TypeError(f"{name} must be a tensor of one of {tuple(_DTYPES)} (got {getattr(t, 'dtype', type(t))})")
+    return kind
+
+
+def mx_quantize(x, codes, scales, gated: bool = False, stream=None) -> None:
+    """Round x [R, C] (fp16, bf16 or fp32; rows may lie apart) to a microscaled
+    matrix, or, when gated, silu(gate) * up of x = [gate | up] [R, 2 C]."""
+    _torch or _load_torch()
+    kind = _dtype_of(x, "x")
+    pc, ps, rows, cols, bits = _mx_matrix(codes, scales, ("codes", "scales"))
+    px, xs = _row_stride(x, "x", (rows, 2 * cols if gated else cols))
+    _check((_lib or lib()).wq_mx_quantize(px, pc, ps, rows, cols, xs, kind, 1 if gated else 0, bits, _stream(stream, x)))
+
+
+def mx_dequantize(codes, scales, out, stream=None) -> None:
+    """What a microscaled matrix stands for, into out [R, C] (fp16, bf16 or fp32;
+    rows may lie apart)."""
+    _torch or _load_torch()
+    kind = _dtype_of(out, "out")
+    pc, ps, rows, cols, bits = _mx_matrix(codes, scales, ("codes", "scales"))
+    po, os_ = _row_stride(out, "out", (rows, cols))
+    _check((_lib or lib()).wq_mx_dequantize(pc, ps, po, rows, cols, os_, bits, kind, _stream(stream, codes)))
+
+
+def mx_linear_workspace(w_codes, x_codes):
+    """A device workspace (uint8 tensor, or None) for mx_linear of these codes."""
+    _torch or _load_torch()
+    bits = MX_FP4 if x_codes.dtype is _torch.uint8 else MX_FP8
+    n = ctypes.c_size_t(0)
+    _check(lib().wq_mx_linear_workspace_size(w_codes.shape[0], 2 * w_codes.shape[1], x_codes.shape[0], bits, ctypes.byref(n)))
+    return _torch.empty(n.value, dtype=_torch.uint8, device=x_codes.device) if n.value else None
+
+
+def mx_linear(w_codes, w_scales, x_codes, x_scales, y, workspace=None, stream=None) -> None:
+    """y [M, N] (fp16 or bf16; rows may lie apart) = x [M, K] . w [N, K]^T of two
+    microscaled matrices, w in 4 bits, x in 4 or 8.  `workspace` is from
+    mx_linear_workspace (allocated here when omitted)."""
+    _torch or _load_torch()
+    kind = _dtype_of(y, "y")
+    pw, pws, n, k, w_bits = _mx_matrix(w_codes, w_scales, ("w_codes", "w_scales"))
+    px, pxs, m, x_cols, x_bits = _mx_matrix(x_codes, x_scales, ("x_codes", "x_scales"))
+    if w_bits != MX_FP4:
+        raise TypeError(f"w_codes must be uint8 pairs of 4-bit elements (got {w_codes.dtype})")
+    if x_cols != k:
+        raise ValueError(f"x has {x_cols} columns, w {k}")
+    py, ys = _row_stride(y, "y", (m, n))
+    if workspace is None:
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = mx_linear_workspace(w_codes, x_codes)
+    pk, nk = _workspace(workspace, y)
+    _check((_lib or lib()).wq_mx_linear(pw, pws, px, pxs, py, n, k, m, ys, x_bits, kind, pk, nk, _stream(stream, y)))
+
+
+# ------------------------------------------------------- residual and norm
+
+def add_rmsnorm(x, weight, eps: float, out=None, residual=None, total=None, codes=None, scales=None, stream=None) -> None:
+    """The root-mean-square norm of x + residual (or of x) [R, D] times weight [D],
+    into out [R, D] and / or a microscaled matrix (codes, scales); the sum itself
+    into total [R, D].  x, weight, residual, total and out share one type (fp16,
+    bf16 or fp32), their rows may lie apart; total and out may be x or residual."""
+    _torch or _load_torch()
+    kind = _dtype_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [R, D]")
+    shape = rows, dim = x.shape
+
+    def matrix(t, name):
+        if t is None:
+            return None, 0
+        if isinstance(t, _Tensor) and t.dtype is not x.dtype:
+            raise TypeError(f"{name} has dtype {t.dtype}, x {x.dtype}")
+        return _row_stride(t, name, shape)
+
+    px, xs = matrix(x, "x")
+    pr, rs = matrix(residual, "residual")
+    pt, ts = matrix(total, "total")
+    po, os_ = matrix(out, "out")
+    pw = _dev_tensor(weight, "weight", (x.dtype,), (dim,))
+    pc = ps = None
+    bits = 0
+    if codes is not None or scales is not None:
+        if codes is None or scales is None:
+            raise ValueError("codes and scales go together")
+        pc, ps, r, d, bits = _mx_matrix(codes, scales, ("codes", "scales"))
+        if (r, d) != tuple(shape):
+            raise ValueError(f"codes hold {r} rows of {d}, expected {rows} of {dim}")
+    call = WqNormCall(px, pr, pw, pt, po, pc, ps, rows, dim, xs, rs, ts, os_, kind, bits, eps)
+    _check((_lib or lib()).wq_add_rmsnorm(ctypes.addressof(call), _stream(stream, x)))
+
+
+# ------------------------------------------------------- the next word by chance
+
+def sample_workspace(logits):
+    """A device workspace (uint8 tensor, or None) for sample_logits."""
+    _torch or _load_torch()
+    n = ctypes.c_size_t(0)
+    _check(lib().wq_sample_logits_workspace_size(logits.shape[0], logits.shape[1], _DTYPES[logits.dtype], ctypes.byref(n)))
+    return _torch.empty(n.value, dtype=_torch.uint8, device=logits.device) if n.value else None
+
+
+def sample_logits(logits, random, token, temperature=None, top_k=None, top_p=None, min_p=None, share=None, workspace=None, stream=None) -> None:
+    """A word of each row of logits [R, V] (fp16, bf16 or fp32; rows may lie apart)
+    into token (int32 [R]), chosen by random (fp32 [R], in [0, 1)) from what
+    temperature, top_k (int32), top_p and min_p [R] leave; its share of the
+    probability left into share (fp32 [R]).  A temperature of 0 takes the best
+    word.  What is None is left out (include/wq_sample.h has the formulas).
+    `workspace` is from sample_workspace (allocated here when omitted)."""
+    _torch or _load_torch()
+    kind = _dtype_of(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [R, V]")
+    rows, vocab = logits.shape
+    one = (rows,)
+    px, xs = _row_stride(logits, "logits", logits.shape)
+    pr = _dev_tensor(random, "random", _FLOATS, one)
+    po = _dev_tensor(token, "token", _INTS, one)
+    pt = pk = pp = pm = psh = None
+    if temperature is not None:
+        pt = _dev_tensor(temperature, "temperature", _FLOATS, one)
+    if top_k is not None:
+        pk = _dev_tensor(top_k, "top_k", _INTS, one)
+    if top_p is not None:
+        pp = _dev_tensor(top_p, "top_p", _FLOATS, one)
+    if min_p is not None:
+        pm = _dev_tensor(min_p, "min_p", _FLOATS, one)
+    if share is not None:
+        psh = _dev_tensor(share, "share", _FLOATS, one)
+    if workspace is None:
+        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+            workspace = sample_workspace(logits)
+    pw, nw = _workspace(workspace, logits)
+    call = WqSampleCall(px, pr, pt, pk, pp, pm, po, psh, rows, vocab, xs, kind)
+    _check((_lib or lib()).wq_sample_logits(ctypes.addressof(call), pw, nw, _stream(stream, logits)))
 
 
 # ------------------------------------------------------- measurement probe
