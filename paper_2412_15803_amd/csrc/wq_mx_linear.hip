@@ -193,6 +193,12 @@ template <typename V>
 __device__ __forceinline__ void lds_write(uint32_t addr, V v) {
     *reinterpret_cast<__attribute__((address_space(3))) V*>((lds_u8*)(size_t)addr) = v;
 }
+// An address whose origin the compiler does not see, so that constants added to it
+// become offsets of the instructions instead of registers of their own.
+__device__ __forceinline__ uint32_t opaque(uint32_t addr) {
+    asm("" : "+v"(addr));
+    return addr;
+}
 
 // 16 bytes per lane from base + offset straight into LDS, lane after lane.  Written
 // out because the compiler would wait for every load in flight before any LDS
@@ -200,108 +206,171 @@ __device__ __forceinline__ void lds_write(uint32_t addr, V v) {
 __device__ __forceinline__ void dma16(const uint8_t* base, uint32_t offset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "memory");
 }
-// All but the newest N loads of this wave are done, its LDS writes too, and so for all waves.
-template <int N>
-__device__ __forceinline__ void arrive() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+// The same from an address of each lane's own.
+__device__ __forceinline__ void dma16(const uint8_t* src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds) : "memory");
 }
+__device__ const uint8_t kZeros[16] = {};
+// All but the newest N loads and stores of this wave are done.
+template <int N>
+__device__ __forceinline__ void wait_vector() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// A barrier that ends a turn: LDS reads and writes before it are done.
+__device__ __forceinline__ void turn_over() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+    if constexpr (N > 0) {
+        unrolled<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
+// Rows of BYTES (64 or 128) in LDS.  A load fetches them with consecutive lanes on
+// consecutive pieces of 16 bytes of a row, for which the cache looks up a line once;
+// lanes on different rows cost it a look-up each, which bounded the kernel.  A row's
+// pieces lie in an order of its own, so that the same piece of 16 rows comes from all
+// 64 banks, in the groups of lanes in which LDS serves 16-byte reads (0-3, 12-15,
+// 20-27; 4-11, 16-19, 28-31; the same 32 further on).
+template <int BYTES>
+struct Places {
+    static constexpr uint32_t kPieces = BYTES / 16, kRows = 1024 / BYTES;  // rows of a load
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (BYTES == 64 ? 0u - row / 4 : row / 2) % kPieces; }
+    static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece) { return row * BYTES + (piece ^ turn(row)) * 16; }
+};
 
 // How BM rows of x and BN of W are multiplied by WM x WN waves.
 template <int XF, int BM_, int BN_, int WM_, int WN_>
 struct Shape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kWaves = WM * WN;
-    static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;          // tiles of 16 of a wave
-    static constexpr int kXRegs = Piece<XF>::kRegs;
-    static constexpr int kWBytes = BN * 64, kXBytes = BM * 64 * kXRegs;  // of a step
+    static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // tiles of 16 of a wave
+    static constexpr int kXRegs = Piece<XF>::kRegs, kXRow = 64 * kXRegs;
+    static constexpr int kWBytes = BN * 64, kXBytes = BM * kXRow;  // of a step
     static constexpr int kStage = kWBytes + kXBytes, kStages = 3;
-    static constexpr int kLoads = kStage / 1024, kEach = kLoads / kWaves;  // per stage and per wave
-    static constexpr int kScaleBytes = (BM + BN) * 16;                   // of kSteps steps
+    static constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves, kLoads = kWLoads + kXLoads;  // of a wave
+    static constexpr int kScaleBytes = (BM + BN) * 16;  // of kSteps steps
     static constexpr int kScaleAt = kStages * kStage;
     static constexpr int kLds = kScaleAt + 2 * kScaleBytes;
-    static_assert(kLoads % kWaves == 0 && (BM + BN) / 64 <= kWaves && kLds <= 160 * 1024, "");
+    static constexpr bool kTurns = kWaves == 8;  // two waves to a SIMD
+    static constexpr int kPerCu = 160 * 1024 / kLds;
+    static constexpr int kOutTiles = FN < 4 ? FN : 4;  // tiles of 16 outputs side by side that are stored together
+    static_assert(kWLoads * kWaves * 1024 == kWBytes && kXLoads * kWaves * 1024 == kXBytes && (BM + BN) / 64 <= kWaves && kPerCu >= 1, "");
+    static_assert(FN % kOutTiles == 0 && kOutTiles * 512 <= kWLoads * 1024, "outputs pass through the wave's own part of a stage");
 };
 
-// Workgroups are dealt to the 8 XCDs in turn; give each a run of tiles, so
-// that its L2 holds what they share.
-__device__ __forceinline__ uint32_t xcd_run(uint32_t b, uint32_t blocks) {
-    const uint32_t xcd = b % 8, per = blocks / 8, more = blocks % 8;
-    return xcd * per + std::min(xcd, more) + b / 8;
-}
+// The tiles of a launch in the order in which they are taken, a run of them for each
+// XCD (workgroups are dealt to the 8 XCDs in turn), so that its L2 holds what they
+// share: bands of 8 tiles along x.
+struct Order {
+    uint32_t at, end, by;
+    __device__ __forceinline__ explicit Order(uint32_t tiles) {
+        const uint32_t xcd = blockIdx.x % 8, per = tiles / 8, more = tiles % 8;
+        const uint32_t first = xcd * per + std::min(xcd, more);
+        at = first + blockIdx.x / 8;
+        end = first + per + (xcd < more ? 1 : 0);
+        by = gridDim.x / 8;
+    }
+};
 
+// A workgroup takes tile after tile.  Loads run two steps ahead of the products, into the
+// next tile's first steps too, while a tile's outputs are stored.
+//
+// Two waves of a SIMD take turns (kTurns): while those of one group multiply, the
+// others fetch their operands from LDS.  A barrier ends each turn, the second group is
+// one turn behind:
+//   turn      2s          2s + 1
+//   first     fetch s     multiply s
+//   second    multiply    fetch s
+//             s - 1
+// Stage s + 2 is loaded in the place of stage s - 1, which was last read in turn 2s - 1;
+// stage s + 1 has arrived when turn 2s + 1 ends.
 template <typename T, int XF, typename S>
 __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p) {
     __shared__ __align__(16) uint8_t memory[S::kLds];
     const uint32_t lds = (uint32_t)(size_t)(lds_u8*)memory;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int r = lane % 16, q = lane / 16;
-    const int wm = wave % S::WM, wn = wave / S::WM;
-    // Bands of 8 tiles along x, so that a run's tiles share rows of both matrices.
-    uint32_t tm, tn;
-    {
-        const uint32_t b = xcd_run(blockIdx.x, gridDim.x), band = 8 * p.tiles_n, first = b / band * 8;
-        const uint32_t high = std::min(p.tiles_m - first, 8u), in = b % band;
-        tm = first + in % high;
-        tn = in / high;
-    }
-    const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
-    const uint32_t rows_m = (uint32_t)std::min<int64_t>(p.m - m0, S::BM), rows_n = (uint32_t)std::min<int64_t>(p.n - n0, S::BN);
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t r = lane % 16, q = lane / 16;
+    const uint32_t wm = wave % S::WM, wn = wave / S::WM;
     const uint32_t x_row = XF == WQ_MX_FP8 ? p.k : p.k / 2, w_row = p.k / 2;
-    const uint8_t* const w_base = p.w_codes + n0 * w_row;
-    const uint8_t* const x_base = p.x_codes + m0 * x_row;
     const uint32_t steps = (p.blocks + 3) / 4, supers = (p.blocks + 15) / 16, last = p.blocks % 4;
+    Order order(p.tiles_n * p.tiles_m);
+    if (order.at >= order.end) return;
 
-    // Load i of a stage fills its bytes [1024 i, + 1024): tile i of W, or tile and half (i - BN / 16)
-    // of x.  Rows past the end stand in for the last one.
-    uint32_t offset[S::kEach];
-    bool of_w[S::kEach];
-    uint32_t half[S::kEach];
+    // What is being loaded: tile `order.at`, step `load_step` of it, into stage `load_slot`.
+    const uint8_t *w_base, *x_base, *scale_base;
+    uint32_t most_n, most_m, scale_most, load_step = 0, load_slot = 0;
+    constexpr uint32_t kScaleLoads = (S::BM + S::BN) / 64;
+    auto tile_rows = [&](uint32_t tile, int64_t& m0, int64_t& n0) {
+        const uint32_t band = 8 * p.tiles_n, first = tile / band * 8, high = std::min(p.tiles_m - first, 8u), in = tile % band;
+        m0 = (int64_t)(first + in % high) * S::BM;
+        n0 = (int64_t)(in / high) * S::BN;
+    };
+    auto aim = [&] {
+        int64_t m0, n0;
+        tile_rows(order.at, m0, n0);
+        most_m = (uint32_t)std::min<int64_t>(p.m - m0, S::BM) - 1;
+        most_n = (uint32_t)std::min<int64_t>(p.n - n0, S::BN) - 1;
+        w_base = p.w_codes + n0 * w_row;
+        x_base = p.x_codes + m0 * x_row;
+        // Scales: 64 rows to a wave, those of W first.
+        const bool of_w = wave * 64 < S::BN;
+        scale_base = of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride;
+        scale_most = of_w ? most_n : most_m;
+    };
+    const uint32_t w_first = wave * S::kWLoads * Places<64>::kRows + lane / 4, w_piece = lane % 4 ^ Places<64>::turn(lane / 4);
+    const uint32_t x_first = wave * S::kXLoads * Places<S::kXRow>::kRows + lane / Places<S::kXRow>::kPieces;
+    const uint32_t x_piece = lane % Places<S::kXRow>::kPieces ^ Places<S::kXRow>::turn(x_first);
+    // Rows past the end stand in for the last one.
+    auto w_offset = [&](int i) { return __umul24(std::min(w_first + i * Places<64>::kRows, most_n), w_row) + w_piece * 16; };
+    auto x_turned = [&](int i) { return x_piece ^ (S::kXRow == 128 && i % 2 ? 4u : 0u); };  // (Every second load's rows are 8 further on.)
+    auto x_offset = [&](int i) { return __umul24(std::min(x_first + i * Places<S::kXRow>::kRows, most_m), x_row) + x_turned(i) * 16; };
+    // Loads the next step; of the last tile's last one, nothing.
+    auto load_stage = [&]() -> bool {
+        if (order.at >= order.end) return false;
+        const uint32_t w_to = lds + load_slot * S::kStage + wave * (S::kWLoads * 1024), x_to = lds + load_slot * S::kStage + S::kWBytes + wave * (S::kXLoads * 1024);
+        if (last == 0 || load_step + 1 < steps) {
 #pragma unroll
-    for (int i = 0; i < S::kEach; ++i) {
-        const int load = wave * S::kEach + i, xl = load - S::BN / 16;
-        of_w[i] = load < S::BN / 16;
-        half[i] = of_w[i] ? 0 : xl % S::kXRegs;
-        const uint32_t row = of_w[i] ? std::min<uint32_t>(load * 16 + r, rows_n - 1) : std::min<uint32_t>(xl / S::kXRegs * 16 + r, rows_m - 1);
-        offset[i] = row * (of_w[i] ? w_row : x_row) + half[i] * 64 + q * 16;
-    }
-    auto load_stage = [&](uint32_t step) {
-        const uint32_t to = lds + step % S::kStages * S::kStage + wave * (S::kEach * 1024);
-        if (last == 0 || step + 1 < steps) {
+            for (int i = 0; i < S::kWLoads; ++i) dma16(w_base, w_offset(i), w_to + i * 1024);
 #pragma unroll
-            for (int i = 0; i < S::kEach; ++i)
-                dma16((of_w[i] ? w_base : x_base) + (int64_t)step * (of_w[i] || XF == WQ_MX_FP4 ? 64 : 128), offset[i], to + i * 1024);
+            for (int i = 0; i < S::kXLoads; ++i) dma16(x_base, x_offset(i), x_to + i * 1024);
         } else {
             // The last blocks of a row: what lies past them counts as zeros, and is not read.
 #pragma unroll
-            for (int i = 0; i < S::kEach; ++i) {
-                const bool fp4 = of_w[i] || XF == WQ_MX_FP4;
-                u32x4 v = {0, 0, 0, 0};
-                if ((fp4 ? (uint32_t)q : half[i] * 2 + q / 2) < last)
-                    v = *gbl(reinterpret_cast<const u32x4*>((of_w[i] ? w_base : x_base) + (int64_t)step * (fp4 ? 64 : 128) + offset[i]));
-                lds_write(to + i * 1024 + lane * 16, v);
-            }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            for (int i = 0; i < S::kWLoads; ++i) dma16(w_piece < last ? w_base + w_offset(i) : kZeros, w_to + i * 1024);
+#pragma unroll
+            for (int i = 0; i < S::kXLoads; ++i) dma16(x_turned(i) / S::kXRegs < last ? x_base + x_offset(i) : kZeros, x_to + i * 1024);
+        }
+        w_base += 64;
+        x_base += S::kXRow;
+        load_slot = load_slot + 1 == S::kStages ? 0 : load_slot + 1;
+        if (++load_step == steps) {
+            load_step = 0;
+            order.at += order.by;
+            if (order.at < order.end) aim();
+        }
+        return true;
+    };
+    // The scales of four steps, 16 bytes of every row.
+    auto load_scales = [&](const uint8_t* base, uint32_t most, uint32_t buffer) {
+        if (wave < kScaleLoads) {
+            const uint32_t first = wave * 64 < S::BN ? wave * 64 : wave * 64 - S::BN;
+            dma16(base, std::min(first + lane, most) * (uint32_t)p.scale_stride, lds + S::kScaleAt + buffer * S::kScaleBytes + wave * 1024);
         }
     };
-    // The scales of four steps: 16 bytes of every row of W, then of x.
-    constexpr int kScaleLoads = (S::BM + S::BN) / 64;
-    const int scale_row = wave * 64 + lane;
-    const bool scale_of_w = scale_row < S::BN;
-    const uint8_t* const scale_base = wave * 64 < S::BN ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride;
-    const uint32_t scale_offset = (scale_of_w ? std::min<uint32_t>(scale_row, rows_n - 1) : std::min<uint32_t>(scale_row - S::BN, rows_m - 1)) * (uint32_t)p.scale_stride;
-    auto load_scales = [&](uint32_t super) {
-        if (wave < kScaleLoads) dma16(scale_base + super * 16, scale_offset, lds + S::kScaleAt + super % 2 * S::kScaleBytes + wave * 1024);
-    };
     // Turned, so that a lane's four bytes of a row, one for each step, lie in one word.
-    auto turn_scales = [&](uint32_t super) {
+    auto turn_scales = [&](uint32_t left, uint32_t buffer) {
         if (wave < kScaleLoads) {
-            const uint32_t at = lds + S::kScaleAt + super % 2 * S::kScaleBytes + wave * 1024 + lane * 16;
+            const uint32_t at = lds + S::kScaleAt + buffer * S::kScaleBytes + wave * 1024 + lane * 16;
             u32x4 v = lds_read<u32x4>(at);
-            const uint32_t left = p.blocks - super * 16;
             if (left < 16) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (uint32_t i = 0; i < 4; ++i) {
                     // Bytes past the last block stand for the scale 1.
-                    const uint32_t keep = left >= 4u * i + 4 ? ~0u : left <= 4u * i ? 0u : (1u << (left - 4 * i) * 8) - 1;
+                    const uint32_t keep = left >= 4 * i + 4 ? ~0u : left <= 4 * i ? 0u : (1u << (left - 4 * i) * 8) - 1;
                     v[i] = (v[i] & keep) | (0x7F7F7F7Fu & ~keep);
                 }
             }
@@ -313,65 +382,127 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         }
     };
 
-    float4v acc[S::FN][S::FM] = {};
-    load_scales(0);
-    load_stage(0);
-    if (steps > 1) load_stage(1);
-    // (With one step fewer loads are in flight than counted here; the wait is the stricter one then.)
-    if (steps > 1) arrive<2 * S::kEach>();
-    else arrive<0>();
-    turn_scales(0);
-    for (uint32_t super = 0; super < supers; ++super) {
+    uint32_t tile = order.at, slot = 0, buffer = 0;
+    aim();
+    // The scales' own cursor: their tile may be one behind the stages'.
+    const uint8_t* tile_scales = scale_base;
+    uint32_t tile_most = scale_most;
+    load_scales(tile_scales, tile_most, 0);
+    load_stage();
+    load_stage();
+    wait_vector<0>();
+    turn_scales(p.blocks, 0);
+    turn_over();
+    if (S::kTurns && wave >= S::kWaves / 2) turn_over();
+
+    const uint32_t w_at = wn * S::FN * 1024 + Places<64>::place(r, q);
+    uint32_t x_at[S::kXRegs];
+#pragma unroll
+    for (int h = 0; h < S::kXRegs; ++h) x_at[h] = S::kWBytes + wm * S::FM * 16 * S::kXRow + Places<S::kXRow>::place(r, h * 4 + q);
+    const uint32_t sw_at = S::kScaleAt + wn * S::FN * 256 + r * 16 + q * 4, sx_at = S::kScaleAt + S::BN * 16 + wm * S::FM * 256 + r * 16 + q * 4;
+
+    for (;;) {
+        const uint32_t next = tile + order.by;
+        float4v acc[S::FN][S::FM] = {};
         uint32_t sw[S::FN], sx[S::FM];
+        for (uint32_t super = 0; super < supers; ++super) {
+            unrolled<kSteps>([&](auto T_) {
+                constexpr int t = decltype(T_)::value;
+                const uint32_t step = super * kSteps + t;
+                if (step >= steps) return;
+                if constexpr (t == 0) {
+                    const uint32_t from = opaque(lds + buffer * S::kScaleBytes);
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            const uint32_t step = super * kSteps + t;
-            if (step >= steps) break;
-            if (step + 1 < steps) arrive<S::kEach>();
-            else arrive<0>();
-            if (t == 0 && super + 1 < supers) load_scales(super + 1);
-            if (step + 2 < steps) load_stage(step + 2);
-            if (t == 0) {
-                const uint32_t at = lds + S::kScaleAt + super % 2 * S::kScaleBytes + r * 16 + q * 4;
+                    for (int i = 0; i < S::FN; ++i) sw[i] = lds_read<uint32_t>(from + sw_at + i * 256);
 #pragma unroll
-                for (int i = 0; i < S::FN; ++i) sw[i] = lds_read<uint32_t>(at + (wn * S::FN + i) * 256);
+                    for (int j = 0; j < S::FM; ++j) sx[j] = lds_read<uint32_t>(from + sx_at + j * 256);
+                    buffer ^= 1;
+                    // Where the next super-step's scales are: in this tile, or the next.
+                    if (super + 1 < supers) {
+                        load_scales(tile_scales + (super + 1) * 16, tile_most, buffer);
+                    } else if (next < order.end) {
+                        int64_t m0, n0;
+                        tile_rows(next, m0, n0);
+                        const bool of_w = wave * 64 < S::BN;
+                        tile_scales = of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride;
+                        tile_most = (uint32_t)std::min<int64_t>(of_w ? p.n - n0 : p.m - m0, of_w ? S::BN : S::BM) - 1;
+                        load_scales(tile_scales, tile_most, buffer);
+                    }
+                }
+                const bool loaded = load_stage();
+                const uint32_t from = lds + slot * S::kStage, w_from = opaque(from + w_at);
+                slot = slot + 1 == S::kStages ? 0 : slot + 1;
+                Piece<XF> xv[S::FM];
+                u32x4 wv[S::FN];
 #pragma unroll
-                for (int j = 0; j < S::FM; ++j) sx[j] = lds_read<uint32_t>(at + S::BN * 16 + (wm * S::FM + j) * 256);
-            }
-            if (t == kSteps - 1 && super + 1 < supers) turn_scales(super + 1);
-            const uint32_t from = lds + step % S::kStages * S::kStage + lane * 16;
-            Piece<XF> xv[S::FM];
-            u32x4 wv[S::FN];
+                for (int h = 0; h < S::kXRegs; ++h) {
+                    const uint32_t x_from = opaque(from + x_at[h]);
 #pragma unroll
-            for (int j = 0; j < S::FM; ++j)
+                    for (int j = 0; j < S::FM; ++j) xv[j].v[h] = lds_read<u32x4>(x_from + j * 16 * S::kXRow);
+                }
 #pragma unroll
-                for (int h = 0; h < S::kXRegs; ++h) xv[j].v[h] = lds_read<u32x4>(from + S::kWBytes + ((wm * S::FM + j) * S::kXRegs + h) * 1024);
-#pragma unroll
-            for (int i = 0; i < S::FN; ++i) wv[i] = lds_read<u32x4>(from + (wn * S::FN + i) * 1024);
-            auto products = [&](auto T_) {
+                for (int i = 0; i < S::FN; ++i) wv[i] = lds_read<u32x4>(w_from + i * 1024);
+                // All but the newest stage have arrived, the scales among them.  (A tile's second stage did
+                // before the outputs of the last tile were stored.)
+                const bool turn = t == kSteps - 1 || step + 1 == steps;
+                if (step > 0 || turn) {
+                    if (loaded) wait_vector<S::kLoads>();
+                    else wait_vector<0>();
+                }
+                if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? p.blocks - (super + 1) * 16 : p.blocks, buffer);
+                turn_over();
+                if constexpr (S::kTurns) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int i = 0; i < S::FN; ++i)
 #pragma unroll
-                    for (int j = 0; j < S::FM; ++j) acc[i][j] = mma<XF, decltype(T_)::value, decltype(T_)::value>(wv[i], xv[j], acc[i][j], sw[i], sx[j]);
-            };
-            if (t == 0) products(std::integral_constant<int, 0>());
-            else if (t == 1) products(std::integral_constant<int, 1>());
-            else if (t == 2) products(std::integral_constant<int, 2>());
-            else products(std::integral_constant<int, 3>());
+                    for (int j = 0; j < S::FM; ++j) acc[i][j] = mma<XF, t, t>(wv[i], xv[j], acc[i][j], sw[i], sx[j]);
+                if constexpr (S::kTurns) {
+                    __builtin_amdgcn_s_setprio(0);
+                    turn_over();
+                }
+            });
         }
-    }
-    const bool vector = p.y_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 8 == 0;
+        // The last step's stage is free: the wave's own part of it takes 16 rows of outputs at a time, to be
+        // stored in whole rows.  (Nothing is loaded there before this wave itself does.)
+        wait_vector<0>();
+        if constexpr (!S::kTurns) turn_over();
+        int64_t m0, n0;
+        tile_rows(tile, m0, n0);
+        const bool vector = p.y_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
+        const uint32_t out = lds + (slot == 0 ? S::kStages - 1 : slot - 1) * S::kStage + wave * (S::kWLoads * 1024);
+        constexpr uint32_t kRow = S::kOutTiles * 32, kPieces = kRow / 16, kRows = 64 / kPieces;  // bytes and pieces of a row, rows of a store
+        typedef T vec4 __attribute__((ext_vector_type(4)));
+        typedef T vec8 __attribute__((ext_vector_type(8)));
 #pragma unroll
-    for (int j = 0; j < S::FM; ++j) {
-        const int64_t row = m0 + (wm * S::FM + j) * 16 + r;
-        if (row < p.m) {
+        for (int j = 0; j < S::FM; ++j) {
 #pragma unroll
-            for (int i = 0; i < S::FN; ++i) {
-                const int64_t col = n0 + (wn * S::FN + i) * 16 + q * 4;
-                if (col < p.n) store_outputs<T>(p, row, col, acc[i][j], vector && col + 4 <= p.n);
+            for (int g = 0; g < S::FN; g += S::kOutTiles) {
+#pragma unroll
+                for (int i = 0; i < S::kOutTiles; ++i)
+                    lds_write(out + r * kRow + ((i * 2 + q / 2) ^ (r % kPieces)) * 16 + q % 2 * 8, __builtin_convertvector(acc[g + i][j], vec4));
+#pragma unroll
+                for (uint32_t h = 0; h < 16 / kRows; ++h) {
+                    const uint32_t at = h * kRows + lane / kPieces, piece = lane % kPieces;
+                    const vec8 v = __builtin_bit_cast(vec8, lds_read<u32x4>(out + at * kRow + (piece ^ (at % kPieces)) * 16));
+                    const int64_t row = m0 + (wm * S::FM + j) * 16 + at, col = n0 + (wn * S::FN + g) * 16 + piece * 8;
+                    if (row < p.m) {
+                        T* const y = static_cast<T*>(p.y) + row * p.y_stride + col;
+                        if (vector && col + 8 <= p.n) {
+                            *gbl(reinterpret_cast<u32x4*>(y)) = __builtin_bit_cast(u32x4, v);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (col + e < p.n) gbl(y)[e] = v[e];
+                        }
+                    }
+                }
             }
         }
+        if constexpr (S::kTurns) turn_over();
+        if (next >= order.end) break;
+        tile = next;
     }
+    if (S::kTurns && wave < S::kWaves / 2) turn_over();  // the second group's last
 }
 
 // ------------------------------------------------------------------ host
@@ -399,7 +530,9 @@ template <typename T, int XF, typename S>
 void launch_tiles_as(Params p, hipStream_t st) {
     p.tiles_n = (uint32_t)((p.n + S::BN - 1) / S::BN);
     p.tiles_m = (uint32_t)((p.m + S::BM - 1) / S::BM);
-    hipLaunchKernelGGL((tile_kernel<T, XF, S>), dim3(p.tiles_n * p.tiles_m), dim3(S::kWaves * 64), 0, st, p);
+    // As many workgroups as fit the CUs, a multiple of the XCDs.
+    const uint32_t all = p.tiles_n * p.tiles_m, most = 256u * std::min(S::kPerCu, 4), grid = std::min((all + 7) / 8 * 8, most);
+    hipLaunchKernelGGL((tile_kernel<T, XF, S>), dim3(grid), dim3(S::kWaves * 64), 0, st, p);
 }
 
 int64_t tiles(int64_t n, int64_t m, int64_t bn, int64_t bm) { return (n + bn - 1) / bn * ((m + bm - 1) / bm); }

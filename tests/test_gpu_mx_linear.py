@@ -56,9 +56,11 @@ def test_sizes(dtype, bits, n, k, m):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("n,k,m", [(3600, 512, 3200), (3300, 672, 3400), (1536, 1024, 2100), (2100, 288, 1500)])
+@pytest.mark.parametrize("n,k,m", [(3600, 512, 3200), (3300, 672, 3400), (1536, 1024, 2100), (2100, 288, 1500), (4400, 96, 5000), (5000, 160, 4400), (4500, 288, 4600),
+                                   (4700, 512, 4300), (4600, 544, 4353), (4354, 1184, 4700), (3000, 32, 3001), (3010, 256, 3000), (3000, 544, 2900), (2990, 640, 3030)])
 def test_large_tiles(bits, n, k, m):
-    """Sizes at which the larger tiles run, ragged ones among them; float64 on the GPU."""
+    """Sizes at which the larger tiles run and workgroups take several of them, ragged ones among them, from one
+    step of K on; float64 on the GPU."""
     rng = np.random.default_rng(n)
     w, ws = mg.random_matrix(rng, n, k, 4, 124, 130)
     x, xs = mg.random_matrix(rng, m, k, bits, 124, 130)
