@@ -442,13 +442,10 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                 }
 #pragma unroll
                 for (int i = 0; i < S::FN; ++i) wv[i] = lds_read<u32x4>(w_from + i * 1024);
-                // All but the newest stage have arrived, the scales among them.  (A tile's second stage did
-                // before the outputs of the last tile were stored.)
+                // All but the newest stage have arrived, the scales among them.
+                if (loaded) wait_vector<S::kLoads>();
+                else wait_vector<0>();
                 const bool turn = t == kSteps - 1 || step + 1 == steps;
-                if (step > 0 || turn) {
-                    if (loaded) wait_vector<S::kLoads>();
-                    else wait_vector<0>();
-                }
                 if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? p.blocks - (super + 1) * 16 : p.blocks, buffer);
                 turn_over();
                 if constexpr (S::kTurns) __builtin_amdgcn_s_setprio(1);
@@ -464,8 +461,6 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         }
         // The last step's stage is free: the wave's own part of it takes 16 rows of outputs at a time, to be
         // stored in whole rows.  (Nothing is loaded there before this wave itself does.)
-        wait_vector<0>();
-        if constexpr (!S::kTurns) turn_over();
         int64_t m0, n0;
         tile_rows(tile, m0, n0);
         const bool vector = p.y_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
