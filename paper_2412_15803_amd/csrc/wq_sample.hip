@@ -2,14 +2,28 @@
 // top-p, min-p and a given random number.
 //
 // The words that stay are a beginning of the order (logit falling, word rising), so
-// they are told by the last of them, the cut.  It is found by digits of an
-// order-preserving integer of the logit: a histogram of one digit (of counts for
-// top-k, of weights for top-p) in LDS tells which value the cut's digit has, and the
-// next pass looks only at words that share the digits found so far; equal logits
-// are told apart by their words in the same way, where the cut falls among them.
+// they are told by the last of them, the cut.  Two launches, a workgroup to a chunk of
+// a row in both:
+//   survey   a workgroup to a chunk of a row, which it reads into registers: the largest
+//            logit, and what the row's settings ask for: the sum of the weights, or a
+//            histogram over the distance from a reference near the row's largest logit
+//            (of counts for top-k, of weights for top-p; bins as fine as 1/64 of the
+//            distance).
+//   plan     a workgroup to a row: adds up the histograms, which tell the bin that the cut
+//            lies in.  Without top-k, top-p and min-p it chooses the word.
+//   choose   a workgroup to a chunk, read again from the caches: lists the words that may
+//            be the cut; those that surely stay are listed too while they are few, or
+//            else their weights summed.  The last workgroup of the row to be done sorts
+//            the list, finds the cut, the chunk that the random number falls into, and
+//            in it the word.
+// Rows whose list would be too long (thousands of equal logits) are worked out by that
+// workgroup alone, which then looks through the row instead of the list.
+//
+// A lane takes 8 words of a chunk at once and without branches: what bounds few rows is how
+// long one workgroup takes (loads, then the chain of fp64 operations of a weight).
 //
 // Weights are formed in fp64 and held as whole multiples of 2^-s: their sums do
-// not depend on the order in which they are added, so LDS atomics may add them.
+// not depend on the order in which they are added, so atomics may add them.
 // A 32-bit weight would move the border between two words by up to 2^-24 of the
 // total, which random numbers of 24 bits hit.
 #include <hip/hip_runtime.h>
@@ -31,46 +45,102 @@ using dev::gbl;
 using dev::u32x4;
 using namespace host;
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kBins = 2048;
+constexpr int kChunk = 8192;    // words of a chunk
+constexpr int kAbove = 512, kBelow = 1024, kBins = kAbove + kBelow;  // of a histogram, above and below its reference
+constexpr int kList = 4096;     // words that are listed
+constexpr int kRanked = 256;    // words of a list that are put in order by comparing all with all
+constexpr int kPartBits = 9, kParts = 1 << kPartBits;  // of a list's range
+constexpr int kAhead = 16;      // histograms that are read at once
+
+template <typename T>
+constexpr int kPer = 16 / sizeof(T);  // words of a 16-byte load
+template <typename T>
+constexpr int kVectors = kChunk / kPer<T>;  // of a chunk
+
+// What survey leaves of a chunk: its best word, the sum of its weights, and the bins
+// [low, high) that are not empty.
+struct Record {
+    uint64_t sum;
+    uint32_t key;
+    int32_t word;
+    int32_t low, high;
+    float reference;  // of the row's bins
+    int32_t unused;
+};
+// What choose does with a row.
+enum Way { kDone, kMinP, kCount, kWeight };
+// What plan tells choose, and what choose's workgroups share.
+struct Plan {
+    uint64_t ahead, need;       // words, or weights, before the cut's bin, and of it up to the cut
+    uint32_t best;              // key of the largest logit
+    int32_t word;               // and its word
+    float reference;
+    int32_t way, cut_bin, few, alone;
+    uint32_t done, listed;      // workgroups that are done, and words listed
+    int32_t unused[3];
+};
 
 struct Params {
     wq_sample_call c;
     int32_t weight_bits;  // s
+    int32_t has;          // which lists are given: 1 temperature, 2 top_p, 4 min_p, 8 top_k
+    int32_t chunks;       // of a row
+    int32_t list_size;    // words that a row's list holds
+    Record* records;      // [rows][chunks]
+    uint64_t* bins;       // [rows][chunks][kBins]
+    uint64_t* sums;       // [rows][chunks] weights that surely stay
+    uint64_t* list;       // [rows][list_size]
+    Plan* plans;          // [rows]
 };
-
-template <typename T>
-constexpr int kPer = 16 / sizeof(T);  // words of a 16-byte load
 
 // One row's logits: vector v holds the words v * kPer - lead .. + kPer - 1, so that whole vectors
 // are aligned whatever word the row starts at.
 template <typename T>
 struct Row {
+    typedef T vec __attribute__((ext_vector_type(kPer<T>)));
     const T* x;
     int vocab, lead, vectors;
+    int inside, outside;  // vectors [inside, outside) lie in the row whole
     __device__ __forceinline__ Row(const Params& p, int64_t row) {
         x = static_cast<const T*>(p.c.logits) + row * p.c.logits_stride;
         vocab = (int)p.c.vocab;
         lead = (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) % kPer<T>);
         vectors = (vocab + lead + kPer<T> - 1) / kPer<T>;
+        inside = lead ? 1 : 0;
+        outside = (vocab + lead) / kPer<T>;
+    }
+    __device__ __forceinline__ int chunk_of(int word) const { return (word + lead) / kChunk; }
+    // The bits of vector v, or of one that lies in the row whole, if there is one, where v does not.  (No branch on v,
+    // so that loads of several vectors do not wait for each other.)
+    __device__ __forceinline__ u32x4 fetch(int v) const {
+        if (outside <= inside) return u32x4{0, 0, 0, 0};
+        return *gbl(reinterpret_cast<const u32x4*>(x + (min(max(v, inside), outside - 1) * kPer<T> - lead)));
     }
     // The words of vector v as fp32; NaN and what lies outside the row as -infinity.
-    __device__ __forceinline__ void load(int v, float (&out)[kPer<T>]) const {
-        const int first = v * kPer<T> - lead;
-        if (first >= 0 && first + kPer<T> <= vocab) {
-            typedef T vec __attribute__((ext_vector_type(kPer<T>)));
-            const vec r = __builtin_bit_cast(vec, *gbl(reinterpret_cast<const u32x4*>(x + first)));
+    __device__ __forceinline__ void words(int v, u32x4 bits, float (&out)[kPer<T>]) const {
+        const vec w = __builtin_bit_cast(vec, bits);
 #pragma unroll
-            for (int i = 0; i < kPer<T>; ++i) out[i] = (float)r[i];
-        } else {
+        for (int i = 0; i < kPer<T>; ++i) out[i] = (float)w[i];
+        if (v < inside || v >= outside) {
+            const int first = v * kPer<T> - lead;
 #pragma unroll
             for (int i = 0; i < kPer<T>; ++i) out[i] = first + i >= 0 && first + i < vocab ? (float)gbl(x)[first + i] : -INFINITY;
         }
 #pragma unroll
         for (int i = 0; i < kPer<T>; ++i) out[i] = out[i] != out[i] ? -INFINITY : out[i] + 0.0f;  // -0 is 0
     }
+    // f(logit, word) for the words of the vectors [from, end); words that take no part have -infinity.
+    template <typename F>
+    __device__ __forceinline__ void each(int from, int end, F f) const {
+#pragma unroll 1
+        for (int v = from + threadIdx.x; v < end; v += blockDim.x) {
+            float y[kPer<T>];
+            words(v, fetch(v), y);
+#pragma unroll
+            for (int i = 0; i < kPer<T>; ++i) f(y[i], v * kPer<T> - lead + i);
+        }
+    }
 };
-
 // Larger for larger logits.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
@@ -108,10 +178,10 @@ struct Weights {
     double top, factor, low;  // largest logit; log2(e) / temperature; smallest log2 w that stays under min-p
     double steps;             // 2^s
     bool infinite;
-    // log2 w; at most 0, not below -2000.
+    // log2 w; at most 0, not below -2000, which weighs nothing, as -infinity does.
     __device__ __forceinline__ double log2_of(float x) const {
-        if (infinite) return x == INFINITY ? 0.0 : -2000.0;
-        return fmax(((double)x - top) * factor, -2000.0);
+        const double t = x == -INFINITY ? -2000.0 : fmax(((double)x - top) * factor, -2000.0);
+        return infinite ? (x == INFINITY ? 0.0 : -2000.0) : t;
     }
     // A whole number of steps, rounded to nearest.  (Below 2^52, adding 2^52 leaves the number in the low bits.)
     __device__ __forceinline__ uint64_t of(double log2w) const {
@@ -127,255 +197,632 @@ struct Cut {
     __device__ __forceinline__ bool keeps(uint32_t k, int w) const { return k > key || (k == key && w <= word); }
 };
 
-struct Shared {
-    uint64_t bins[kBins];
-    uint64_t tiles[WQ_SAMPLE_MAX_VOCAB / (kThreads * 4) + 2];
-    uint64_t parts[kWaves];
-    uint64_t before, found;
-    uint32_t keys[kWaves];
-    uint32_t digit;
-    int words[kWaves];
+// A row's settings, those that change nothing left out.
+struct Settings {
+    double temperature, random;
+    int top_k;      // 0: all
+    float top_p;    // 1: all
+    float min_p;    // 0: all
+    bool greedy;
+    __device__ __forceinline__ Settings(const Params& p, int64_t r) {
+        // (Lists that are not given point at the random numbers, so that no load waits behind a branch.)
+        const wq_sample_call& c = p.c;
+        const float u = gbl(c.random)[r], given_t = gbl(c.temperature)[r], given_p = gbl(c.top_p)[r], given_m = gbl(c.min_p)[r];
+        const int given_k = gbl(c.top_k)[r];
+        const float t = p.has & 1 ? given_t : 1.0f, tp = p.has & 2 ? given_p : 1.0f, mp = p.has & 4 ? given_m : 0.0f;
+        const int k = p.has & 8 ? given_k : 0;
+        temperature = t;
+        greedy = !(t > 0.0f);
+        top_k = k > 0 && k < c.vocab ? k : 0;
+        top_p = tp < 1.0f ? fmaxf(tp, 0.0f) : 1.0f;
+        min_p = mp > 0.0f ? fminf(mp, 1.0f) : 0.0f;
+        random = u > 0.0f ? fmin((double)u, 0.99999999999999989) : 0.0;
+    }
+    __device__ __forceinline__ Weights weights(const Params& p, float top) const {
+        Weights w;
+        w.infinite = top == INFINITY;
+        w.top = top;
+        w.factor = 1.44269504088896340736 / temperature;
+        w.low = min_p > 0.0f ? log2((double)min_p) : -4000.0;
+        w.steps = __builtin_ldexp(1.0, p.weight_bits);
+        return w;
+    }
+    __device__ __forceinline__ uint64_t goal(uint64_t total) const {
+        const uint64_t g = (uint64_t)(random * (double)total);
+        return g < total ? g : total - 1;
+    }
 };
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) v += __shfl_xor((unsigned long long)v, d);
-    return v;
+// Bin of a logit by its distance from the reference, the largest logits in the lowest bins: 32 bins to an
+// octave above it and 64 below, from 2^-5 to 2^11.  Larger logits are never in higher bins: the difference
+// and its rounding keep their order.
+__device__ __forceinline__ int bin_of(float x, float reference) {
+    const float d = reference - x;
+    const int bits = (int)(__builtin_bit_cast(uint32_t, d) & 0x7FFFFFFFu);
+    if (d < 0.0f) return kAbove - 1 - min(max((bits >> 18) - ((127 - 5) << 5), 0), kAbove - 1);
+    return kAbove + min(max((bits >> 17) - ((127 - 5) << 6), 0), kBelow - 1);
 }
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {  // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t o = __shfl_up((unsigned long long)v, d);
-        if ((int)(threadIdx.x % 64) >= d) v += o;
-    }
-    return v;
-}
-// Sum over the block of v in the lanes before this one; `total` the sum of all.
-__device__ __forceinline__ uint64_t block_before(Shared& s, uint64_t v, uint64_t& total) {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint64_t up = wave_scan(v);
-    __syncthreads();
-    if (lane == 63) s.parts[wave] = up;
-    __syncthreads();
-    uint64_t before = 0;
-    total = 0;
-    for (int i = 0; i < kWaves; ++i) {
-        const uint64_t part = s.parts[i];
-        if (i < wave) before += part;
-        total += part;
-    }
-    return before + up - v;
+__device__ __forceinline__ Way way_of(const Settings& set) { return set.top_k ? kCount : set.top_p < 1.0f ? kWeight : set.min_p > 0.0f ? kMinP : kDone; }
+
+// The least whole number of steps that reaches a share of the total, at least one.
+__device__ __forceinline__ uint64_t share_of(float share, uint64_t total) {
+    const double want = ceil((double)share * (double)total);
+    return want < 1.0 ? 1 : want >= (double)total ? total : (uint64_t)want;
 }
 
-// Which bin, counted from `from_top` or from the bottom, the sum of bins reaches `target`
-// in: the bin, what lies before it, and its own sum, the same in all lanes.
-__device__ __forceinline__ void find_bin(Shared& s, bool from_top, uint64_t target, uint32_t& digit, uint64_t& before, uint64_t& own) {
-    uint64_t v[kBins / kThreads], sum = 0, total;
-#pragma unroll
-    for (int i = 0; i < kBins / kThreads; ++i) {
-        const int at = threadIdx.x * (kBins / kThreads) + i;
-        v[i] = s.bins[from_top ? kBins - 1 - at : at];
-        sum += v[i];
-    }
-    uint64_t up = block_before(s, sum, total);
-#pragma unroll
-    for (int i = 0; i < kBins / kThreads; ++i) {
-        if (up < target && up + v[i] >= target) {
-            const int at = threadIdx.x * (kBins / kThreads) + i;
-            s.digit = from_top ? kBins - 1 - at : at;
-            s.before = up;
-            s.found = v[i];
-        }
-        up += v[i];
-    }
-    __syncthreads();
-    digit = s.digit, before = s.before, own = s.found;
-}
+// A listed word as a number, the smaller the earlier in the order of words; with its halves exchanged, the
+// smaller the lower the word.
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, int word) { return (uint64_t)~key << 32 | (uint32_t)word; }
+__device__ __forceinline__ uint64_t turned(uint64_t e) { return e << 32 | e >> 32; }
+__device__ __forceinline__ float value_of_entry(uint64_t e) { return value_of(~(uint32_t)(e >> 32)); }
 
-__device__ __forceinline__ void clear_bins(Shared& s) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
-    __syncthreads();
+// Values that workgroups of one launch pass on: atomic accesses at the device's scope go past the XCDs'
+// caches, so that no cache has to be written back or emptied for them (a release by every workgroup, which
+// writes back the L2, made the launch take 80 us longer for 256 rows).
+__device__ __forceinline__ void share_out(uint64_t* to, uint64_t v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint64_t share_in(const uint64_t* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// What a listed word weighs in a search.
+struct Weigh {
+    Weights weights;
+    uint64_t last;           // words after this one weigh nothing
+    bool ones, by_word;      // each weighs 1; numbers are turned
+    bool min_p;              // words that min-p leaves out weigh nothing
+    __device__ __forceinline__ uint64_t operator()(uint64_t number) const {
+        if (ones) return 1;
+        const uint64_t e = by_word ? turned(number) : number;
+        const double t = weights.log2_of(value_of_entry(e));
+        const uint64_t w = weights.of(t);
+        return e > last || (min_p && t < weights.low) ? 0 : w;
+    }
+};
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp64(uint64_t v) {  // 0 where no lane is read
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+    return (uint64_t)hi << 32 | lo;
 }
+// Over the lanes up to this one: their sum, or the largest of them.
+template <typename F>
+__device__ __forceinline__ uint64_t scan16(uint64_t v, F f) {  // of 16 lanes
+    v = f(v, dpp64<0x111, 0xF>(v));  // row_shr:1
+    v = f(v, dpp64<0x112, 0xF>(v));
+    v = f(v, dpp64<0x114, 0xF>(v));
+    return f(v, dpp64<0x118, 0xF>(v));
+}
+template <typename F>
+__device__ __forceinline__ uint64_t scan64(uint64_t v, F f) {
+    v = scan16(v, f);
+    v = f(v, dpp64<0x142, 0xA>(v));  // row_bcast:15 into rows 1, 3
+    return f(v, dpp64<0x143, 0xC>(v));  // row_bcast:31 into rows 2, 3
+}
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+struct Sum {
+    __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const { return a + b; }
+};
+struct Most {
+    __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const { return a > b ? a : b; }
+};
 __device__ __forceinline__ void add(uint64_t* at, uint64_t v) { atomicAdd(reinterpret_cast<unsigned long long*>(at), (unsigned long long)v); }
 
-template <typename T, typename F>
-__device__ __forceinline__ void each_word(const Row<T>& row, F f) {
-    for (int v = threadIdx.x; v < row.vectors; v += kThreads) {
-        float x[kPer<T>];
-        row.load(v, x);
-#pragma unroll
-        for (int i = 0; i < kPer<T>; ++i)
-            if (x[i] != -INFINITY) f(x[i], v * kPer<T> + i - row.lead);
-    }
+// What workgroups of kThreads lanes do.
+template <int kThreads>
+struct Block {
+static constexpr int kWaves = kThreads / 64;
+template <typename T>
+static constexpr int kEach = kVectors<T> / kThreads;  // vectors of a lane
+
+struct Small {  // what a block's lanes exchange
+    uint64_t parts[2][kWaves];
+    uint64_t before, found;
+    uint32_t digit, base, count;
+    int low, high;
+    int turn[kWaves];  // of parts; each wave has its own
+};
+static __device__ __forceinline__ void begin(Small& s) {
+    if (threadIdx.x % 64 == 0) s.turn[threadIdx.x / 64] = 0;
 }
 
-// The cut at which the words kept by `in` reach the target: `share` of their weights (share > 0) or
-// `count` of them (share = 0).
+
+// A chunk's words of a lane.
 template <typename T>
-__device__ Cut find_cut(Shared& s, const Row<T>& row, const Weights& weights, Cut in, double share, uint64_t count) {
-    const bool by_weight = share > 0.0;
-    uint64_t target = count, before = 0, own = 0;
-    uint32_t prefix = 0, digit;
-    // Digits of the logit, from the top: 11, 11 and 10 bits.  The integers of 16-bit logits end with the second.
-    constexpr int kLevels = sizeof(T) == 2 ? 2 : 3;
+struct Chunk {
+    u32x4 bits[kEach<T>];
+    float x[kEach<T>][kPer<T>];
+    int first;
+    __device__ __forceinline__ Chunk(const Row<T>& row, int chunk) {
+        first = chunk * kVectors<T> + threadIdx.x;
 #pragma unroll
-    for (int level = 0; level < kLevels; ++level) {
-        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, above = level == 0 ? 32 : level == 1 ? 21 : 10;
-        clear_bins(s);
-        each_word(row, [&](float x, int word) {
-            const uint32_t key = key_of(x);
-            if ((level == 0 || key >> above % 32 == prefix >> above % 32) && in.keeps(key, word))
-                add(&s.bins[(key >> shift) & ((1u << (above - shift)) - 1)], by_weight ? weights.of(weights.log2_of(x)) : 1);
-        });
-        __syncthreads();
-        if (level == 0 && by_weight) {
-            uint64_t sum = 0, total;
-            for (int i = threadIdx.x; i < kBins; i += kThreads) sum += s.bins[i];
-            block_before(s, sum, total);
-            const double want = ceil(share * (double)total);
-            target = want < 1.0 ? 1 : want >= (double)total ? total : (uint64_t)want;
-        }
-        uint64_t up;
-        find_bin(s, true, target - before, digit, up, own);
-        before += up;
-        prefix |= digit << shift;
+        for (int i = 0; i < kEach<T>; ++i) bits[i] = row.fetch(first + i * kThreads);
     }
-    // What the 16-bit types' integers leave below the second digit: ten ones for negative logits, zeros for others.
-    const uint32_t key = kLevels == 2 && !(prefix & 0x80000000u) ? prefix | 0x3FFu : prefix;
-    // Of `own`, the words with this logit, the first few are needed.
-    uint64_t each = 1;
-    if (by_weight) {
-        each = weights.of(weights.log2_of(value_of(key)));
-        each = each ? each : 1;
+    __device__ __forceinline__ void take(const Row<T>& row) {
+#pragma unroll
+        for (int i = 0; i < kEach<T>; ++i) row.words(first + i * kThreads, bits[i], x[i]);
     }
-    const uint64_t need = (target - before + each - 1) / each, have = own / each;
-    if (need >= have) return Cut{key, INT32_MAX};
-    uint64_t passed = 0;
+    template <typename F>
+    __device__ __forceinline__ void each(const Row<T>& row, F f) const {
+#pragma unroll
+        for (int i = 0; i < kEach<T>; ++i)
+#pragma unroll
+            for (int j = 0; j < kPer<T>; ++j) f(x[i][j], (first + i * kThreads) * kPer<T> - row.lead + j);
+    }
+};
+
+// Over the block: in the lanes before this one, and in all.  (Two places in turn, so that one barrier does.)
+template <typename F>
+static __device__ __forceinline__ uint64_t block_scan(Small& s, uint64_t v, uint64_t& all, F f) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    uint64_t* const parts = s.parts[s.turn[wave]];
+    const uint64_t up = scan64(v, f);
+    if (lane == 63) parts[wave] = up, s.turn[wave] ^= 1;
+    __syncthreads();
+    const uint64_t waves = scan16(lane < kWaves ? parts[lane] : 0, f);
+    all = lane_of(waves, kWaves - 1);
+    const uint64_t before = wave ? lane_of(waves, wave - 1) : 0;
+    const uint64_t mine = dpp64<0x138, 0xF>(up);  // wave_shr:1
+    return f(before, mine);
+}
+// Sum of v in the lanes before this one; `total` that of all.
+static __device__ __forceinline__ uint64_t block_before(Small& s, uint64_t v, uint64_t& total) { return block_scan(s, v, total, Sum()); }
+static __device__ __forceinline__ uint64_t block_sum(Small& s, uint64_t v) {
+    uint64_t total;
+    block_scan(s, v, total, Sum());
+    return total;
+}
+static __device__ __forceinline__ uint64_t block_most(Small& s, uint64_t v) {
+    uint64_t most;
+    block_scan(s, v, most, Most());
+    return most;
+}
+// The best word of the block's words, the same in all lanes: the largest key, of equal ones the lowest word.
+static __device__ __forceinline__ void block_best(Small& s, uint32_t& key, int& word) {
+    const uint64_t best = block_most(s, (uint64_t)key << 32 | ~(uint32_t)word);
+    key = (uint32_t)(best >> 32), word = (int)~(uint32_t)best;
+}
+
+// The reference: the largest logit of the row's first vectors, the same for all of its chunks.
+template <typename T>
+static __device__ __forceinline__ float reference_of(Small& s, const Row<T>& row, u32x4 bits) {
+    uint32_t key = kNothing;
     int word = 0;
+    float y[kPer<T>];
+    row.words(threadIdx.x, bits, y);
 #pragma unroll
-    for (int level = 0; level < 2; ++level) {
-        clear_bins(s);
-        each_word(row, [&](float x, int w) {
-            if (key_of(x) == key && in.keeps(key, w) && (level == 0 || w >> 10 == word >> 10)) add(&s.bins[level == 0 ? w >> 10 : w & 1023], 1);
-        });
-        __syncthreads();
-        uint64_t up;
-        find_bin(s, false, need - passed, digit, up, own);
-        passed += up;
-        word |= digit << (level == 0 ? 10 : 0);
-    }
-    return Cut{key, word};
+    for (int i = 0; i < kPer<T>; ++i) key = max(key, key_of(y[i]));
+    block_best(s, key, word);
+    return key == kNothing || key == kInfinity ? 0.0f : value_of(key);
 }
 
+// Workgroups of a row are `rows` apart, so that a row's run at the same time.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(const Params p) {
-    __shared__ Shared s;
-    const wq_sample_call& c = p.c;
+static __device__ __forceinline__ void survey(const Params& p) {
+    __shared__ struct : Small {
+        uint64_t bins[kBins];
+    } s;
     const int64_t r = blockIdx.x;
+    const int chunk = blockIdx.y;
     const Row<T> row(p, r);
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-
-    // The best word.
+    begin(s);
+    Chunk<T> x(row, chunk);
+    const u32x4 ahead = row.fetch(threadIdx.x);
+    const Settings set(p, r);
+    const Way way = way_of(set);
+    const bool binned = !set.greedy && (way == kCount || way == kWeight);
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
+    if (threadIdx.x == 0) s.low = kBins, s.high = 0;
+    x.take(row);
     uint32_t best = kNothing;
     int word = INT32_MAX;
-    each_word(row, [&](float x, int w) {
-        const uint32_t key = key_of(x);
-        if (key > best) best = key, word = w;  // (A lane's words rise.)
+    x.each(row, [&](float v, int w) {
+        const uint32_t key = key_of(v);
+        word = key > best ? w : word;  // (A lane's words rise.)
+        best = max(best, key);
     });
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        const uint32_t k = __shfl_xor(best, d);
-        const int w = __shfl_xor(word, d);
-        if (k > best || (k == best && w < word)) best = k, word = w;
-    }
-    if (lane == 0) s.keys[wave] = best, s.words[wave] = word;
-    __syncthreads();
-    for (int i = 0; i < kWaves; ++i) {
-        const uint32_t k = s.keys[i];
-        const int w = s.words[i];
-        if (k > best || (k == best && w < word)) best = k, word = w;
-    }
-    const float temperature = c.temperature ? gbl(c.temperature)[r] : 1.0f;
-    if (best == kNothing || !(temperature > 0.0f)) {
-        if (threadIdx.x == 0) {
-            gbl(c.token)[r] = best == kNothing ? -1 : word;
-            if (c.share) gbl(c.share)[r] = best == kNothing ? 0.0f : 1.0f;
-        }
-        return;
-    }
-    const int top_k = c.top_k ? gbl(c.top_k)[r] : 0;
-    const float top_p = c.top_p ? gbl(c.top_p)[r] : 1.0f, min_p = c.min_p ? gbl(c.min_p)[r] : 0.0f;
-    Weights weights;
-    weights.infinite = best == kInfinity;
-    weights.top = (double)value_of(best);
-    weights.factor = 1.44269504088896340736 / (double)temperature;
-    weights.low = min_p > 0.0f ? log2((double)fminf(min_p, 1.0f)) : -4000.0;
-    weights.steps = __builtin_ldexp(1.0, p.weight_bits);
-
-    Cut cut{kNothing, INT32_MAX};
-    if (top_k > 0 && top_k < row.vocab) {
-        uint64_t n = 0, total;
-        each_word(row, [&](float, int) { ++n; });
-        block_before(s, n, total);
-        if ((uint64_t)top_k < total) cut = find_cut(s, row, weights, cut, 0.0, (uint64_t)top_k);
-    }
-    if (top_p < 1.0f) cut = top_p > 0.0f ? find_cut(s, row, weights, cut, (double)top_p, 0) : Cut{best, word};
-
-    // The weights of the words that stay, by tiles of one vector per lane.
-    auto weight = [&](float x, int w) -> uint64_t {
-        if (x == -INFINITY || !cut.keeps(key_of(x), w)) return 0;
-        const double t = weights.log2_of(x);
-        return t >= weights.low ? weights.of(t) : 0;
-    };
-    const int tiles = (row.vectors + kThreads - 1) / kThreads;
-    __syncthreads();
-    for (int i = threadIdx.x; i < tiles; i += kThreads) s.tiles[i] = 0;
-    __syncthreads();
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int v = tile * kThreads + threadIdx.x;
+    block_best(s, best, word);
+    Record record{0, best, word, 0, 0, 0.0f, 0};
+    const int64_t at = r * p.chunks + chunk;
+    if (binned) record.reference = reference_of(s, row, ahead);
+    if (!set.greedy && best != kNothing && way != kMinP) {
+        const Weights weights = set.weights(p, value_of(best));
         uint64_t sum = 0;
-        if (v < row.vectors) {
-            float x[kPer<T>];
-            row.load(v, x);
-#pragma unroll
-            for (int i = 0; i < kPer<T>; ++i) sum += weight(x[i], v * kPer<T> + i - row.lead);
+        if (way == kCount) {
+            x.each(row, [&](float v, int) {
+                if (v > -INFINITY) add(&s.bins[bin_of(v, record.reference)], 1);
+            });
+        } else {
+            // The weights first, so that their chains of operations run side by side.
+            uint64_t w[kEach<T> * kPer<T>];
+            int n = 0;
+            x.each(row, [&](float v, int) { w[n++] = weights.of(weights.log2_of(v)); });
+            n = 0;
+            x.each(row, [&](float v, int) {
+                if (binned && w[n]) add(&s.bins[bin_of(v, record.reference)], w[n]);
+                sum += w[n++];
+            });
         }
-        sum = wave_sum(sum);
-        if (lane == 0 && sum) add(&s.tiles[tile], sum);
+        if (binned) {
+            __syncthreads();
+            int low = kBins, high = 0;
+            for (int i = threadIdx.x; i < kBins; i += kThreads)
+                if (s.bins[i]) low = min(low, i), high = max(high, i + 1);
+            if (high) atomicMin(&s.low, low), atomicMax(&s.high, high);
+            __syncthreads();
+            record.low = s.low, record.high = s.high;
+            for (int i = s.low + threadIdx.x; i < s.high; i += kThreads) gbl(p.bins)[at * kBins + i] = s.bins[i];
+        } else {
+            record.sum = block_sum(s, sum);
+        }
+    }
+    if (threadIdx.x == 0) p.records[at] = record;
+}
+
+// The word of a chunk at which the sum of weights passes `goal`.
+template <typename T, typename F>
+static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p, int64_t r, const Row<T>& row, int chunk, uint64_t goal, double total, F weight) {
+    // Words in their order are vector by vector, and the lanes of a round are consecutive ones.
+#pragma unroll 1
+    for (int i = 0; i < kEach<T>; ++i) {
+        const int v = chunk * kVectors<T> + threadIdx.x + i * kThreads;
+        float y[kPer<T>];
+        row.words(v, row.fetch(v), y);
+        uint64_t w[kPer<T>], sum = 0, all;
+#pragma unroll
+        for (int j = 0; j < kPer<T>; ++j) {
+            w[j] = weight(y[j], v * kPer<T> + j - row.lead);
+            sum += w[j];
+        }
+        uint64_t up = block_before(s, sum, all);
+        if (goal < all) {
+#pragma unroll
+            for (int j = 0; j < kPer<T>; ++j) {
+                if (up <= goal && goal < up + w[j]) {
+                    gbl(p.c.token)[r] = v * kPer<T> + j - row.lead;
+                    if (p.c.share) gbl(p.c.share)[r] = (float)((double)w[j] / total);
+                }
+                up += w[j];
+            }
+            return;
+        }
+        goal -= all;
+    }
+}
+
+// A workgroup to a row.
+template <typename T>
+static __device__ __forceinline__ void plan(const Params& p) {
+    __shared__ struct : Small {
+        double scales[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+        int ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+    } s;
+    const int64_t r = blockIdx.x;
+    begin(s);
+    const Row<T> row(p, r);
+    const Settings set(p, r);
+    // What survey left: thread i has chunk i's.
+    const bool has = (int)threadIdx.x < p.chunks;
+    Record record{0, kNothing, INT32_MAX, 0, 0, 0.0f, 0};
+    if (has) record = p.records[r * p.chunks + threadIdx.x];
+    uint32_t best = record.key;
+    int word = record.word;
+    block_best(s, best, word);
+    Plan plan{};
+    plan.best = best, plan.word = word, plan.reference = record.reference, plan.cut_bin = kBins;
+    plan.way = best == kNothing || set.greedy ? kDone : way_of(set);
+    if (best == kNothing || set.greedy) {
+        if (threadIdx.x == 0) {
+            gbl(p.c.token)[r] = best == kNothing ? -1 : word;
+            if (p.c.share) gbl(p.c.share)[r] = best == kNothing ? 0.0f : 1.0f;
+        }
+    } else if (plan.way != kMinP) {
+        // A chunk's weights are multiples of those of its largest logit.
+        const Weights weights = set.weights(p, value_of(best));
+        const double scale = plan.way == kCount ? 1.0 : record.key == kNothing ? 0.0 : exp2_of(weights.log2_of(value_of(record.key)));
+        auto scaled = [](uint64_t sum, double by) { return (uint64_t)__builtin_rint((double)sum * by); };
+        if (plan.way == kDone) {
+            const uint64_t mine = scaled(record.sum, scale);
+            uint64_t total;
+            const uint64_t up = block_before(s, mine, total), goal = set.goal(total);
+            if (up <= goal && goal < up + mine) {
+                const uint64_t within = (uint64_t)((double)(goal - up) / scale);
+                s.digit = threadIdx.x, s.before = within < record.sum ? within : record.sum - 1;
+                s.scales[0] = (double)total / scale, s.base = record.key;
+            }
+            __syncthreads();
+            const Weights own = set.weights(p, value_of(s.base));
+            choose_in_chunk(s, p, r, row, (int)s.digit, s.before, s.scales[0], [&](float v, int) { return own.of(own.log2_of(v)); });
+        } else {
+            // The bin that the cut lies in, and what lies before it.
+            if ((int)threadIdx.x < p.chunks + kAhead) s.scales[threadIdx.x] = scale, s.ranges[threadIdx.x] = has ? record.low | record.high << 16 : 0;
+            __syncthreads();
+            constexpr int kMine = (kBins + kThreads - 1) / kThreads;  // (Of the last lanes none.)
+            uint64_t v[kMine] = {}, sum = 0, total;
+            const int first = threadIdx.x * kMine;
+#pragma unroll 1
+            for (int c = 0; c < p.chunks; c += kAhead) {
+                uint64_t b[kAhead][kMine];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    const uint64_t* const bins = p.bins + (r * p.chunks + min(c + a, p.chunks - 1)) * kBins + min(first, kBins - kMine);
+#pragma unroll
+                    for (int i = 0; i < kMine; ++i) b[a][i] = gbl(bins)[i];
+                }
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    const int low = s.ranges[c + a] & 0xFFFF, high = s.ranges[c + a] >> 16;
+                    const double by = s.scales[c + a];
+#pragma unroll
+                    for (int i = 0; i < kMine; ++i) {
+                        const uint64_t held = first + i >= low && first + i < high ? b[a][i] : 0;  // (What lies outside was not written.)
+                        v[i] += plan.way == kCount ? held : scaled(held, by);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) sum += v[i];
+            uint64_t up = block_before(s, sum, total);
+            const uint64_t target = plan.way == kCount ? std::min<uint64_t>(set.top_k, total) : share_of(set.top_p, total);
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                if (up < target && up + v[i] >= target) s.digit = first + i, s.before = up, s.found = v[i];
+                up += v[i];
+            }
+            __syncthreads();
+            plan.cut_bin = (int)s.digit, plan.ahead = s.before, plan.need = target - s.before;
+            // While all words that may stay are few, all are listed.  A long list, and top-p behind a long
+            // top-k, are worked out by one workgroup.
+            if (plan.way == kCount) {
+                plan.few = s.before + s.found <= (uint64_t)p.list_size;
+                plan.alone = !plan.few && (set.top_p < 1.0f || s.found > (uint64_t)p.list_size);
+            }
+        }
+    }
+    if (threadIdx.x == 0) p.plans[r] = plan;
+}
+
+struct Choice : Small {
+    uint64_t list[kList];
+    uint64_t bins[kParts];
+    uint64_t active[kRanked];
+    uint64_t chunks[WQ_SAMPLE_MAX_VOCAB / kChunk + 1];
+};
+
+// f for every number of the list, or for every word of the row.
+template <typename T, typename F>
+static __device__ __forceinline__ void each_number(Choice& s, const Row<T>& row, bool of_row, int listed, F f) {
+    if (of_row) {
+        row.each(0, row.vectors, [&](float v, int w) {
+            if (v > -INFINITY) f(entry_of(key_of(v), w));
+        });
+    } else {
+#pragma unroll 1
+        for (int i = threadIdx.x; i < listed; i += kThreads) f(s.list[i]);
+    }
+}
+
+// The number up to which, in rising order, the numbers' weights reach `target` (which their sum does).  Their
+// range is cut into kParts; of the part that it lies in, the range again, until each lane has one number left
+// and can add up those below it.
+template <typename T>
+static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& row, bool of_row, int listed, uint64_t target, const Weigh& weigh) {
+    uint64_t low = 0, high = ~0ull;  // it lies in here
+#pragma unroll 1
+    for (;;) {
+        uint64_t least = ~0ull, most = 0;
+        uint32_t total = listed;
+        const bool all_few = !of_row && listed <= kRanked;
+        __syncthreads();
+        if (!all_few) {
+            uint32_t left = 0;
+            each_number(s, row, of_row, listed, [&](uint64_t e) {
+                if (e >= low && e <= high) least = std::min(least, e), most = std::max(most, e), ++left;
+            });
+            least = ~block_most(s, ~least);
+            most = block_most(s, most);
+            total = (uint32_t)block_sum(s, left);
+        }
+        if (total <= kRanked) {
+            if (!all_few) {
+                if (threadIdx.x == 0) s.count = 0;
+                __syncthreads();
+                each_number(s, row, of_row, listed, [&](uint64_t e) {
+                    if (e >= low && e <= high) s.active[atomicAdd(&s.count, 1u)] = e;
+                });
+                __syncthreads();
+            }
+            const uint64_t* const numbers = all_few ? s.list : s.active;
+            const bool mine = threadIdx.x < total;
+            const uint64_t e = mine ? numbers[threadIdx.x] : 0, w = mine ? weigh(e) : 0;
+            if (mine) s.bins[threadIdx.x] = w;
+            __syncthreads();
+            uint64_t below = 0;
+            if (mine) {
+#pragma unroll 8
+                for (uint32_t i = 0; i < total; ++i) below += numbers[i] < e ? s.bins[i] : 0;
+                if (below < target && below + w >= target) s.found = e;
+            }
+            __syncthreads();
+            return s.found;
+        }
+        const int bits = 64 - __builtin_clzll(most - least), shift = bits > kPartBits ? bits - kPartBits : 0;
+        for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
+        __syncthreads();
+        each_number(s, row, of_row, listed, [&](uint64_t e) {
+            if (e >= low && e <= high) add(&s.bins[(e - least) >> shift], weigh(e));
+        });
+        __syncthreads();
+        constexpr int kMine = (kParts + kThreads - 1) / kThreads;
+        uint64_t own[kMine], sum = 0, all;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int at = threadIdx.x * kMine + i;
+            own[i] = at < kParts ? s.bins[at] : 0;
+            sum += own[i];
+        }
+        uint64_t up = block_before(s, sum, all);
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (up < target && up + own[i] >= target) s.digit = threadIdx.x * kMine + i, s.before = up;
+            up += own[i];
+        }
+        __syncthreads();
+        low = least + ((uint64_t)s.digit << shift);
+        high = low + (((uint64_t)1 << shift) - 1);
+        target -= s.before;
+    }
+}
+
+template <typename T>
+static __device__ __forceinline__ void choose(const Params& p) {
+    __shared__ Choice s;
+    const int64_t r = blockIdx.x;
+    const int chunk = blockIdx.y;
+    const Row<T> row(p, r);
+    begin(s);
+    Chunk<T> x(row, chunk);
+    Plan* const plan = p.plans + r;
+    const Way way = (Way)plan->way;
+    if (way == kDone) return;
+    const Settings set(p, r);
+    Weigh weigh{set.weights(p, value_of(plan->best)), ~0ull, false, false, false};
+    const Weights& weights = weigh.weights;
+    const uint64_t need = plan->need, ahead = plan->ahead;
+    const bool few = plan->few, alone = plan->alone;
+    if (alone) {
+        if (chunk != 0) return;
+    } else {
+        const float reference = plan->reference;
+        const int cut_bin = plan->cut_bin;
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        x.take(row);
+        uint64_t sum = 0;
+        if (!few) {
+            x.each(row, [&](float v, int) {
+                const double t = weights.log2_of(v);
+                const uint64_t w = weights.of(t);
+                sum += t >= weights.low && (way == kMinP || bin_of(v, reference) < cut_bin) ? w : 0;
+            });
+        }
+        if (way != kMinP) {
+            x.each(row, [&](float v, int w) {
+                const int bin = v > -INFINITY ? bin_of(v, reference) : kBins;
+                if (bin == cut_bin || (few && bin < cut_bin)) {
+                    const uint64_t e = entry_of(key_of(v), w);
+                    const uint32_t at = atomicAdd(&s.count, 1u);
+                    if (at < kList) {
+                        s.list[at] = e;
+                    } else {
+                        const uint32_t to = atomicAdd(&plan->listed, 1u);
+                        if (to < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + to, e);
+                    }
+                }
+            });
+        }
+        if (!few) {
+            sum = block_sum(s, sum);
+            if (threadIdx.x == 0) share_out(p.sums + r * p.chunks + chunk, sum);
+        }
+        __syncthreads();
+        const uint32_t count = std::min<uint32_t>(s.count, kList);
+        if (threadIdx.x == 0 && count) s.base = atomicAdd(&plan->listed, count);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < count; i += kThreads)
+            if (s.base + i < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + s.base + i, s.list[i]);
+        // The last workgroup of the row goes on.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave shares has arrived
+        __syncthreads();
+        if (threadIdx.x == 0) s.digit = __hip_atomic_fetch_add(&plan->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)p.chunks;
+        __syncthreads();
+        if (!s.digit) return;
+        asm volatile("" ::: "memory");
+    }
+    const bool has = (int)threadIdx.x < p.chunks;
+    int listed = alone ? 0 : (int)__hip_atomic_load(&plan->listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool of_row = alone || listed > p.list_size;  // no list, or one that did not hold all
+    __syncthreads();
+    if (!of_row)
+        for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = share_in(p.list + r * p.list_size + i);
+    if (has) s.chunks[threadIdx.x] = few || of_row ? 0 : share_in(p.sums + r * p.chunks + threadIdx.x);
+    __syncthreads();
+    // The searches: the last word that stays, by number for top-k and by weight for top-p; where all words that stay
+    // are listed, then the word that the random number falls on, in the order of words.
+    const bool complete = few || of_row;  // the list, or the row, holds what lies ahead of the cut's bin too
+    uint64_t total = 0;
+#pragma unroll 1
+    for (int search = 0; search < 3; ++search) {
+        uint64_t target;
+        if (search == 0) {
+            if (way != kCount) continue;
+            weigh.ones = true;
+            target = complete ? ahead + need : need;
+        } else if (search == 1) {
+            if (way == kMinP || set.top_p >= 1.0f) continue;
+            weigh.ones = false;
+            uint64_t sum = 0;
+            each_number(s, row, of_row, listed, [&](uint64_t e) { sum += weigh(e); });
+            sum = block_sum(s, sum);
+            target = complete ? share_of(set.top_p, sum) : std::min(need, sum);
+            if (target == 0) continue;  // words too light to weigh anything: it does not matter which stay
+        } else {
+            weigh.ones = false, weigh.min_p = true;
+            if (!few || of_row) continue;
+            uint64_t sum = 0;
+            each_number(s, row, of_row, listed, [&](uint64_t e) { sum += weigh(e); });
+            total = block_sum(s, sum);
+            target = set.goal(total) + 1;
+            for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = turned(s.list[i]);
+            weigh.by_word = true;
+        }
+        const uint64_t found = find_number(s, row, of_row, listed, target, weigh);
+        if (search < 2) {
+            weigh.last = found;
+        } else {
+            if (threadIdx.x == 0) {
+                gbl(p.c.token)[r] = (int)(found >> 32);
+                if (p.c.share) gbl(p.c.share)[r] = (float)((double)weigh(found) / (double)total);
+            }
+            return;
+        }
+    }
+    // The chunks' weights, those of the list among them, and the chunk that the random number falls into.
+    if (of_row) {
+#pragma unroll 1
+        for (int c = 0; c < p.chunks; ++c) {
+            uint64_t sum = 0;
+            row.each(c * kVectors<T>, min((c + 1) * kVectors<T>, row.vectors), [&](float v, int w) { sum += weigh(entry_of(key_of(v), w)); });
+            if (sum) add(&s.chunks[c], sum);
+        }
+    } else {
+#pragma unroll 1
+        for (int i = threadIdx.x; i < listed; i += kThreads) {
+            const uint64_t w = weigh(s.list[i]);
+            if (w) add(&s.chunks[row.chunk_of((int)(uint32_t)s.list[i])], w);
+        }
     }
     __syncthreads();
-    // The tile in which the sum passes random * total, found by every lane for itself from its share of the tiles.
-    uint64_t total;
-    const uint64_t mine = (int)threadIdx.x < tiles ? s.tiles[threadIdx.x] : 0;
-    const uint64_t up = block_before(s, mine, total);
-    const float random = gbl(c.random)[r];
-    const double u = random > 0.0f ? fmin((double)random, 0.99999999999999989) : 0.0;
-    uint64_t goal = (uint64_t)(u * (double)total);
-    goal = goal < total ? goal : total - 1;
+    const uint64_t mine = has ? s.chunks[threadIdx.x] : 0, up = block_before(s, mine, total), goal = set.goal(total);
     if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = up;
     __syncthreads();
-    const int tile = (int)s.digit;
-    goal -= s.before;
-    // Its words.
-    const int v = tile * kThreads + threadIdx.x;
-    uint64_t w[kPer<T>], sum = 0;
-    float x[kPer<T>];
-    if (v < row.vectors) row.load(v, x);
-#pragma unroll
-    for (int i = 0; i < kPer<T>; ++i) {
-        w[i] = v < row.vectors ? weight(x[i], v * kPer<T> + i - row.lead) : 0;
-        sum += w[i];
-    }
-    uint64_t unused, at = block_before(s, sum, unused);
-#pragma unroll
-    for (int i = 0; i < kPer<T>; ++i) {
-        if (at <= goal && goal < at + w[i]) {
-            gbl(c.token)[r] = v * kPer<T> + i - row.lead;
-            if (c.share) gbl(c.share)[r] = (float)((double)w[i] / (double)total);
-        }
-        at += w[i];
-    }
+    const int target = (int)s.digit;
+    const uint64_t within = goal - s.before;
+    choose_in_chunk(s, p, r, row, target, within, (double)total, [&](float v, int w) { return weigh(entry_of(key_of(v), w)); });
+}
+};
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void survey_kernel(const Params p) {
+    Block<THREADS>::template survey<T>(p);
+}
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void plan_kernel(const Params p) {
+    Block<THREADS>::template plan<T>(p);
+}
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void choose_kernel(const Params p) {
+    Block<THREADS>::template choose<T>(p);
 }
 
 // ------------------------------------------------------------------ host
@@ -388,7 +835,62 @@ wq_status check_sizes(const char* fn, int64_t rows, int64_t vocab, int64_t dtype
     return WQ_OK;
 }
 
-size_t workspace_of(int64_t, int64_t, int64_t) { return 0; }
+// Chunks of a row, wherever in 16 bytes it starts.
+int64_t chunks_of(int64_t vocab, int64_t dtype) {
+    const int64_t lead = dtype == WQ_DTYPE_F32 ? 3 : 7;
+    return (vocab + lead + kChunk - 1) / kChunk;
+}
+constexpr int kFewThreads = 1024, kManyThreads = 256;  // of a workgroup, in small batches and in large ones
+static_assert(WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead <= kManyThreads && kRanked <= kManyThreads, "a lane for every chunk and for every word compared");
+
+// The parts of the workspace, each a multiple of 16 bytes.
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+size_t lay_out(Params& p, uint8_t* base) {
+    const size_t rows = (size_t)p.c.rows, chunks = rows * p.chunks;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        uint8_t* const part = base ? base + at : nullptr;
+        at += round16(bytes);
+        return part;
+    };
+    p.records = reinterpret_cast<Record*>(take(chunks * sizeof(Record)));
+    p.sums = reinterpret_cast<uint64_t*>(take(chunks * 8));
+    p.plans = reinterpret_cast<Plan*>(take(rows * sizeof(Plan)));
+    p.list = reinterpret_cast<uint64_t*>(take(rows * p.list_size * 8));
+    p.bins = reinterpret_cast<uint64_t*>(take(chunks * kBins * 8));
+    return at;
+}
+
+void set_sizes(Params& p) {
+    p.chunks = (int32_t)chunks_of(p.c.vocab, p.c.dtype);
+    p.list_size = (int32_t)std::min<int64_t>(kList, p.c.vocab);
+    p.weight_bits = std::min(51, 62 - log2_of(p.c.vocab));
+}
+// Rows of one pair of launches: enough chunks to fill the CUs several times over; more rows take more
+// launches, which share the workspace.
+int64_t slab_of(const Params& p) { return std::max<int64_t>(1, 4096 / p.chunks); }
+
+size_t workspace_of(int64_t rows, int64_t vocab, int64_t dtype) {
+    Params p{};
+    p.c.vocab = vocab;
+    p.c.dtype = dtype;
+    set_sizes(p);
+    p.c.rows = std::min(rows, slab_of(p));
+    return lay_out(p, nullptr);
+}
+
+template <typename T, int THREADS>
+void launch_as(const Params& p, hipStream_t st) {
+    const dim3 grid((unsigned)p.c.rows, (unsigned)p.chunks), block(THREADS);
+    hipLaunchKernelGGL((survey_kernel<T, THREADS>), grid, block, 0, st, p);
+    hipLaunchKernelGGL((plan_kernel<T, THREADS>), dim3((unsigned)p.c.rows), block, 0, st, p);
+    hipLaunchKernelGGL((choose_kernel<T, THREADS>), grid, block, 0, st, p);
+}
+template <typename T>
+void launch(const Params& p, hipStream_t st) {
+    if (p.c.rows * p.chunks < 512) launch_as<T, kFewThreads>(p, st);
+    else launch_as<T, kManyThreads>(p, st);
+}
 
 }  // namespace
 }  // namespace sample
@@ -433,13 +935,27 @@ wq_status wq_sample_logits(const wq_sample_call* call, void* workspace, size_t w
         if (overlaps(s, token) || overlaps(s, share) || overlaps(s, work)) return err(WQ_ERR_INVALID_ARG, "%s: an output or the workspace overlaps an input", fn);
     if (overlaps(token, share) || overlaps(token, work) || overlaps(share, work))
         return err(WQ_ERR_INVALID_ARG, "%s: token, share and the workspace must not overlap", fn);
-    p.weight_bits = std::min(51, 62 - log2_of(c.vocab));
+    set_sizes(p);
+    p.has = (c.temperature ? 1 : 0) | (c.top_p ? 2 : 0) | (c.min_p ? 4 : 0) | (c.top_k ? 8 : 0);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)c.rows), block(kThreads);
     (void)hipGetLastError();
-    if (c.dtype == WQ_DTYPE_F16) hipLaunchKernelGGL((sample_kernel<_Float16>), grid, block, 0, st, p);
-    else if (c.dtype == WQ_DTYPE_BF16) hipLaunchKernelGGL((sample_kernel<__bf16>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((sample_kernel<float>), grid, block, 0, st, p);
+    const int64_t slab = slab_of(p);
+    for (int64_t row = 0; row < call->rows; row += slab) {
+        p.c = *call;
+        p.c.rows = std::min(slab, call->rows - row);
+        p.c.logits = static_cast<const uint8_t*>(call->logits) + row * call->logits_stride * size;
+        p.c.random += row;
+        p.c.token += row;
+        p.c.temperature = call->temperature ? call->temperature + row : p.c.random;
+        p.c.top_p = call->top_p ? call->top_p + row : p.c.random;
+        p.c.min_p = call->min_p ? call->min_p + row : p.c.random;
+        p.c.top_k = call->top_k ? call->top_k + row : reinterpret_cast<const int32_t*>(p.c.random);
+        if (p.c.share) p.c.share += row;
+        lay_out(p, static_cast<uint8_t*>(workspace));
+        if (call->dtype == WQ_DTYPE_F16) launch<_Float16>(p, st);
+        else if (call->dtype == WQ_DTYPE_BF16) launch<__bf16>(p, st);
+        else launch<float>(p, st);
+    }
     return wq::host::hip_result(fn, hipGetLastError());
 }
 
