@@ -61,23 +61,25 @@ constexpr int kVectors = kChunk / kPer<T>;  // of a chunk
 // [low, high) that are not empty.
 struct Record {
     uint64_t sum;
+    double offset;  // of its weights
     uint32_t key;
     int32_t word;
     int32_t low, high;
-    float reference;  // of the row's bins
+    float reference;  // of the row's bins and weights
     int32_t unused;
 };
 // What choose does with a row.
 enum Way { kDone, kMinP, kCount, kWeight };
 // What plan tells choose, and what choose's workgroups share.
 struct Plan {
+    double offset;              // of the weights
     uint64_t ahead, need;       // words, or weights, before the cut's bin, and of it up to the cut
     uint32_t best;              // key of the largest logit
     int32_t word;               // and its word
     float reference;
     int32_t way, cut_bin, few, alone;
     uint32_t done, listed;      // workgroups that are done, and words listed
-    int32_t unused[3];
+    int32_t unused;
 };
 
 struct Params {
@@ -173,14 +175,17 @@ __device__ __forceinline__ double exp2_of(double t) {
     return __builtin_ldexp(r, (int)n);
 }
 
-// How a row's logits become weights.
+// How a row's logits become weights: w = 2^((x - base) log2(e) / temperature - offset), a multiple of exp((x -
+// max x) / temperature) that all of the row's chunks can share, as base and the whole number offset do not need
+// to be the largest logit's; w is at most 1.
 struct Weights {
-    double top, factor, low;  // largest logit; log2(e) / temperature; smallest log2 w that stays under min-p
-    double steps;             // 2^s
-    bool infinite;
-    // log2 w; at most 0, not below -2000, which weighs nothing, as -infinity does.
+    double base, factor, offset;
+    double low;      // smallest log2 w that min-p leaves
+    double steps;    // 2^s
+    bool infinite;   // the largest logit is +infinity
+    // log2 w; not below -2000, which weighs nothing, as -infinity does.
     __device__ __forceinline__ double log2_of(float x) const {
-        const double t = x == -INFINITY ? -2000.0 : fmax(((double)x - top) * factor, -2000.0);
+        const double t = x == -INFINITY ? -2000.0 : fmax(fma((double)x - base, factor, -offset), -2000.0);
         return infinite ? (x == INFINITY ? 0.0 : -2000.0) : t;
     }
     // A whole number of steps, rounded to nearest.  (Below 2^52, adding 2^52 leaves the number in the low bits.)
@@ -218,13 +223,16 @@ struct Settings {
         min_p = mp > 0.0f ? fminf(mp, 1.0f) : 0.0f;
         random = u > 0.0f ? fmin((double)u, 0.99999999999999989) : 0.0;
     }
-    __device__ __forceinline__ Weights weights(const Params& p, float top) const {
+    // The smallest offset with which no logit up to `top` weighs more than 1.
+    __device__ __forceinline__ double offset_of(float top, float base) const { return ceil(((double)top - base) * (1.44269504088896340736 / temperature)); }
+    __device__ __forceinline__ Weights weights(const Params& p, float top, float base, double offset) const {
         Weights w;
         w.infinite = top == INFINITY;
-        w.top = top;
+        w.base = base;
         w.factor = 1.44269504088896340736 / temperature;
-        w.low = min_p > 0.0f ? log2((double)min_p) : -4000.0;
+        w.offset = offset;
         w.steps = __builtin_ldexp(1.0, p.weight_bits);
+        w.low = min_p > 0.0f ? w.log2_of(top) + log2((double)min_p) : -4000.0;
         return w;
     }
     __device__ __forceinline__ uint64_t goal(uint64_t total) const {
@@ -422,11 +430,12 @@ static __device__ __forceinline__ void survey(const Params& p) {
         best = max(best, key);
     });
     block_best(s, best, word);
-    Record record{0, best, word, 0, 0, 0.0f, 0};
+    Record record{0, 0.0, best, word, 0, 0, reference_of(s, row, ahead), 0};
     const int64_t at = r * p.chunks + chunk;
-    if (binned) record.reference = reference_of(s, row, ahead);
     if (!set.greedy && best != kNothing && way != kMinP) {
-        const Weights weights = set.weights(p, value_of(best));
+        const bool infinite = best == kInfinity;
+        record.offset = infinite ? 0.0 : set.offset_of(value_of(best), record.reference);
+        const Weights weights = set.weights(p, value_of(best), record.reference, record.offset);
         uint64_t sum = 0;
         if (way == kCount) {
             x.each(row, [&](float v, int) {
@@ -494,7 +503,7 @@ static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p
 template <typename T>
 static __device__ __forceinline__ void plan(const Params& p) {
     __shared__ struct : Small {
-        double scales[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+        int overs[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
         int ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
     } s;
     const int64_t r = blockIdx.x;
@@ -503,39 +512,37 @@ static __device__ __forceinline__ void plan(const Params& p) {
     const Settings set(p, r);
     // What survey left: thread i has chunk i's.
     const bool has = (int)threadIdx.x < p.chunks;
-    Record record{0, kNothing, INT32_MAX, 0, 0, 0.0f, 0};
+    Record record{0, 0.0, kNothing, INT32_MAX, 0, 0, 0.0f, 0};
     if (has) record = p.records[r * p.chunks + threadIdx.x];
     uint32_t best = record.key;
     int word = record.word;
     block_best(s, best, word);
+    const float reference = p.records[r * p.chunks].reference;
     Plan plan{};
-    plan.best = best, plan.word = word, plan.reference = record.reference, plan.cut_bin = kBins;
+    plan.best = best, plan.word = word, plan.cut_bin = kBins, plan.reference = reference;
     plan.way = best == kNothing || set.greedy ? kDone : way_of(set);
     if (best == kNothing || set.greedy) {
         if (threadIdx.x == 0) {
             gbl(p.c.token)[r] = best == kNothing ? -1 : word;
             if (p.c.share) gbl(p.c.share)[r] = best == kNothing ? 0.0f : 1.0f;
         }
-    } else if (plan.way != kMinP) {
-        // A chunk's weights are multiples of those of its largest logit.
-        const Weights weights = set.weights(p, value_of(best));
-        const double scale = plan.way == kCount ? 1.0 : record.key == kNothing ? 0.0 : exp2_of(weights.log2_of(value_of(record.key)));
-        auto scaled = [](uint64_t sum, double by) { return (uint64_t)__builtin_rint((double)sum * by); };
+    } else {
+        // A chunk's offset differs from the row's by a whole number: by as many bits its weights are too large.  (Where the
+        // largest logit is +infinity, only the chunks that have it weigh anything.)
+        const bool infinite = best == kInfinity;
+        plan.offset = infinite ? 0.0 : set.offset_of(value_of(best), reference);
+        const int over = record.key == kNothing || (infinite && record.key != kInfinity) ? 63 : (int)fmin(plan.offset - record.offset, 63.0);
         if (plan.way == kDone) {
-            const uint64_t mine = scaled(record.sum, scale);
+            const uint64_t mine = record.sum >> over;
             uint64_t total;
             const uint64_t up = block_before(s, mine, total), goal = set.goal(total);
-            if (up <= goal && goal < up + mine) {
-                const uint64_t within = (uint64_t)((double)(goal - up) / scale);
-                s.digit = threadIdx.x, s.before = within < record.sum ? within : record.sum - 1;
-                s.scales[0] = (double)total / scale, s.base = record.key;
-            }
+            if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = (goal - up) << over, s.base = record.key, s.ranges[0] = over, s.found = __builtin_bit_cast(uint64_t, record.offset);
             __syncthreads();
-            const Weights own = set.weights(p, value_of(s.base));
-            choose_in_chunk(s, p, r, row, (int)s.digit, s.before, s.scales[0], [&](float v, int) { return own.of(own.log2_of(v)); });
-        } else {
+            const Weights own = set.weights(p, value_of(s.base), reference, __builtin_bit_cast(double, s.found));
+            choose_in_chunk(s, p, r, row, (int)s.digit, s.before, __builtin_ldexp((double)total, s.ranges[0]), [&](float v, int) { return own.of(own.log2_of(v)); });
+        } else if (plan.way != kMinP) {
             // The bin that the cut lies in, and what lies before it.
-            if ((int)threadIdx.x < p.chunks + kAhead) s.scales[threadIdx.x] = scale, s.ranges[threadIdx.x] = has ? record.low | record.high << 16 : 0;
+            if ((int)threadIdx.x < p.chunks + kAhead) s.overs[threadIdx.x] = plan.way == kCount ? 0 : over, s.ranges[threadIdx.x] = has ? record.low | record.high << 16 : 0;
             __syncthreads();
             constexpr int kMine = (kBins + kThreads - 1) / kThreads;  // (Of the last lanes none.)
             uint64_t v[kMine] = {}, sum = 0, total;
@@ -552,12 +559,9 @@ static __device__ __forceinline__ void plan(const Params& p) {
 #pragma unroll
                 for (int a = 0; a < kAhead; ++a) {
                     const int low = s.ranges[c + a] & 0xFFFF, high = s.ranges[c + a] >> 16;
-                    const double by = s.scales[c + a];
+                    const int by = s.overs[c + a];
 #pragma unroll
-                    for (int i = 0; i < kMine; ++i) {
-                        const uint64_t held = first + i >= low && first + i < high ? b[a][i] : 0;  // (What lies outside was not written.)
-                        v[i] += plan.way == kCount ? held : scaled(held, by);
-                    }
+                    for (int i = 0; i < kMine; ++i) v[i] += first + i >= low && first + i < high ? b[a][i] >> by : 0;  // (What lies outside was not written.)
                 }
             }
 #pragma unroll
@@ -686,7 +690,7 @@ static __device__ __forceinline__ void choose(const Params& p) {
     const Way way = (Way)plan->way;
     if (way == kDone) return;
     const Settings set(p, r);
-    Weigh weigh{set.weights(p, value_of(plan->best)), ~0ull, false, false, false};
+    Weigh weigh{set.weights(p, value_of(plan->best), plan->reference, plan->offset), ~0ull, false, false, false};
     const Weights& weights = weigh.weights;
     const uint64_t need = plan->need, ahead = plan->ahead;
     const bool few = plan->few, alone = plan->alone;
@@ -747,6 +751,41 @@ static __device__ __forceinline__ void choose(const Params& p) {
         for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = share_in(p.list + r * p.list_size + i);
     if (has) s.chunks[threadIdx.x] = few || of_row ? 0 : share_in(p.sums + r * p.chunks + threadIdx.x);
     __syncthreads();
+    if (few && !of_row && listed <= kRanked) {
+        // Each lane has a word, and finds by comparing it with all others its places in the order of words and by
+        // number.
+        const bool mine = (int)threadIdx.x < listed;
+        const uint64_t e = mine ? s.list[threadIdx.x] : 0;
+        const double t = mine ? weights.log2_of(value_of_entry(e)) : -2000.0;
+        uint64_t w = mine ? weights.of(t) : 0, all;
+        int rank = 0, place = 0;
+        if (mine) {
+#pragma unroll 8
+            for (int i = 0; i < listed; ++i) {
+                const uint64_t other = s.list[i];
+                rank += other < e;
+                place += (uint32_t)other < (uint32_t)e;
+            }
+        }
+        if (rank >= (int)(ahead + need)) w = 0;  // top-k
+        if (mine) s.bins[rank] = w;
+        __syncthreads();
+        const uint64_t ordered = mine ? s.bins[threadIdx.x] : 0, before = block_before(s, ordered, all);
+        if (mine) s.active[threadIdx.x] = before;
+        __syncthreads();
+        // A word stays for top-p while those before it do not weigh enough.
+        if (mine && (t < weights.low || (set.top_p < 1.0f && s.active[rank] >= share_of(set.top_p, all)))) w = 0;
+        if (mine) s.bins[place] = w;
+        __syncthreads();
+        const uint64_t placed = mine ? s.bins[threadIdx.x] : 0, up = block_before(s, placed, all), goal = set.goal(all);
+        if (mine) s.active[threadIdx.x] = up;
+        __syncthreads();
+        if (mine && s.active[place] <= goal && goal < s.active[place] + w) {
+            gbl(p.c.token)[r] = (int)(uint32_t)e;
+            if (p.c.share) gbl(p.c.share)[r] = (float)((double)w / (double)all);
+        }
+        return;
+    }
     // The searches: the last word that stays, by number for top-k and by weight for top-p; where all words that stay
     // are listed, then the word that the random number falls on, in the order of words.
     const bool complete = few || of_row;  // the list, or the row, holds what lies ahead of the cut's bin too
