@@ -442,15 +442,19 @@ static __device__ __forceinline__ void survey(const Params& p) {
                 if (v > -INFINITY) add(&s.bins[bin_of(v, record.reference)], 1);
             });
         } else {
-            // The weights first, so that their chains of operations run side by side.
-            uint64_t w[kEach<T> * kPer<T>];
-            int n = 0;
-            x.each(row, [&](float v, int) { w[n++] = weights.of(weights.log2_of(v)); });
-            n = 0;
-            x.each(row, [&](float v, int) {
-                if (binned && w[n]) add(&s.bins[bin_of(v, record.reference)], w[n]);
-                sum += w[n++];
-            });
+            // A vector's weights first, so that their chains of operations run side by side.
+#pragma unroll
+            for (int i = 0; i < kEach<T>; ++i) {
+                uint64_t w[kPer<T>];
+#pragma unroll
+                for (int j = 0; j < kPer<T>; ++j) w[j] = weights.of(weights.log2_of(x.x[i][j]));
+#pragma unroll
+                for (int j = 0; j < kPer<T>; ++j) {
+                    sum += w[j];
+                    if (binned && w[j]) add(&s.bins[bin_of(x.x[i][j], record.reference)], w[j]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if (binned) {
             __syncthreads();
@@ -703,7 +707,15 @@ static __device__ __forceinline__ void choose(const Params& p) {
         __syncthreads();
         x.take(row);
         uint64_t sum = 0;
-        if (!few) {
+        if (way == kWeight && set.min_p == 0.0f) {
+            // Survey's histogram has the weights of the bins ahead of the cut's.
+            const Record& record = p.records[r * p.chunks + chunk];
+            const int over = (int)fmin(plan->offset - record.offset, 63.0);
+            const uint64_t* const bins = p.bins + (r * p.chunks + chunk) * kBins;
+            for (int i = record.low + threadIdx.x; i < min(record.high, cut_bin); i += kThreads) sum += gbl(bins)[i];
+            sum = block_sum(s, sum) >> (weights.infinite && record.key != kInfinity ? 63 : over);
+            sum = threadIdx.x == 0 ? sum : 0;
+        } else if (!few) {
             x.each(row, [&](float v, int) {
                 const double t = weights.log2_of(v);
                 const uint64_t w = weights.of(t);
@@ -922,7 +934,7 @@ template <typename T, int THREADS>
 void launch_as(const Params& p, hipStream_t st) {
     const dim3 grid((unsigned)p.c.rows, (unsigned)p.chunks), block(THREADS);
     hipLaunchKernelGGL((survey_kernel<T, THREADS>), grid, block, 0, st, p);
-    hipLaunchKernelGGL((plan_kernel<T, THREADS>), dim3((unsigned)p.c.rows), block, 0, st, p);
+    hipLaunchKernelGGL((plan_kernel<T, kFewThreads>), dim3((unsigned)p.c.rows), dim3(kFewThreads), 0, st, p);
     hipLaunchKernelGGL((choose_kernel<T, THREADS>), grid, block, 0, st, p);
 }
 template <typename T>
