@@ -10,10 +10,8 @@
 // Both kernels read the matrices as they are defined, row by row: the four lanes
 // of a row take 64 consecutive bytes.
 //
-//   few_kernel   up to 64 rows of x: bound by the bytes of W.  A workgroup takes
-//                16 or 32 rows of W whole, its waves the 512-element steps of K in
-//                turn, straight from memory into the matrix cores' registers;
-//                the waves' sums are added in LDS.
+//   few_kernel   up to 16 rows of x: bound by the bytes of W.  A workgroup takes 16 rows
+//                of W whole; the waves' sums are added in LDS.
 //   tile_kernel  more rows: bound by the matrix cores.  Tiles of both matrices go
 //                from memory straight into LDS, in the order in which lanes read
 //                them (no bank conflicts), two steps ahead of the products.
@@ -48,7 +46,10 @@ struct Params {
     void* y;
     int64_t n, m, y_stride, scale_stride;
     uint32_t k, blocks;             // blocks of 32 of a row
-    uint32_t tiles_n, tiles_m;      // tile_kernel
+    // tile_kernel: tiles along both sides, the parts that K is cut into, and the steps of 512 of a part
+    uint32_t tiles_n, tiles_m, parts, part_supers;
+    float* sums;                    // [parts][m][sums_stride], of more than one part
+    int64_t sums_stride;
 };
 
 template <int XF>
@@ -85,105 +86,7 @@ __device__ __forceinline__ void store_outputs(const Params& p, int64_t row, int6
     }
 }
 
-// ------------------------------------------------------------ up to 64 rows
-
-// TN tiles of 16 rows of W and TM of x to a workgroup of up to WAVES waves.
-template <typename T, int XF, int TN, int TM, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void few_kernel(const Params p) {
-    __shared__ float4v sums[WAVES][TN * TM][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
-    const int r = lane % 16, q = lane / 16;
-    const int64_t n0 = (int64_t)blockIdx.x * (TN * 16);
-    const uint8_t *w[TN], *ws[TN], *x[TM], *xs[TM];
-    // Rows past the end stand in for the last one: every output has sums of its own.
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-        const int64_t row = std::min(n0 + i * 16 + r, p.n - 1);
-        w[i] = p.w_codes + row * (p.k / 2);
-        ws[i] = p.w_scales + row * p.scale_stride;
-    }
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-        const int64_t row = std::min((int64_t)(j * 16 + r), p.m - 1);
-        x[j] = p.x_codes + row * (XF == WQ_MX_FP8 ? p.k : p.k / 2);
-        xs[j] = p.x_scales + row * p.scale_stride;
-    }
-    float4v acc[TN][TM] = {};
-    const uint32_t supers = (p.blocks + 15) / 16;
-    for (uint32_t s = wave; s < supers; s += waves) {
-        const uint32_t left = p.blocks - s * 16;
-        u32x4 sw[TN], sx[TM], wv[kSteps][TN];
-        Piece<XF> xv[kSteps][TM];
-#pragma unroll
-        for (int i = 0; i < TN; ++i) sw[i] = *gbl(reinterpret_cast<const u32x4*>(ws[i] + s * 16));
-#pragma unroll
-        for (int j = 0; j < TM; ++j) sx[j] = *gbl(reinterpret_cast<const u32x4*>(xs[j] + s * 16));
-        if (left >= 16) {
-#pragma unroll
-            for (int t = 0; t < kSteps; ++t) {
-                const uint32_t e = s * kSuper + t * kStep;
-#pragma unroll
-                for (int i = 0; i < TN; ++i) wv[t][i] = *gbl(reinterpret_cast<const u32x4*>(w[i] + (e / 2 + q * 16)));
-#pragma unroll
-                for (int j = 0; j < TM; ++j) {
-                    if constexpr (XF == WQ_MX_FP8) {
-                        xv[t][j].v[0] = *gbl(reinterpret_cast<const u32x4*>(x[j] + (e + q * 16)));
-                        xv[t][j].v[1] = *gbl(reinterpret_cast<const u32x4*>(x[j] + (e + 64 + q * 16)));
-                    } else {
-                        xv[t][j].v[0] = *gbl(reinterpret_cast<const u32x4*>(x[j] + (e / 2 + q * 16)));
-                    }
-                }
-            }
-        } else {
-            // The last blocks of a row: what lies past them counts as zeros under a scale of 1, and
-            // is read from the last block instead.
-            const u32x4 zero = {0, 0, 0, 0};
-            auto masked = [&](const uint8_t* row, uint32_t block, uint32_t at, uint32_t bytes) {
-                const uint32_t b = block < left ? block : left - 1;
-                const u32x4 v = *gbl(reinterpret_cast<const u32x4*>(row + (s * 16 + b) * bytes + at));
-                return block < left ? v : zero;
-            };
-#pragma unroll
-            for (int t = 0; t < kSteps; ++t) {
-#pragma unroll
-                for (int i = 0; i < TN; ++i) wv[t][i] = masked(w[i], t * 4 + q, 0, 16);
-#pragma unroll
-                for (int j = 0; j < TM; ++j) {
-                    if constexpr (XF == WQ_MX_FP8) {
-                        xv[t][j].v[0] = masked(x[j], t * 4 + q / 2, q % 2 * 16, 32);
-                        xv[t][j].v[1] = masked(x[j], t * 4 + 2 + q / 2, q % 2 * 16, 32);
-                    } else {
-                        xv[t][j].v[0] = masked(x[j], t * 4 + q, 0, 16);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < TN; ++i) sw[i][t] = t * 4 + q < left ? sw[i][t] : kOne << q * 8;
-#pragma unroll
-                for (int j = 0; j < TM; ++j) sx[j][t] = t * 4 + q < left ? sx[j][t] : kOne << q * 8;
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < kSteps; ++t)
-#pragma unroll
-            for (int i = 0; i < TN; ++i)
-#pragma unroll
-                for (int j = 0; j < TM; ++j) acc[i][j] = mma<XF, 0, 0>(wv[t][i], xv[t][j], acc[i][j], sw[i][t] >> q * 8, sx[j][t] >> q * 8);
-    }
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j) sums[wave][i * TM + j][lane] = acc[i][j];
-    __syncthreads();
-    const bool vector = p.y_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 8 == 0;
-    for (int o = wave; o < TN * TM; o += waves) {
-        float4v v = sums[0][o][lane];
-        for (int i = 1; i < waves; ++i) v += sums[i][o][lane];
-        const int64_t row = o % TM * 16 + r, col = n0 + o / TM * 16 + q * 4;
-        if (row < p.m && col < p.n) store_outputs<T>(p, row, col, v, vector && col + 4 <= p.n);
-    }
-}
-
-// ----------------------------------------------------------------- tiles
+// --------------------------------------------------------- LDS and loads
 
 template <typename V>
 __device__ __forceinline__ V lds_read(uint32_t addr) {
@@ -222,6 +125,87 @@ __device__ __forceinline__ void turn_over() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
+// ------------------------------------------------------------ up to 16 rows
+
+// 16 rows of W to a workgroup of up to kFewWaves waves, which take the 512-element
+// steps of K in turn.  W goes from memory into the registers in the matrix cores'
+// order, 16 rows of 64 bytes a load.  x goes through LDS, in whole rows: loads in the
+// matrix cores' order cost a look-up of the cache for each lane, three of them (W, two
+// of x) for 1 KB of W, which bounded one token at 4.2 TB/s.  In LDS a row's pieces of 16
+// bytes lie in an order of its own, for the banks.
+constexpr int kFewWaves = 8;
+
+template <typename T, int XF, int ROWS>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Params p) {
+    constexpr int kXStep = XF == WQ_MX_FP8 ? 512 : 256, kPieces = kXStep / 16;  // bytes and pieces of a row of x in a step
+    constexpr int kLoadRows = 64 / kPieces, kLoads = (ROWS + kLoadRows - 1) / kLoadRows;
+    __shared__ union {
+        uint8_t x[kFewWaves][kLoads * 1024];
+        float4v sums[kFewWaves][64];
+    } s;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
+    const uint32_t r = lane % 16, q = lane / 16;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const uint32_t x_row = XF == WQ_MX_FP8 ? p.k : p.k / 2;
+    // Rows past the end stand in for the last one: every output has sums of its own.
+    const int64_t w_index = std::min(n0 + r, p.n - 1);
+    const uint32_t x_last = (uint32_t)p.m - 1, x_index = std::min(r, x_last);
+    const uint8_t* const w = p.w_codes + w_index * (p.k / 2) + q * 16;
+    const uint8_t* const ws = p.w_scales + w_index * p.scale_stride;
+    const uint8_t* const xs = p.x_scales + x_index * p.scale_stride;
+    const uint32_t lds = (uint32_t)(size_t)(lds_u8*)s.x[wave];
+    float4v acc = {0, 0, 0, 0};
+    const uint32_t supers = (p.blocks + 15) / 16;
+    for (uint32_t super = wave; super < supers; super += waves) {
+        const uint32_t left = p.blocks - super * 16;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's reads of its last step are done
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            // Rows and pieces that there are not are not read.
+            const uint32_t row = i * kLoadRows + lane / kPieces, piece = lane % kPieces ^ row % kPieces;
+            const uint8_t* const at = p.x_codes + (int64_t)std::min(row, x_last) * x_row + super * kXStep + piece * 16;
+            dma16((XF == WQ_MX_FP8 ? piece / 2 : piece) < left ? at : kZeros, lds + i * 1024);
+        }
+        u32x4 sw = *gbl(reinterpret_cast<const u32x4*>(ws + super * 16)), sx = *gbl(reinterpret_cast<const u32x4*>(xs + super * 16)), wv[kSteps];
+        if (left >= 16) {
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) wv[t] = *gbl(reinterpret_cast<const u32x4*>(w + (super * (kSuper / 2) + t * (kStep / 2))));
+        } else {
+            // The last blocks of a row: what lies past them counts as zeros under a scale of 1, and is read from the
+            // last block instead.
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+                const uint32_t block = t * 4 + q;
+                const u32x4 v = *gbl(reinterpret_cast<const u32x4*>(w - q * 16 + (super * 16 + std::min(block, left - 1)) * 16));
+                wv[t] = block < left ? v : u32x4{0, 0, 0, 0};
+                sw[t] = block < left ? sw[t] : kOne << q * 8;
+                sx[t] = block < left ? sx[t] : kOne << q * 8;
+            }
+        }
+        wait_vector<0>();
+        const uint32_t at = lds + x_index * kXStep;
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+            Piece<XF> xv;
+#pragma unroll
+            for (int h = 0; h < Piece<XF>::kRegs; ++h) xv.v[h] = lds_read<u32x4>(at + ((t * 4 * Piece<XF>::kRegs + h * 4 + q) ^ x_index % kPieces) * 16);
+            acc = mma<XF, 0, 0>(wv[t], xv, acc, sw[t] >> q * 8, sx[t] >> q * 8);
+        }
+    }
+    __syncthreads();
+    s.sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0) {
+        float4v v = s.sums[0][lane];
+        for (uint32_t i = 1; i < waves; ++i) v += s.sums[i][lane];
+        const int64_t col = n0 + q * 4;
+        const bool vector = p.y_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 8 == 0;
+        if (r < p.m && col < p.n) store_outputs<T>(p, r, col, v, vector && col + 4 <= p.n);
+    }
+}
+
+// ----------------------------------------------------------------- tiles
+
 template <int N, typename F>
 __device__ __forceinline__ void unrolled(F f) {
     if constexpr (N > 0) {
@@ -296,16 +280,17 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     const uint32_t r = lane % 16, q = lane / 16;
     const uint32_t wm = wave % S::WM, wn = wave / S::WM;
     const uint32_t x_row = XF == WQ_MX_FP8 ? p.k : p.k / 2, w_row = p.k / 2;
-    const uint32_t steps = (p.blocks + 3) / 4, supers = (p.blocks + 15) / 16, last = p.blocks % 4;
-    Order order(p.tiles_n * p.tiles_m);
+    Order order(p.tiles_n * p.tiles_m * p.parts);
     if (order.at >= order.end) return;
 
-    // What is being loaded: tile `order.at`, step `load_step` of it, into stage `load_slot`.
+    // What is being loaded: item `order.at` (a tile, a part of K), step `load_step` of it, into stage `load_slot`.
     const uint8_t *w_base, *x_base, *scale_base;
-    uint32_t most_n, most_m, scale_most, load_step = 0, load_slot = 0;
+    uint32_t most_n, most_m, scale_most, load_steps, load_last, load_step = 0, load_slot = 0;
     constexpr uint32_t kScaleLoads = (S::BM + S::BN) / 64;
-    auto tile_rows = [&](uint32_t tile, int64_t& m0, int64_t& n0) {
-        const uint32_t band = 8 * p.tiles_n, first = tile / band * 8, high = std::min(p.tiles_m - first, 8u), in = tile % band;
+    // Blocks of 32 of an item.
+    auto part_blocks = [&](uint32_t item) { return std::min(p.blocks - item % p.parts * p.part_supers * 16, p.part_supers * 16); };
+    auto tile_rows = [&](uint32_t item, int64_t& m0, int64_t& n0) {
+        const uint32_t tile = item / p.parts, band = 8 * p.tiles_n, first = tile / band * 8, high = std::min(p.tiles_m - first, 8u), in = tile % band;
         m0 = (int64_t)(first + in % high) * S::BM;
         n0 = (int64_t)(in / high) * S::BN;
     };
@@ -314,11 +299,14 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         tile_rows(order.at, m0, n0);
         most_m = (uint32_t)std::min<int64_t>(p.m - m0, S::BM) - 1;
         most_n = (uint32_t)std::min<int64_t>(p.n - n0, S::BN) - 1;
-        w_base = p.w_codes + n0 * w_row;
-        x_base = p.x_codes + m0 * x_row;
+        const uint32_t first = order.at % p.parts * p.part_supers, blocks = part_blocks(order.at);
+        w_base = p.w_codes + n0 * w_row + first * (kSuper / 2);
+        x_base = p.x_codes + m0 * x_row + first * (kSteps * S::kXRow);
+        load_steps = (blocks + 3) / 4;
+        load_last = blocks % 4;
         // Scales: 64 rows to a wave, those of W first.
         const bool of_w = wave * 64 < S::BN;
-        scale_base = of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride;
+        scale_base = (of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride) + first * 16;
         scale_most = of_w ? most_n : most_m;
     };
     const uint32_t w_first = wave * S::kWLoads * Places<64>::kRows + lane / 4, w_piece = lane % 4 ^ Places<64>::turn(lane / 4);
@@ -332,7 +320,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     auto load_stage = [&]() -> bool {
         if (order.at >= order.end) return false;
         const uint32_t w_to = lds + load_slot * S::kStage + wave * (S::kWLoads * 1024), x_to = lds + load_slot * S::kStage + S::kWBytes + wave * (S::kXLoads * 1024);
-        if (last == 0 || load_step + 1 < steps) {
+        if (load_last == 0 || load_step + 1 < load_steps) {
 #pragma unroll
             for (int i = 0; i < S::kWLoads; ++i) dma16(w_base, w_offset(i), w_to + i * 1024);
 #pragma unroll
@@ -340,14 +328,14 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         } else {
             // The last blocks of a row: what lies past them counts as zeros, and is not read.
 #pragma unroll
-            for (int i = 0; i < S::kWLoads; ++i) dma16(w_piece < last ? w_base + w_offset(i) : kZeros, w_to + i * 1024);
+            for (int i = 0; i < S::kWLoads; ++i) dma16(w_piece < load_last ? w_base + w_offset(i) : kZeros, w_to + i * 1024);
 #pragma unroll
-            for (int i = 0; i < S::kXLoads; ++i) dma16(x_turned(i) / S::kXRegs < last ? x_base + x_offset(i) : kZeros, x_to + i * 1024);
+            for (int i = 0; i < S::kXLoads; ++i) dma16(x_turned(i) / S::kXRegs < load_last ? x_base + x_offset(i) : kZeros, x_to + i * 1024);
         }
         w_base += 64;
         x_base += S::kXRow;
         load_slot = load_slot + 1 == S::kStages ? 0 : load_slot + 1;
-        if (++load_step == steps) {
+        if (++load_step == load_steps) {
             load_step = 0;
             order.at += order.by;
             if (order.at < order.end) aim();
@@ -391,7 +379,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     load_stage();
     load_stage();
     wait_vector<0>();
-    turn_scales(p.blocks, 0);
+    turn_scales(part_blocks(tile), 0);
     turn_over();
     if (S::kTurns && wave >= S::kWaves / 2) turn_over();
 
@@ -402,7 +390,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     const uint32_t sw_at = S::kScaleAt + wn * S::FN * 256 + r * 16 + q * 4, sx_at = S::kScaleAt + S::BN * 16 + wm * S::FM * 256 + r * 16 + q * 4;
 
     for (;;) {
-        const uint32_t next = tile + order.by;
+        const uint32_t next = tile + order.by, blocks = part_blocks(tile), steps = (blocks + 3) / 4, supers = (blocks + 15) / 16;
         float4v acc[S::FN][S::FM] = {};
         uint32_t sw[S::FN], sx[S::FM];
         for (uint32_t super = 0; super < supers; ++super) {
@@ -424,7 +412,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                         int64_t m0, n0;
                         tile_rows(next, m0, n0);
                         const bool of_w = wave * 64 < S::BN;
-                        tile_scales = of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride;
+                        tile_scales = (of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride) + next % p.parts * p.part_supers * 16;
                         tile_most = (uint32_t)std::min<int64_t>(of_w ? p.n - n0 : p.m - m0, of_w ? S::BN : S::BM) - 1;
                         load_scales(tile_scales, tile_most, buffer);
                     }
@@ -446,7 +434,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                 if (loaded) wait_vector<S::kLoads>();
                 else wait_vector<0>();
                 const bool turn = t == kSteps - 1 || step + 1 == steps;
-                if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? p.blocks - (super + 1) * 16 : p.blocks, buffer);
+                if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? blocks - (super + 1) * 16 : part_blocks(next), buffer);
                 turn_over();
                 if constexpr (S::kTurns) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -458,6 +446,23 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                     turn_over();
                 }
             });
+        }
+        if (p.parts > 1) {
+            int64_t m0, n0;
+            tile_rows(tile, m0, n0);
+#pragma unroll
+            for (int j = 0; j < S::FM; ++j) {
+                const int64_t row = m0 + (wm * S::FM + j) * 16 + r;
+#pragma unroll
+                for (int i = 0; i < S::FN; ++i) {
+                    const int64_t col = n0 + (wn * S::FN + i) * 16 + q * 4;
+                    if (row < p.m && col < p.sums_stride) *gbl(reinterpret_cast<float4v*>(p.sums + (tile % p.parts * p.m + row) * p.sums_stride + col)) = acc[i][j];
+                }
+            }
+            if constexpr (S::kTurns) turn_over();
+            if (next >= order.end) break;
+            tile = next;
+            continue;
         }
         // The last step's stage is free: the wave's own part of it takes 16 rows of outputs at a time, to be
         // stored in whole rows.  (Nothing is loaded there before this wave itself does.)
@@ -500,49 +505,83 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     if (S::kTurns && wave < S::kWaves / 2) turn_over();  // the second group's last
 }
 
+// The sums of the parts of K, in their order, rounded: four neighbouring outputs to a lane.
+constexpr int kJoinThreads = 256;
+template <typename T>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const Params p) {
+    const int64_t fours = p.sums_stride / 4, at = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+    if (at >= p.m * fours) return;
+    const int64_t row = at / fours, col = at % fours * 4;
+    const float* const from = p.sums + row * p.sums_stride + col;
+    float4v v = {0, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t i = 0; i < p.parts; ++i) v += *gbl(reinterpret_cast<const float4v*>(from + i * p.m * p.sums_stride));
+    store_outputs<T>(p, row, col, v, p.y_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 8 == 0 && col + 4 <= p.n);
+}
+
 // ------------------------------------------------------------------ host
 
-constexpr int64_t kFewRows = 64;
-
-template <typename T, int XF, int TN, int TM, int WAVES>
-void launch_few_as(const Params& p, hipStream_t st) {
-    const int supers = (int)((p.blocks + 15) / 16);
-    // As many waves as take equal numbers of steps.
-    const int rounds = (supers + WAVES - 1) / WAVES, waves = (supers + rounds - 1) / rounds;
-    const dim3 grid((unsigned)((p.n + TN * 16 - 1) / (TN * 16)));
-    hipLaunchKernelGGL((few_kernel<T, XF, TN, TM, WAVES>), grid, dim3(waves * 64), 0, st, p);
-}
+constexpr int64_t kFewRows = 16;
 
 template <typename T, int XF>
 void launch_few(const Params& p, hipStream_t st) {
-    if (p.m <= 16) launch_few_as<T, XF, 1, 1, 8>(p, st);
-    else if (p.m <= 32) launch_few_as<T, XF, 1, 2, 8>(p, st);
-    else if (p.m <= 48) launch_few_as<T, XF, 1, 3, 8>(p, st);
-    else launch_few_as<T, XF, 1, 4, 8>(p, st);
+    const int supers = (int)((p.blocks + 15) / 16);
+    // As many waves as take equal numbers of steps.
+    const int rounds = (supers + kFewWaves - 1) / kFewWaves, waves = (supers + rounds - 1) / rounds;
+    const dim3 grid((unsigned)((p.n + 15) / 16)), block(waves * 64);
+    // (Rows of x that there are not take LDS, and with it waves from the CUs.)
+    if (p.m <= 2) hipLaunchKernelGGL((few_kernel<T, XF, 2>), grid, block, 0, st, p);
+    else if (p.m <= 4) hipLaunchKernelGGL((few_kernel<T, XF, 4>), grid, block, 0, st, p);
+    else if (p.m <= 8) hipLaunchKernelGGL((few_kernel<T, XF, 8>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((few_kernel<T, XF, 16>), grid, block, 0, st, p);
 }
+
+int64_t tiles(int64_t n, int64_t m, int64_t side) { return (n + side - 1) / side * ((m + side - 1) / side); }
+
+// The side of a tile, and how many parts K is cut into.
+struct Cut {
+    int64_t side, parts, part_supers;
+};
+Cut cut_of(int64_t n, int64_t k, int64_t m) {
+    const int64_t supers = (k + kSuper - 1) / kSuper;
+    for (int64_t side : {256, 128})
+        if (tiles(n, m, side) >= 192) return {side, 1, supers};
+    // Few tiles: K is cut, so that there are about two workgroups to a CU, into parts of two steps of 512 at least.
+    const int64_t wanted = std::max<int64_t>(1, std::min(supers / 2, 512 / tiles(n, m, 64))), each = (supers + wanted - 1) / wanted;
+    return {64, (supers + each - 1) / each, each};
+}
+
+int64_t sums_stride(int64_t n) { return (n + 3) / 4 * 4; }
 
 template <typename T, int XF, typename S>
 void launch_tiles_as(Params p, hipStream_t st) {
     p.tiles_n = (uint32_t)((p.n + S::BN - 1) / S::BN);
     p.tiles_m = (uint32_t)((p.m + S::BM - 1) / S::BM);
     // As many workgroups as fit the CUs, a multiple of the XCDs.
-    const uint32_t all = p.tiles_n * p.tiles_m, most = 256u * std::min(S::kPerCu, 4), grid = std::min((all + 7) / 8 * 8, most);
+    const uint32_t all = p.tiles_n * p.tiles_m * p.parts, most = 256u * std::min(S::kPerCu, 4), grid = std::min((all + 7) / 8 * 8, most);
     hipLaunchKernelGGL((tile_kernel<T, XF, S>), dim3(grid), dim3(S::kWaves * 64), 0, st, p);
+    if (p.parts > 1) {
+        const int64_t fours = p.m * (p.sums_stride / 4);
+        hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)((fours + kJoinThreads - 1) / kJoinThreads)), dim3(kJoinThreads), 0, st, p);
+    }
 }
 
-int64_t tiles(int64_t n, int64_t m, int64_t bn, int64_t bm) { return (n + bn - 1) / bn * ((m + bm - 1) / bm); }
-
 template <typename T, int XF>
-void launch_tiles(const Params& p, hipStream_t st) {
-    if (tiles(p.n, p.m, 256, 256) >= 192) launch_tiles_as<T, XF, Shape<XF, 256, 256, 4, 2>>(p, st);
-    else if (tiles(p.n, p.m, 128, 128) >= 192) launch_tiles_as<T, XF, Shape<XF, 128, 128, 2, 2>>(p, st);
+void launch_tiles(Params p, float* sums, hipStream_t st) {
+    const Cut cut = cut_of(p.n, p.k, p.m);
+    p.parts = (uint32_t)cut.parts;
+    p.part_supers = (uint32_t)cut.part_supers;
+    p.sums = sums;
+    p.sums_stride = sums_stride(p.n);
+    if (cut.side == 256) launch_tiles_as<T, XF, Shape<XF, 256, 256, 4, 2>>(p, st);
+    else if (cut.side == 128) launch_tiles_as<T, XF, Shape<XF, 128, 128, 2, 2>>(p, st);
     else launch_tiles_as<T, XF, Shape<XF, 64, 64, 2, 2>>(p, st);
 }
 
 template <typename T, int XF>
-void launch(const Params& p, hipStream_t st) {
+void launch(const Params& p, float* sums, hipStream_t st) {
     if (p.m <= kFewRows) launch_few<T, XF>(p, st);
-    else launch_tiles<T, XF>(p, st);
+    else launch_tiles<T, XF>(p, sums, st);
 }
 
 wq_status check_sizes(const char* fn, int64_t n, int64_t k, int64_t m, int64_t x_format) {
@@ -555,7 +594,11 @@ wq_status check_sizes(const char* fn, int64_t n, int64_t k, int64_t m, int64_t x
     return WQ_OK;
 }
 
-size_t workspace_of(int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t workspace_of(int64_t n, int64_t k, int64_t m) {
+    if (m <= kFewRows) return 0;
+    const Cut cut = cut_of(n, k, m);
+    return cut.parts > 1 ? (size_t)(cut.parts * m * sums_stride(n) * 4) : 0;
+}
 
 }  // namespace
 }  // namespace mxl
@@ -569,7 +612,7 @@ wq_status wq_mx_linear_workspace_size(int64_t N, int64_t K, int64_t M, int64_t x
     static const char* fn = "wq_mx_linear_workspace_size";
     if (!bytes) return err(WQ_ERR_INVALID_ARG, "%s: null output pointer", fn);
     WQ_TRY(check_sizes(fn, N, K, M, x_format));
-    *bytes = workspace_of(N, K, M, x_format);
+    *bytes = workspace_of(N, K, M);
     return WQ_OK;
 }
 
@@ -584,7 +627,7 @@ wq_status wq_mx_linear(const uint8_t* w_codes, const uint8_t* w_scales, const ui
     for (const void* ptr : {(const void*)w_codes, (const void*)w_scales, (const void*)x_codes, (const void*)x_scales})
         if (!aligned(ptr, 16)) return err(WQ_ERR_MISALIGNED, "%s: codes and scales must be 16-byte aligned", fn);
     if (!aligned(y, 2)) return err(WQ_ERR_MISALIGNED, "%s: y must be aligned to its elements", fn);
-    const size_t ws = workspace_of(N, K, M, x_format);
+    const size_t ws = workspace_of(N, K, M);
     if (ws > 0) {
         if (!workspace || workspace_bytes < ws)
             return err(WQ_ERR_INVALID_ARG, "%s: a workspace of %zu bytes is needed (got %zu)", fn, ws, workspace ? workspace_bytes : (size_t)0);
@@ -597,12 +640,13 @@ wq_status wq_mx_linear(const uint8_t* w_codes, const uint8_t* w_scales, const ui
     for (const Span& s : inputs)
         if (overlaps(s, out) || overlaps(s, work)) return err(WQ_ERR_INVALID_ARG, "%s: y or the workspace overlaps an input", fn);
     if (overlaps(out, work)) return err(WQ_ERR_INVALID_ARG, "%s: y overlaps the workspace", fn);
-    const Params p{w_codes, w_scales, x_codes, x_scales, y, N, M, y_stride, (int64_t)scale_stride, (uint32_t)K, (uint32_t)(K / kBlock), 0, 0};
+    const Params p{w_codes, w_scales, x_codes, x_scales, y, N, M, y_stride, (int64_t)scale_stride, (uint32_t)K, (uint32_t)(K / kBlock), 0, 0, 1, 0, nullptr, 0};
+    float* const sums = static_cast<float*>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     (void)hipGetLastError();
     const bool half = dtype == WQ_DTYPE_F16;
-    if (x_format == WQ_MX_FP8) half ? launch<_Float16, WQ_MX_FP8>(p, st) : launch<__bf16, WQ_MX_FP8>(p, st);
-    else half ? launch<_Float16, WQ_MX_FP4>(p, st) : launch<__bf16, WQ_MX_FP4>(p, st);
+    if (x_format == WQ_MX_FP8) half ? launch<_Float16, WQ_MX_FP8>(p, sums, st) : launch<__bf16, WQ_MX_FP8>(p, sums, st);
+    else half ? launch<_Float16, WQ_MX_FP4>(p, sums, st) : launch<__bf16, WQ_MX_FP4>(p, sums, st);
     return wq::host::hip_result(fn, hipGetLastError());
 }
 
