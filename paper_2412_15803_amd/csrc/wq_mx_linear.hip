@@ -128,76 +128,72 @@ __device__ __forceinline__ void turn_over() {
 // ------------------------------------------------------------ up to 16 rows
 
 // 16 rows of W to a workgroup of up to kFewWaves waves, which take the 512-element
-// steps of K in turn.  W goes from memory into the registers in the matrix cores'
-// order, 16 rows of 64 bytes a load.  x goes through LDS, in whole rows: loads in the
-// matrix cores' order cost a look-up of the cache for each lane, three of them (W, two
-// of x) for 1 KB of W, which bounded one token at 4.2 TB/s.  In LDS a row's pieces of 16
-// bytes lie in an order of its own, for the banks.
-constexpr int kFewWaves = 8;
+// steps of K in turn.  Everything goes through LDS, each wave's own part of it, in whole
+// rows: loads in the matrix cores' order, consecutive lanes on different rows, cost a
+// look-up of the cache for each lane, which bounded one token at 4.2 TB/s (x too in that
+// order) and 5.3 TB/s (W alone).  In LDS a row's pieces of 16 bytes lie in an order of its
+// own, for the banks.
+constexpr int kFewWaves = 16;
+
+template <int XF, int ROWS>
+struct Few {
+    static constexpr int kXStep = XF == WQ_MX_FP8 ? 512 : 256, kPieces = kXStep / 16;  // bytes and pieces of a row of x in a step
+    static constexpr int kLoadRows = 64 / kPieces, kLoads = (ROWS + kLoadRows - 1) / kLoadRows;
+    static constexpr int kXAt = 4096, kScalesAt = kXAt + kLoads * 1024, kBytes = kScalesAt + 512;
+};
 
 template <typename T, int XF, int ROWS>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(const Params p) {
-    constexpr int kXStep = XF == WQ_MX_FP8 ? 512 : 256, kPieces = kXStep / 16;  // bytes and pieces of a row of x in a step
-    constexpr int kLoadRows = 64 / kPieces, kLoads = (ROWS + kLoadRows - 1) / kLoadRows;
-    __shared__ union {
-        uint8_t x[kFewWaves][kLoads * 1024];
-        float4v sums[kFewWaves][64];
-    } s;
+    using F = Few<XF, ROWS>;
+    extern __shared__ __align__(16) uint8_t memory[];  // F::kBytes for every wave
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
     const uint32_t r = lane % 16, q = lane / 16;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const uint32_t x_row = XF == WQ_MX_FP8 ? p.k : p.k / 2;
+    const uint32_t w_row = p.k / 2, x_row = XF == WQ_MX_FP8 ? p.k : p.k / 2;
     // Rows past the end stand in for the last one: every output has sums of its own.
-    const int64_t w_index = std::min(n0 + r, p.n - 1);
-    const uint32_t x_last = (uint32_t)p.m - 1, x_index = std::min(r, x_last);
-    const uint8_t* const w = p.w_codes + w_index * (p.k / 2) + q * 16;
-    const uint8_t* const ws = p.w_scales + w_index * p.scale_stride;
-    const uint8_t* const xs = p.x_scales + x_index * p.scale_stride;
-    const uint32_t lds = (uint32_t)(size_t)(lds_u8*)s.x[wave];
+    const uint32_t w_last = (uint32_t)std::min<int64_t>(p.n - n0, 16) - 1, x_last = (uint32_t)p.m - 1, x_index = std::min(r, x_last);
+    const uint8_t* const w_base = p.w_codes + n0 * w_row;
+    const uint8_t* const scales = lane < 16 ? p.w_scales + (n0 + std::min(lane, w_last)) * p.scale_stride : p.x_scales + x_index * p.scale_stride;
+    const uint32_t lds = (uint32_t)(size_t)(lds_u8*)memory + wave * F::kBytes;
     float4v acc = {0, 0, 0, 0};
     const uint32_t supers = (p.blocks + 15) / 16;
     for (uint32_t super = wave; super < supers; super += waves) {
         const uint32_t left = p.blocks - super * 16;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's reads of its last step are done
+        // Blocks that there are not are not read; their elements are zeros.
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            // Rows and pieces that there are not are not read.
-            const uint32_t row = i * kLoadRows + lane / kPieces, piece = lane % kPieces ^ row % kPieces;
-            const uint8_t* const at = p.x_codes + (int64_t)std::min(row, x_last) * x_row + super * kXStep + piece * 16;
-            dma16((XF == WQ_MX_FP8 ? piece / 2 : piece) < left ? at : kZeros, lds + i * 1024);
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t row = i * 4 + lane / 16, piece = lane % 16 ^ row;
+            dma16(piece < left ? w_base + (std::min(row, w_last) * w_row + super * (kSuper / 2) + piece * 16) : kZeros, lds + i * 1024);
         }
-        u32x4 sw = *gbl(reinterpret_cast<const u32x4*>(ws + super * 16)), sx = *gbl(reinterpret_cast<const u32x4*>(xs + super * 16)), wv[kSteps];
-        if (left >= 16) {
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t) wv[t] = *gbl(reinterpret_cast<const u32x4*>(w + (super * (kSuper / 2) + t * (kStep / 2))));
-        } else {
-            // The last blocks of a row: what lies past them counts as zeros under a scale of 1, and is read from the
-            // last block instead.
-#pragma unroll
-            for (int t = 0; t < kSteps; ++t) {
-                const uint32_t block = t * 4 + q;
-                const u32x4 v = *gbl(reinterpret_cast<const u32x4*>(w - q * 16 + (super * 16 + std::min(block, left - 1)) * 16));
-                wv[t] = block < left ? v : u32x4{0, 0, 0, 0};
-                sw[t] = block < left ? sw[t] : kOne << q * 8;
-                sx[t] = block < left ? sx[t] : kOne << q * 8;
-            }
+        for (uint32_t i = 0; i < F::kLoads; ++i) {
+            const uint32_t row = i * F::kLoadRows + lane / F::kPieces, piece = lane % F::kPieces ^ row % F::kPieces;
+            const uint8_t* const at = p.x_codes + (std::min(row, x_last) * x_row + super * F::kXStep + piece * 16);
+            dma16((XF == WQ_MX_FP8 ? piece / 2 : piece) < left ? at : kZeros, lds + F::kXAt + i * 1024);
         }
+        if (lane < 32) dma16(scales + super * 16, lds + F::kScalesAt);  // of W, then of x
         wait_vector<0>();
-        const uint32_t at = lds + x_index * kXStep;
+        u32x4 sw = lds_read<u32x4>(lds + F::kScalesAt + r * 16), sx = lds_read<u32x4>(lds + F::kScalesAt + 256 + r * 16);
+        const uint32_t w_at = lds + r * 256, x_at = lds + F::kXAt + x_index * F::kXStep;
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
+        for (uint32_t t = 0; t < kSteps; ++t) {
+            const u32x4 wv = lds_read<u32x4>(w_at + ((t * 4 + q) ^ r) * 16);
             Piece<XF> xv;
 #pragma unroll
-            for (int h = 0; h < Piece<XF>::kRegs; ++h) xv.v[h] = lds_read<u32x4>(at + ((t * 4 * Piece<XF>::kRegs + h * 4 + q) ^ x_index % kPieces) * 16);
-            acc = mma<XF, 0, 0>(wv[t], xv, acc, sw[t] >> q * 8, sx[t] >> q * 8);
+            for (uint32_t h = 0; h < Piece<XF>::kRegs; ++h) xv.v[h] = lds_read<u32x4>(x_at + ((t * 4 * Piece<XF>::kRegs + h * 4 + q) ^ x_index % F::kPieces) * 16);
+            // (The scale of blocks that there are not: 1.)
+            const bool held = t * 4 + q < left;
+            acc = mma<XF, 0, 0>(wv, xv, acc, held ? sw[t] >> q * 8 : kOne, held ? sx[t] >> q * 8 : kOne);
         }
     }
     __syncthreads();
-    s.sums[wave][lane] = acc;
+    float4v* const sums = reinterpret_cast<float4v*>(memory);
+    sums[wave * 64 + lane] = acc;
     __syncthreads();
     if (wave == 0) {
-        float4v v = s.sums[0][lane];
-        for (uint32_t i = 1; i < waves; ++i) v += s.sums[i][lane];
+        float4v v = sums[lane];
+        for (uint32_t i = 1; i < waves; ++i) v += sums[i * 64 + lane];
         const int64_t col = n0 + q * 4;
         const bool vector = p.y_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.y) % 8 == 0;
         if (r < p.m && col < p.n) store_outputs<T>(p, r, col, v, vector && col + 4 <= p.n);
@@ -523,17 +519,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Params p) {
 
 constexpr int64_t kFewRows = 16;
 
+template <typename T, int XF, int ROWS>
+void launch_few_as(const Params& p, hipStream_t st) {
+    using F = Few<XF, ROWS>;
+    const int64_t grid = (p.n + 15) / 16;
+    const int supers = (int)((p.blocks + 15) / 16);
+    // As many waves as LDS has room for, three workgroups to a CU where there are more than one, and as take equal
+    // numbers of steps.
+    const int most = std::min(kFewWaves, (grid > 256 ? 53 : 160) * 1024 / F::kBytes), rounds = (supers + most - 1) / most, waves = (supers + rounds - 1) / rounds;
+    hipLaunchKernelGGL((few_kernel<T, XF, ROWS>), dim3((unsigned)grid), dim3(waves * 64), waves * F::kBytes, st, p);
+}
+
 template <typename T, int XF>
 void launch_few(const Params& p, hipStream_t st) {
-    const int supers = (int)((p.blocks + 15) / 16);
-    // As many waves as take equal numbers of steps.
-    const int rounds = (supers + kFewWaves - 1) / kFewWaves, waves = (supers + rounds - 1) / rounds;
-    const dim3 grid((unsigned)((p.n + 15) / 16)), block(waves * 64);
     // (Rows of x that there are not take LDS, and with it waves from the CUs.)
-    if (p.m <= 2) hipLaunchKernelGGL((few_kernel<T, XF, 2>), grid, block, 0, st, p);
-    else if (p.m <= 4) hipLaunchKernelGGL((few_kernel<T, XF, 4>), grid, block, 0, st, p);
-    else if (p.m <= 8) hipLaunchKernelGGL((few_kernel<T, XF, 8>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((few_kernel<T, XF, 16>), grid, block, 0, st, p);
+    if (p.m <= 2) launch_few_as<T, XF, 2>(p, st);
+    else if (p.m <= 4) launch_few_as<T, XF, 4>(p, st);
+    else if (p.m <= 8) launch_few_as<T, XF, 8>(p, st);
+    else launch_few_as<T, XF, 16>(p, st);
 }
 
 int64_t tiles(int64_t n, int64_t m, int64_t side) { return (n + side - 1) / side * ((m + side - 1) / side); }
