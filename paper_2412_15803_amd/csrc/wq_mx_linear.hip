@@ -224,13 +224,13 @@ struct Places {
 };
 
 // How BM rows of x and BN of W are multiplied by WM x WN waves.
-template <int XF, int BM_, int BN_, int WM_, int WN_>
+template <int XF, int BM_, int BN_, int WM_, int WN_, int STAGES>
 struct Shape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kWaves = WM * WN;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // tiles of 16 of a wave
     static constexpr int kXRegs = Piece<XF>::kRegs, kXRow = 64 * kXRegs;
     static constexpr int kWBytes = BN * 64, kXBytes = BM * kXRow;  // of a step
-    static constexpr int kStage = kWBytes + kXBytes, kStages = 3;
+    static constexpr int kStage = kWBytes + kXBytes, kStages = STAGES, kAhead = STAGES - 1;  // loads run kAhead steps ahead of the products
     static constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves, kLoads = kWLoads + kXLoads;  // of a wave
     static constexpr int kScaleBytes = (BM + BN) * 16;  // of kSteps steps
     static constexpr int kScaleAt = kStages * kStage;
@@ -256,8 +256,8 @@ struct Order {
     }
 };
 
-// A workgroup takes tile after tile.  Loads run two steps ahead of the products, into the
-// next tile's first steps too, while a tile's outputs are stored.
+// A workgroup takes tile after tile.  Loads run two or three steps ahead of the products, into
+// the next tile's first steps too, while a tile's outputs are stored.
 //
 // Two waves of a SIMD take turns (kTurns): while those of one group multiply, the
 // others fetch their operands from LDS.  A barrier ends each turn, the second group is
@@ -372,9 +372,11 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     const uint8_t* tile_scales = scale_base;
     uint32_t tile_most = scale_most;
     load_scales(tile_scales, tile_most, 0);
-    load_stage();
-    load_stage();
-    wait_vector<0>();
+    bool loaded = true;
+#pragma unroll
+    for (int i = 0; i < S::kAhead; ++i) loaded = load_stage();
+    if (loaded) wait_vector<(S::kAhead - 1) * S::kLoads>();
+    else wait_vector<0>();
     turn_scales(part_blocks(tile), 0);
     turn_over();
     if (S::kTurns && wave >= S::kWaves / 2) turn_over();
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                         load_scales(tile_scales, tile_most, buffer);
                     }
                 }
-                const bool loaded = load_stage();
+                loaded = load_stage();
                 const uint32_t from = lds + slot * S::kStage, w_from = opaque(from + w_at);
                 slot = slot + 1 == S::kStages ? 0 : slot + 1;
                 Piece<XF> xv[S::FM];
@@ -426,10 +428,12 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                 }
 #pragma unroll
                 for (int i = 0; i < S::FN; ++i) wv[i] = lds_read<u32x4>(w_from + i * 1024);
-                // All but the newest stage have arrived, the scales among them.
-                if (loaded) wait_vector<S::kLoads>();
-                else wait_vector<0>();
+                // The next step's stage has arrived, and before they are turned the scales, which were loaded ahead of the
+                // stages of this super-step.
                 const bool turn = t == kSteps - 1 || step + 1 == steps;
+                if (!loaded) wait_vector<0>();
+                else if (turn) wait_vector<std::min(S::kAhead - 1, t + 1) * S::kLoads>();
+                else wait_vector<(S::kAhead - 1) * S::kLoads>();
                 if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? blocks - (super + 1) * 16 : part_blocks(next), buffer);
                 turn_over();
                 if constexpr (S::kTurns) __builtin_amdgcn_s_setprio(1);
@@ -549,8 +553,10 @@ Cut cut_of(int64_t n, int64_t k, int64_t m) {
     const int64_t supers = (k + kSuper - 1) / kSuper;
     for (int64_t side : {256, 128})
         if (tiles(n, m, side) >= 192) return {side, 1, supers};
-    // Few tiles: K is cut, so that there are about two workgroups to a CU, into parts of two steps of 512 at least.
-    const int64_t wanted = std::max<int64_t>(1, std::min(supers / 2, 512 / tiles(n, m, 64))), each = (supers + wanted - 1) / wanted;
+    // Few tiles: K is cut, so that every CU has a workgroup, into parts of two steps of 512 at least.  (4096 x 14336, 33
+    // rows, 64 tiles: 38.3 us whole, 14.7 in four parts; 4096 x 4096, 100 rows, 128 tiles: 13.2 and 11.9 in two; two to a CU
+    // gain nothing there, and cost 1003 x 2080, 777 rows, 208 tiles, 13.3 us instead of 9.7.)
+    const int64_t wanted = std::max<int64_t>(1, std::min(supers / 2, 256 / tiles(n, m, 64))), each = (supers + wanted - 1) / wanted;
     return {64, (supers + each - 1) / each, each};
 }
 
@@ -576,9 +582,9 @@ void launch_tiles(Params p, float* sums, hipStream_t st) {
     p.part_supers = (uint32_t)cut.part_supers;
     p.sums = sums;
     p.sums_stride = sums_stride(p.n);
-    if (cut.side == 256) launch_tiles_as<T, XF, Shape<XF, 256, 256, 4, 2>>(p, st);
-    else if (cut.side == 128) launch_tiles_as<T, XF, Shape<XF, 128, 128, 2, 2>>(p, st);
-    else launch_tiles_as<T, XF, Shape<XF, 64, 64, 2, 2>>(p, st);
+    if (cut.side == 256) launch_tiles_as<T, XF, Shape<XF, 256, 256, 4, 2, 3>>(p, st);
+    else if (cut.side == 128) launch_tiles_as<T, XF, Shape<XF, 128, 128, 2, 2, 3>>(p, st);
+    else launch_tiles_as<T, XF, Shape<XF, 64, 64, 2, 2, 4>>(p, st);
 }
 
 template <typename T, int XF>

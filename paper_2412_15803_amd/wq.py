@@ -187,13 +187,13 @@ def _check(status: int) -> None:
 # turn them into C values).
 
 _torch = _Tensor = None
-_WORDS = _HALVES = _FLOATS = _INTS = _BYTES = _SCALES = ()
+_WORDS = _HALVES = _FLOATS = _INTS = _BYTES = _CODES = _SCALES = ()
 _DTYPES = {}  # WQ_DTYPE_* of include/wq_logits.h
 _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _Tensor, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _SCALES, _DTYPES, _raw_stream
+    global _torch, _Tensor, _WORDS, _HALVES, _FLOATS, _INTS, _BYTES, _CODES, _SCALES, _DTYPES, _raw_stream
     import torch
 
     _WORDS = (torch.int32, torch.uint32)
@@ -201,6 +201,7 @@ def _load_torch():
     _FLOATS = (torch.float32,)
     _INTS = (torch.int32,)
     _BYTES = (torch.uint8,)
+    _CODES = (torch.uint8, torch.float8_e4m3fn)
     _SCALES = (torch.uint8, torch.float8_e8m0fnu)
     _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
     # The current stream's handle without building a Stream object.
@@ -758,19 +759,17 @@ def mx_empty(rows: int, cols: int, bits: int, device="cuda"):
 def _mx_matrix(codes, scales, names):
     """Addresses of a microscaled matrix's codes and scales, its rows, columns and
     element type."""
+    if isinstance(codes, _Tensor) and isinstance(scales, _Tensor):
+        shape, kind = codes.shape, codes.dtype
+        if len(shape) == 2 and len(scales.shape) == 2:
+            rows, width = shape
+            bits, cols = (MX_FP4, 2 * width) if kind is _torch.uint8 else (MX_FP8, width)
+            return (_dev_tensor(codes, names[0], _CODES, shape), _dev_tensor(scales, names[1], _SCALES, (rows, -(-cols // 512) * 16)), rows, cols, bits)
     for t, name in zip((codes, scales), names):
         if not isinstance(t, _Tensor):
             raise TypeError(f"{name} must be a torch.Tensor")
         if t.dim() != 2:
             raise ValueError(f"{name} must be 2-D (got {t.dim()} dimensions)")
-    rows, width = codes.shape
-    if codes.dtype is _torch.uint8:
-        kinds, bits, cols = _BYTES, MX_FP4, 2 * width
-    else:
-        kinds, bits, cols = (_torch.float8_e4m3fn,), MX_FP8, width
-    pc = _dev_tensor(codes, names[0], kinds, (rows, width))
-    ps = _dev_tensor(scales, names[1], _SCALES, (rows, mx_scale_stride(cols)))
-    return pc, ps, rows, cols, bits
 
 
 def _dtype_of(t, name):
@@ -800,13 +799,19 @@ def mx_dequantize(codes, scales, out, stream=None) -> None:
     _check((_lib or lib()).wq_mx_dequantize(pc, ps, po, rows, cols, os_, bits, kind, _stream(stream, codes)))
 
 
+def mx_linear_workspace_size(n: int, k: int, m: int, x_bits: int) -> int:
+    """Bytes of device workspace wq_mx_linear needs (0: none)."""
+    out = ctypes.c_size_t(0)
+    _check((_lib or lib()).wq_mx_linear_workspace_size(n, k, m, x_bits, ctypes.byref(out)))
+    return out.value
+
+
 def mx_linear_workspace(w_codes, x_codes):
     """A device workspace (uint8 tensor, or None) for mx_linear of these codes."""
     _torch or _load_torch()
     bits = MX_FP4 if x_codes.dtype is _torch.uint8 else MX_FP8
-    n = ctypes.c_size_t(0)
-    _check(lib().wq_mx_linear_workspace_size(w_codes.shape[0], 2 * w_codes.shape[1], x_codes.shape[0], bits, ctypes.byref(n)))
-    return _torch.empty(n.value, dtype=_torch.uint8, device=x_codes.device) if n.value else None
+    n = mx_linear_workspace_size(w_codes.shape[0], 2 * w_codes.shape[1], x_codes.shape[0], bits)
+    return _torch.empty(n, dtype=_torch.uint8, device=x_codes.device) if n else None
 
 
 def mx_linear(w_codes, w_scales, x_codes, x_scales, y, workspace=None, stream=None) -> None:
@@ -823,13 +828,21 @@ def mx_linear(w_codes, w_scales, x_codes, x_scales, y, workspace=None, stream=No
         raise ValueError(f"x has {x_cols} columns, w {k}")
     py, ys = _row_stride(y, "y", (m, n))
     if workspace is None:
-        with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
-            workspace = mx_linear_workspace(w_codes, x_codes)
+        size = mx_linear_workspace_size(n, k, m, x_bits)
+        if size:
+            with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
+                workspace = _torch.empty(size, dtype=_torch.uint8, device=y.device)
     pk, nk = _workspace(workspace, y)
     _check((_lib or lib()).wq_mx_linear(pw, pws, px, pxs, py, n, k, m, ys, x_bits, kind, pk, nk, _stream(stream, y)))
 
 
 # ------------------------------------------------------- residual and norm
+
+def _typed_rows(t, name, dtype, shape):
+    if isinstance(t, _Tensor) and t.dtype is not dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, x {dtype}")
+    return _row_stride(t, name, shape)
+
 
 def add_rmsnorm(x, weight, eps: float, out=None, residual=None, total=None, codes=None, scales=None, stream=None) -> None:
     """The root-mean-square norm of x + residual (or of x) [R, D] times weight [D],
@@ -838,29 +851,25 @@ def add_rmsnorm(x, weight, eps: float, out=None, residual=None, total=None, code
     bf16 or fp32), their rows may lie apart; total and out may be x or residual."""
     _torch or _load_torch()
     kind = _dtype_of(x, "x")
-    if x.dim() != 2:
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2:
         raise ValueError("x must be [R, D]")
-    shape = rows, dim = x.shape
-
-    def matrix(t, name):
-        if t is None:
-            return None, 0
-        if isinstance(t, _Tensor) and t.dtype is not x.dtype:
-            raise TypeError(f"{name} has dtype {t.dtype}, x {x.dtype}")
-        return _row_stride(t, name, shape)
-
-    px, xs = matrix(x, "x")
-    pr, rs = matrix(residual, "residual")
-    pt, ts = matrix(total, "total")
-    po, os_ = matrix(out, "out")
-    pw = _dev_tensor(weight, "weight", (x.dtype,), (dim,))
-    pc = ps = None
-    bits = 0
+    rows, dim = shape
+    px, xs = _row_stride(x, "x", shape)
+    pw = _dev_tensor(weight, "weight", (dtype,), (dim,))
+    pr = pt = po = pc = ps = None
+    rs = ts = os_ = bits = 0
+    if residual is not None:
+        pr, rs = _typed_rows(residual, "residual", dtype, shape)
+    if total is not None:
+        pt, ts = _typed_rows(total, "total", dtype, shape)
+    if out is not None:
+        po, os_ = _typed_rows(out, "out", dtype, shape)
     if codes is not None or scales is not None:
         if codes is None or scales is None:
             raise ValueError("codes and scales go together")
         pc, ps, r, d, bits = _mx_matrix(codes, scales, ("codes", "scales"))
-        if (r, d) != tuple(shape):
+        if r != rows or d != dim:
             raise ValueError(f"codes hold {r} rows of {d}, expected {rows} of {dim}")
     call = WqNormCall(px, pr, pw, pt, po, pc, ps, rows, dim, xs, rs, ts, os_, kind, bits, eps)
     _check((_lib or lib()).wq_add_rmsnorm(ctypes.addressof(call), _stream(stream, x)))
