@@ -468,32 +468,40 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         // stored in whole rows.  (Nothing is loaded there before this wave itself does.)
         int64_t m0, n0;
         tile_rows(tile, m0, n0);
-        const bool vector = p.y_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
         const uint32_t out = lds + (slot == 0 ? S::kStages - 1 : slot - 1) * S::kStage + wave * (S::kWLoads * 1024);
         constexpr uint32_t kRow = S::kOutTiles * 32, kPieces = kRow / 16, kRows = 64 / kPieces;  // bytes and pieces of a row, rows of a store
         typedef T vec4 __attribute__((ext_vector_type(4)));
         typedef T vec8 __attribute__((ext_vector_type(8)));
+        const uint32_t to_row = lane / kPieces, to_piece = lane % kPieces;
+        uint32_t put[S::kOutTiles], get[16 / kRows];
+#pragma unroll
+        for (uint32_t i = 0; i < S::kOutTiles; ++i) put[i] = out + r * kRow + ((i * 2 + q / 2) ^ (r % kPieces)) * 16 + q % 2 * 8;
+#pragma unroll
+        for (uint32_t h = 0; h < 16 / kRows; ++h) get[h] = out + (h * kRows + to_row) * kRow + (to_piece ^ ((h * kRows + to_row) % kPieces)) * 16;
+        const int64_t row0 = m0 + wm * S::FM * 16 + to_row, col0 = n0 + wn * S::FN * 16 + to_piece * 8;
+        T* const y = static_cast<T*>(p.y) + row0 * p.y_stride + col0;
+        // A tile that lies in y whole, in rows of 16 bytes, needs no checks.
+        const bool whole = p.y_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0 && m0 + S::BM <= p.m && n0 + S::BN <= p.n;
 #pragma unroll
         for (int j = 0; j < S::FM; ++j) {
 #pragma unroll
             for (int g = 0; g < S::FN; g += S::kOutTiles) {
 #pragma unroll
-                for (int i = 0; i < S::kOutTiles; ++i)
-                    lds_write(out + r * kRow + ((i * 2 + q / 2) ^ (r % kPieces)) * 16 + q % 2 * 8, __builtin_convertvector(acc[g + i][j], vec4));
+                for (int i = 0; i < S::kOutTiles; ++i) lds_write(put[i], __builtin_convertvector(acc[g + i][j], vec4));
+                u32x4 v[16 / kRows];
 #pragma unroll
-                for (uint32_t h = 0; h < 16 / kRows; ++h) {
-                    const uint32_t at = h * kRows + lane / kPieces, piece = lane % kPieces;
-                    const vec8 v = __builtin_bit_cast(vec8, lds_read<u32x4>(out + at * kRow + (piece ^ (at % kPieces)) * 16));
-                    const int64_t row = m0 + (wm * S::FM + j) * 16 + at, col = n0 + (wn * S::FN + g) * 16 + piece * 8;
-                    if (row < p.m) {
-                        T* const y = static_cast<T*>(p.y) + row * p.y_stride + col;
-                        if (vector && col + 8 <= p.n) {
-                            *gbl(reinterpret_cast<u32x4*>(y)) = __builtin_bit_cast(u32x4, v);
-                        } else {
+                for (uint32_t h = 0; h < 16 / kRows; ++h) v[h] = lds_read<u32x4>(get[h]);
+                if (whole) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (col + e < p.n) gbl(y)[e] = v[e];
-                        }
+                    for (uint32_t h = 0; h < 16 / kRows; ++h) *gbl(reinterpret_cast<u32x4*>(y + (j * 16 + h * kRows) * p.y_stride + g * 16)) = v[h];
+                } else {
+#pragma unroll
+                    for (uint32_t h = 0; h < 16 / kRows; ++h) {
+                        const int64_t row = row0 + j * 16 + h * kRows, col = col0 + g * 16;
+                        const vec8 e = __builtin_bit_cast(vec8, v[h]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (row < p.m && col + i < p.n) gbl(y)[(j * 16 + h * kRows) * p.y_stride + g * 16 + i] = e[i];
                     }
                 }
             }
