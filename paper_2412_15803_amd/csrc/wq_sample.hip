@@ -65,7 +65,7 @@ struct Record {
     uint32_t key;
     int32_t word;
     int32_t low, high;
-    float reference;  // of the row's bins and weights
+    float reference;  // of the row's bins
     int32_t unused;
 };
 // What choose does with a row.
@@ -175,17 +175,18 @@ __device__ __forceinline__ double exp2_of(double t) {
     return __builtin_ldexp(r, (int)n);
 }
 
-// How a row's logits become weights: w = 2^((x - base) log2(e) / temperature - offset), a multiple of exp((x -
-// max x) / temperature) that all of the row's chunks can share, as base and the whole number offset do not need
-// to be the largest logit's; w is at most 1.
+// How a row's logits become weights: w = 2^(x log2(e) / temperature - offset), offset the whole number that
+// brings the largest logit's to (1/2, 1].  So those of a chunk's largest logit and those of the row's differ by
+// a whole power of two.  Formed as 2^((x - top) log2(e) / temperature + rest), top the largest logit, whose own
+// weight takes `rest`: however large logits or small temperatures are, the difference keeps its digits.
 struct Weights {
-    double base, factor, offset;
+    double top, factor, rest;
     double low;      // smallest log2 w that min-p leaves
     double steps;    // 2^s
     bool infinite;   // the largest logit is +infinity
     // log2 w; not below -2000, which weighs nothing, as -infinity does.
     __device__ __forceinline__ double log2_of(float x) const {
-        const double t = x == -INFINITY ? -2000.0 : fmax(fma((double)x - base, factor, -offset), -2000.0);
+        const double t = x == -INFINITY ? -2000.0 : fmax(fma((double)x - top, factor, rest), -2000.0);
         return infinite ? (x == INFINITY ? 0.0 : -2000.0) : t;
     }
     // A whole number of steps, rounded to nearest.  (Below 2^52, adding 2^52 leaves the number in the low bits.)
@@ -224,13 +225,14 @@ struct Settings {
         random = u > 0.0f ? fmin((double)u, 0.99999999999999989) : 0.0;
     }
     // The smallest offset with which no logit up to `top` weighs more than 1.
-    __device__ __forceinline__ double offset_of(float top, float base) const { return ceil(((double)top - base) * (1.44269504088896340736 / temperature)); }
-    __device__ __forceinline__ Weights weights(const Params& p, float top, float base, double offset) const {
+    __device__ __forceinline__ double offset_of(float top) const { return ceil((double)top * (1.44269504088896340736 / temperature)); }
+    __device__ __forceinline__ Weights weights(const Params& p, float top, double offset) const {
         Weights w;
         w.infinite = top == INFINITY;
-        w.base = base;
+        w.top = top;
         w.factor = 1.44269504088896340736 / temperature;
-        w.offset = offset;
+        // (Past 2^52 the product has no fraction left, but then any other logit's weight is 0.)
+        w.rest = fmin(fmax(fma(w.top, w.factor, -offset), -1.0), 0.0);
         w.steps = __builtin_ldexp(1.0, p.weight_bits);
         w.low = min_p > 0.0f ? w.log2_of(top) + log2((double)min_p) : -4000.0;
         return w;
@@ -391,7 +393,9 @@ static __device__ __forceinline__ void block_best(Small& s, uint32_t& key, int& 
     key = (uint32_t)(best >> 32), word = (int)~(uint32_t)best;
 }
 
-// The reference: the largest logit of the row's first vectors, the same for all of its chunks.
+// The reference: the largest logit of the row's first vectors, the same for all of its chunks; 0 where that is no
+// logit that words worth choosing have (the lowest value of a type stands for a mask), as all of those would lie in
+// one bin.
 template <typename T>
 static __device__ __forceinline__ float reference_of(Small& s, const Row<T>& row, u32x4 bits) {
     uint32_t key = kNothing;
@@ -401,7 +405,8 @@ static __device__ __forceinline__ float reference_of(Small& s, const Row<T>& row
 #pragma unroll
     for (int i = 0; i < kPer<T>; ++i) key = max(key, key_of(y[i]));
     block_best(s, key, word);
-    return key == kNothing || key == kInfinity ? 0.0f : value_of(key);
+    const float most = value_of(key);
+    return fabsf(most) < 1024.0f ? most : 0.0f;
 }
 
 // Workgroups of a row are `rows` apart, so that a row's run at the same time.
@@ -434,8 +439,8 @@ static __device__ __forceinline__ void survey(const Params& p) {
     const int64_t at = r * p.chunks + chunk;
     if (!set.greedy && best != kNothing && way != kMinP) {
         const bool infinite = best == kInfinity;
-        record.offset = infinite ? 0.0 : set.offset_of(value_of(best), record.reference);
-        const Weights weights = set.weights(p, value_of(best), record.reference, record.offset);
+        record.offset = infinite ? 0.0 : set.offset_of(value_of(best));
+        const Weights weights = set.weights(p, value_of(best), record.offset);
         uint64_t sum = 0;
         if (way == kCount) {
             x.each(row, [&](float v, int) {
@@ -472,7 +477,8 @@ static __device__ __forceinline__ void survey(const Params& p) {
     if (threadIdx.x == 0) p.records[at] = record;
 }
 
-// The word of a chunk at which the sum of weights passes `goal`.
+// The word of a chunk at which the sum of weights passes `goal`.  Where it does not quite (the chunk's weight was
+// summed from other roundings than these), it is the chunk's best word, which stays if any of the chunk does.
 template <typename T, typename F>
 static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p, int64_t r, const Row<T>& row, int chunk, uint64_t goal, double total, F weight) {
     // Words in their order are vector by vector, and the lanes of a round are consecutive ones.
@@ -500,6 +506,11 @@ static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p
             return;
         }
         goal -= all;
+    }
+    if (threadIdx.x == 0) {
+        const Record& record = p.records[r * p.chunks + chunk];
+        gbl(p.c.token)[r] = record.word;
+        if (p.c.share) gbl(p.c.share)[r] = (float)((double)weight(value_of(record.key), record.word) / total);
     }
 }
 
@@ -534,7 +545,7 @@ static __device__ __forceinline__ void plan(const Params& p) {
         // A chunk's offset differs from the row's by a whole number: by as many bits its weights are too large.  (Where the
         // largest logit is +infinity, only the chunks that have it weigh anything.)
         const bool infinite = best == kInfinity;
-        plan.offset = infinite ? 0.0 : set.offset_of(value_of(best), reference);
+        plan.offset = infinite ? 0.0 : set.offset_of(value_of(best));
         const int over = record.key == kNothing || (infinite && record.key != kInfinity) ? 63 : (int)fmin(plan.offset - record.offset, 63.0);
         if (plan.way == kDone) {
             const uint64_t mine = record.sum >> over;
@@ -542,7 +553,7 @@ static __device__ __forceinline__ void plan(const Params& p) {
             const uint64_t up = block_before(s, mine, total), goal = set.goal(total);
             if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = (goal - up) << over, s.base = record.key, s.ranges[0] = over, s.found = __builtin_bit_cast(uint64_t, record.offset);
             __syncthreads();
-            const Weights own = set.weights(p, value_of(s.base), reference, __builtin_bit_cast(double, s.found));
+            const Weights own = set.weights(p, value_of(s.base), __builtin_bit_cast(double, s.found));
             choose_in_chunk(s, p, r, row, (int)s.digit, s.before, __builtin_ldexp((double)total, s.ranges[0]), [&](float v, int) { return own.of(own.log2_of(v)); });
         } else if (plan.way != kMinP) {
             // The bin that the cut lies in, and what lies before it.
@@ -694,7 +705,7 @@ static __device__ __forceinline__ void choose(const Params& p) {
     const Way way = (Way)plan->way;
     if (way == kDone) return;
     const Settings set(p, r);
-    Weigh weigh{set.weights(p, value_of(plan->best), plan->reference, plan->offset), ~0ull, false, false, false};
+    Weigh weigh{set.weights(p, value_of(plan->best), plan->offset), ~0ull, false, false, false};
     const Weights& weights = weigh.weights;
     const uint64_t need = plan->need, ahead = plan->ahead;
     const bool few = plan->few, alone = plan->alone;
