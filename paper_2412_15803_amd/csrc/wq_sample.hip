@@ -2,25 +2,32 @@
 // top-p, min-p and a given random number.
 //
 // The words that stay are a beginning of the order (logit falling, word rising), so
-// they are told by the last of them, the cut.  Two launches, a workgroup to a chunk of
-// a row in both:
+// they are told by the last of them, the cut.
 //   survey   a workgroup to a chunk of a row, which it reads into registers: the largest
 //            logit, and what the row's settings ask for: the sum of the weights, or a
 //            histogram over the distance from a reference near the row's largest logit
 //            (of counts for top-k, of weights for top-p; bins as fine as 1/64 of the
 //            distance).
-//   plan     a workgroup to a row: adds up the histograms, which tell the bin that the cut
-//            lies in.  Without top-k, top-p and min-p it chooses the word.
-//   choose   a workgroup to a chunk, read again from the caches: lists the words that may
+//   plan     adds up a row's histograms, which tell the bin that the cut lies in.
+//            Without top-k, top-p and min-p it chooses the word.
+//   list     a workgroup to a chunk, read again from the caches: lists the words that may
 //            be the cut; those that surely stay are listed too while they are few, or
-//            else their weights summed.  The last workgroup of the row to be done sorts
-//            the list, finds the cut, the chunk that the random number falls into, and
-//            in it the word.
-// Rows whose list would be too long (thousands of equal logits) are worked out by that
-// workgroup alone, which then looks through the row instead of the list.
+//            else their weights summed.
+//   finish   finds the cut in a row's list, the chunk that the random number falls into,
+//            and in it the word.
+// Few rows take two launches, as launches and waiting bound them: the second has the
+// chunks' workgroups each make the plan for themselves, and the row's last one to be
+// done with its list finish it (1 x 128256: 20.2 us; with a launch for plan 22.6).  In
+// many rows plans by every chunk would read the histograms over and over, and finish,
+// in the last of small workgroups with room for a whole list, kept others from their
+// CUs: each has a launch (256 x 100277 fp32: 114 us; list and finish in one 124).
+// Rows whose list would be too long (thousands of equal logits) are worked out by one
+// workgroup, which then looks through the row instead of the list.
 //
-// A lane takes 8 words of a chunk at once and without branches: what bounds few rows is how
-// long one workgroup takes (loads, then the chain of fp64 operations of a weight).
+// A lane takes its words of a chunk at once and without branches: what bounds few rows is how
+// long one workgroup takes (loads, then the chain of fp64 operations of a weight).  Many rows:
+// survey, half of the time, is the loads, weights (16 us of 55) and LDS atomics (9) in turn;
+// more or fewer waves to a workgroup or to a SIMD were no faster.
 //
 // Weights are formed in fp64 and held as whole multiples of 2^-s: their sums do
 // not depend on the order in which they are added, so atomics may add them.
@@ -48,6 +55,7 @@ using namespace host;
 constexpr int kChunk = 8192;    // words of a chunk
 constexpr int kAbove = 512, kBelow = 1024, kBins = kAbove + kBelow;  // of a histogram, above and below its reference
 constexpr int kList = 4096;     // words that are listed
+constexpr int kStaged = 512;    // of a chunk's that are listed together
 constexpr int kRanked = 256;    // words of a list that are put in order by comparing all with all
 constexpr int kPartBits = 9, kParts = 1 << kPartBits;  // of a list's range
 constexpr int kAhead = 16;      // histograms that are read at once
@@ -68,9 +76,9 @@ struct Record {
     float reference;  // of the row's bins
     int32_t unused;
 };
-// What choose does with a row.
+// What is done with a row.
 enum Way { kDone, kMinP, kCount, kWeight };
-// What plan tells choose, and what choose's workgroups share.
+// What plan tells the others, and what a row's workgroups share.
 struct Plan {
     double offset;              // of the weights
     uint64_t ahead, need;       // words, or weights, before the cut's bin, and of it up to the cut
@@ -154,24 +162,21 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 constexpr uint32_t kNothing = 0x007FFFFFu;  // of -infinity
 constexpr uint32_t kInfinity = 0xFF800000u;  // of +infinity
 
-// 2^t for t <= 0, relative error below 2^-50: a Taylor series in the fraction's
-// logarithm, |f ln 2| <= 0.347, whose first missing term is 0.347^14 / 14!.
+// 2^t for t <= 0, relative error below 2^-50: a polynomial in the fraction, |f| <= 1/2, the Chebyshev series of 2^f
+// cut behind its eleventh term and written in powers of f (2^-51.5 from 2^f, and the roundings).
 __device__ __forceinline__ double exp2_of(double t) {
-    const double n = __builtin_rint(t), y = (t - n) * 0.693147180559945309417;
-    double r = 1.0 / 6227020800.0;
-    r = fma(r, y, 1.0 / 479001600.0);
-    r = fma(r, y, 1.0 / 39916800.0);
-    r = fma(r, y, 1.0 / 3628800.0);
-    r = fma(r, y, 1.0 / 362880.0);
-    r = fma(r, y, 1.0 / 40320.0);
-    r = fma(r, y, 1.0 / 5040.0);
-    r = fma(r, y, 1.0 / 720.0);
-    r = fma(r, y, 1.0 / 120.0);
-    r = fma(r, y, 1.0 / 24.0);
-    r = fma(r, y, 1.0 / 6.0);
-    r = fma(r, y, 0.5);
-    r = fma(r, y, 1.0);
-    r = fma(r, y, 1.0);
+    const double n = __builtin_rint(t), f = t - n;
+    double r = 0x1.e6228bff026d1p-28;
+    r = fma(r, f, 0x1.b675be272450dp-24);
+    r = fma(r, f, 0x1.62bfc2c7ae40ep-20);
+    r = fma(r, f, 0x1.ffcb54047bef3p-17);
+    r = fma(r, f, 0x1.430913112cb56p-13);
+    r = fma(r, f, 0x1.5d87fe9d7afb3p-10);
+    r = fma(r, f, 0x1.3b2ab6fb9f1a3p-7);
+    r = fma(r, f, 0x1.c6b08d703ce43p-5);
+    r = fma(r, f, 0x1.ebfbdff82c5aep-3);
+    r = fma(r, f, 0x1.62e42fefa3a19p-1);
+    r = fma(r, f, 1.0);
     return __builtin_ldexp(r, (int)n);
 }
 
@@ -183,11 +188,11 @@ struct Weights {
     double top, factor, rest;
     double low;      // smallest log2 w that min-p leaves
     double steps;    // 2^s
-    bool infinite;   // the largest logit is +infinity
-    // log2 w; not below -2000, which weighs nothing, as -infinity does.
+    bool infinite;   // the largest logit is +infinity: those that are weigh 1
+    // log2 w; not below -2000, which weighs nothing, as -infinity does.  (So does what is no number: zero times infinity.)
     __device__ __forceinline__ double log2_of(float x) const {
-        const double t = x == -INFINITY ? -2000.0 : fmax(fma((double)x - top, factor, rest), -2000.0);
-        return infinite ? (x == INFINITY ? 0.0 : -2000.0) : t;
+        const double t = fmax(fma((double)x - top, factor, rest), -2000.0);
+        return x == INFINITY ? 0.0 : t;
     }
     // A whole number of steps, rounded to nearest.  (Below 2^52, adding 2^52 leaves the number in the low bits.)
     __device__ __forceinline__ uint64_t of(double log2w) const {
@@ -300,6 +305,17 @@ __device__ __forceinline__ uint64_t scan16(uint64_t v, F f) {  // of 16 lanes
     v = f(v, dpp64<0x112, 0xF>(v));
     v = f(v, dpp64<0x114, 0xF>(v));
     return f(v, dpp64<0x118, 0xF>(v));
+}
+// The largest of each 4 or 16 lanes, in all of them.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_most(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {
+    v = dpp_most<0x4E>(dpp_most<0xB1>(v));  // quad_perm [1,0,3,2], [2,3,0,1]
+    if constexpr (LANES == 16) v = dpp_most<0x140>(dpp_most<0x141>(v));  // row_half_mirror, row_mirror
+    return v;
 }
 template <typename F>
 __device__ __forceinline__ uint64_t scan64(uint64_t v, F f) {
@@ -434,6 +450,7 @@ static __device__ __forceinline__ void survey(const Params& p) {
         word = key > best ? w : word;  // (A lane's words rise.)
         best = max(best, key);
     });
+    const uint32_t own = best;
     block_best(s, best, word);
     Record record{0, 0.0, best, word, 0, 0, reference_of(s, row, ahead), 0};
     const int64_t at = r * p.chunks + chunk;
@@ -443,8 +460,14 @@ static __device__ __forceinline__ void survey(const Params& p) {
         const Weights weights = set.weights(p, value_of(best), record.offset);
         uint64_t sum = 0;
         if (way == kCount) {
+            // Where top_k groups of lanes have a word each that is no smaller than this, smaller ones are not among the
+            // row's first top_k, and not counted.
+            uint32_t least = own;
+            if (set.top_k <= kThreads / 4) least = most_of_lanes<4>(least);
+            if (set.top_k <= kThreads / 16) least = most_of_lanes<16>(least);
+            least = set.top_k <= kThreads ? ~(uint32_t)block_most(s, (uint32_t)~least) : 0;
             x.each(row, [&](float v, int) {
-                if (v > -INFINITY) add(&s.bins[bin_of(v, record.reference)], 1);
+                if (v > -INFINITY && key_of(v) >= least) add(&s.bins[bin_of(v, record.reference)], 1);
             });
         } else {
             // A vector's weights first, so that their chains of operations run side by side.
@@ -474,7 +497,10 @@ static __device__ __forceinline__ void survey(const Params& p) {
             record.sum = block_sum(s, sum);
         }
     }
-    if (threadIdx.x == 0) p.records[at] = record;
+    if (threadIdx.x == 0) {
+        p.records[at] = record;
+        if (chunk == 0) p.plans[r].done = p.plans[r].listed = 0;
+    }
 }
 
 // The word of a chunk at which the sum of weights passes `goal`.  Where it does not quite (the chunk's weight was
@@ -482,11 +508,12 @@ static __device__ __forceinline__ void survey(const Params& p) {
 template <typename T, typename F>
 static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p, int64_t r, const Row<T>& row, int chunk, uint64_t goal, double total, F weight) {
     // Words in their order are vector by vector, and the lanes of a round are consecutive ones.
-#pragma unroll 1
+    const Chunk<T> x(row, chunk);
+#pragma unroll
     for (int i = 0; i < kEach<T>; ++i) {
-        const int v = chunk * kVectors<T> + threadIdx.x + i * kThreads;
+        const int v = x.first + i * kThreads;
         float y[kPer<T>];
-        row.words(v, row.fetch(v), y);
+        row.words(v, x.bits[i], y);
         uint64_t w[kPer<T>], sum = 0, all;
 #pragma unroll
         for (int j = 0; j < kPer<T>; ++j) {
@@ -514,17 +541,15 @@ static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p
     }
 }
 
-// A workgroup to a row.
+struct Survey : Small {  // what plan looks up of the chunks
+    int overs[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+    int ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+};
+
+// What is to be done with a row, by a workgroup whose lanes are at least as many as the chunks.  Rows that need no
+// cut are answered here, where `answers`.
 template <typename T>
-static __device__ __forceinline__ void plan(const Params& p) {
-    __shared__ struct : Small {
-        int overs[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
-        int ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
-    } s;
-    const int64_t r = blockIdx.x;
-    begin(s);
-    const Row<T> row(p, r);
-    const Settings set(p, r);
+static __device__ __forceinline__ Plan plan(Survey& s, const Params& p, int64_t r, const Row<T>& row, const Settings& set, bool answers) {
     // What survey left: thread i has chunk i's.
     const bool has = (int)threadIdx.x < p.chunks;
     Record record{0, 0.0, kNothing, INT32_MAX, 0, 0, 0.0f, 0};
@@ -536,6 +561,7 @@ static __device__ __forceinline__ void plan(const Params& p) {
     Plan plan{};
     plan.best = best, plan.word = word, plan.cut_bin = kBins, plan.reference = reference;
     plan.way = best == kNothing || set.greedy ? kDone : way_of(set);
+    if (plan.way == kDone && !answers) return plan;
     if (best == kNothing || set.greedy) {
         if (threadIdx.x == 0) {
             gbl(p.c.token)[r] = best == kNothing ? -1 : word;
@@ -567,7 +593,9 @@ static __device__ __forceinline__ void plan(const Params& p) {
                 uint64_t b[kAhead][kMine];
 #pragma unroll
                 for (int a = 0; a < kAhead; ++a) {
-                    const uint64_t* const bins = p.bins + (r * p.chunks + min(c + a, p.chunks - 1)) * kBins + min(first, kBins - kMine);
+                    // (Lanes whose bins are empty, and were not written, all read the same ones: most are.)
+                    const int low = s.ranges[c + a] & 0xFFFF, high = s.ranges[c + a] >> 16, from = first + kMine > low && first < high ? first : low;
+                    const uint64_t* const bins = p.bins + (r * p.chunks + min(c + a, p.chunks - 1)) * kBins + min(from, kBins - kMine);
 #pragma unroll
                     for (int i = 0; i < kMine; ++i) b[a][i] = gbl(bins)[i];
                 }
@@ -598,10 +626,22 @@ static __device__ __forceinline__ void plan(const Params& p) {
             }
         }
     }
-    if (threadIdx.x == 0) p.plans[r] = plan;
+    return plan;
 }
 
-struct Choice : Small {
+template <typename T>
+static __device__ __forceinline__ void plan_rows(const Params& p) {
+    __shared__ Survey s;
+    const int64_t r = blockIdx.x;
+    begin(s);
+    const Plan made = plan(s, p, r, Row<T>(p, r), Settings(p, r), true);
+    if (threadIdx.x == 0) p.plans[r] = made;
+}
+
+struct Listing : Small {
+    uint64_t staged[kStaged];
+};
+struct Choice : Survey {
     uint64_t list[kList];
     uint64_t bins[kParts];
     uint64_t active[kRanked];
@@ -627,23 +667,37 @@ static __device__ __forceinline__ void each_number(Choice& s, const Row<T>& row,
 template <typename T>
 static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& row, bool of_row, int listed, uint64_t target, const Weigh& weigh) {
     uint64_t low = 0, high = ~0ull;  // it lies in here
+    const bool all_few = !of_row && listed <= kRanked;
+    bool first = true;
 #pragma unroll 1
     for (;;) {
         uint64_t least = ~0ull, most = 0;
         uint32_t total = listed;
-        const bool all_few = !of_row && listed <= kRanked;
         __syncthreads();
-        if (!all_few) {
+        if (!of_row && !first) {
+            // Those that are left are put together, if they are few.
+            if (threadIdx.x == 0) s.count = 0;
+            __syncthreads();
+            each_number(s, row, of_row, listed, [&](uint64_t e) {
+                if (e < low || e > high) return;
+                const uint32_t at = atomicAdd(&s.count, 1u);
+                if (at < kRanked) s.active[at] = e;
+            });
+            __syncthreads();
+            total = s.count;
+        }
+        if (of_row || total > kRanked) {
             uint32_t left = 0;
             each_number(s, row, of_row, listed, [&](uint64_t e) {
                 if (e >= low && e <= high) least = std::min(least, e), most = std::max(most, e), ++left;
             });
             least = ~block_most(s, ~least);
             most = block_most(s, most);
-            total = (uint32_t)block_sum(s, left);
+            if (of_row) total = (uint32_t)block_sum(s, left);
         }
+        first = false;
         if (total <= kRanked) {
-            if (!all_few) {
+            if (of_row) {
                 if (threadIdx.x == 0) s.count = 0;
                 __syncthreads();
                 each_number(s, row, of_row, listed, [&](uint64_t e) {
@@ -693,81 +747,16 @@ static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& 
     }
 }
 
+// The cut, from the listed words, and the word that the random number falls on.
 template <typename T>
-static __device__ __forceinline__ void choose(const Params& p) {
-    __shared__ Choice s;
-    const int64_t r = blockIdx.x;
-    const int chunk = blockIdx.y;
-    const Row<T> row(p, r);
-    begin(s);
-    Chunk<T> x(row, chunk);
-    Plan* const plan = p.plans + r;
-    const Way way = (Way)plan->way;
-    if (way == kDone) return;
-    const Settings set(p, r);
-    Weigh weigh{set.weights(p, value_of(plan->best), plan->offset), ~0ull, false, false, false};
+static __device__ __forceinline__ void finish(Choice& s, const Params& p, int64_t r, const Row<T>& row, const Settings& set, const Plan& plan) {
+    const Way way = (Way)plan.way;
+    Weigh weigh{set.weights(p, value_of(plan.best), plan.offset), ~0ull, false, false, false};
     const Weights& weights = weigh.weights;
-    const uint64_t need = plan->need, ahead = plan->ahead;
-    const bool few = plan->few, alone = plan->alone;
-    if (alone) {
-        if (chunk != 0) return;
-    } else {
-        const float reference = plan->reference;
-        const int cut_bin = plan->cut_bin;
-        if (threadIdx.x == 0) s.count = 0;
-        __syncthreads();
-        x.take(row);
-        uint64_t sum = 0;
-        if (way == kWeight && set.min_p == 0.0f) {
-            // Survey's histogram has the weights of the bins ahead of the cut's.
-            const Record& record = p.records[r * p.chunks + chunk];
-            const int over = (int)fmin(plan->offset - record.offset, 63.0);
-            const uint64_t* const bins = p.bins + (r * p.chunks + chunk) * kBins;
-            for (int i = record.low + threadIdx.x; i < min(record.high, cut_bin); i += kThreads) sum += gbl(bins)[i];
-            sum = block_sum(s, sum) >> (weights.infinite && record.key != kInfinity ? 63 : over);
-            sum = threadIdx.x == 0 ? sum : 0;
-        } else if (!few) {
-            x.each(row, [&](float v, int) {
-                const double t = weights.log2_of(v);
-                const uint64_t w = weights.of(t);
-                sum += t >= weights.low && (way == kMinP || bin_of(v, reference) < cut_bin) ? w : 0;
-            });
-        }
-        if (way != kMinP) {
-            x.each(row, [&](float v, int w) {
-                const int bin = v > -INFINITY ? bin_of(v, reference) : kBins;
-                if (bin == cut_bin || (few && bin < cut_bin)) {
-                    const uint64_t e = entry_of(key_of(v), w);
-                    const uint32_t at = atomicAdd(&s.count, 1u);
-                    if (at < kList) {
-                        s.list[at] = e;
-                    } else {
-                        const uint32_t to = atomicAdd(&plan->listed, 1u);
-                        if (to < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + to, e);
-                    }
-                }
-            });
-        }
-        if (!few) {
-            sum = block_sum(s, sum);
-            if (threadIdx.x == 0) share_out(p.sums + r * p.chunks + chunk, sum);
-        }
-        __syncthreads();
-        const uint32_t count = std::min<uint32_t>(s.count, kList);
-        if (threadIdx.x == 0 && count) s.base = atomicAdd(&plan->listed, count);
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < count; i += kThreads)
-            if (s.base + i < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + s.base + i, s.list[i]);
-        // The last workgroup of the row goes on.
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave shares has arrived
-        __syncthreads();
-        if (threadIdx.x == 0) s.digit = __hip_atomic_fetch_add(&plan->done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)p.chunks;
-        __syncthreads();
-        if (!s.digit) return;
-        asm volatile("" ::: "memory");
-    }
+    const uint64_t need = plan.need, ahead = plan.ahead;
+    const bool few = plan.few, alone = plan.alone;
     const bool has = (int)threadIdx.x < p.chunks;
-    int listed = alone ? 0 : (int)__hip_atomic_load(&plan->listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    int listed = alone ? 0 : (int)__hip_atomic_load(&p.plans[r].listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool of_row = alone || listed > p.list_size;  // no list, or one that did not hold all
     __syncthreads();
     if (!of_row)
@@ -858,11 +847,19 @@ static __device__ __forceinline__ void choose(const Params& p) {
             if (sum) add(&s.chunks[c], sum);
         }
     } else {
+        // (Lanes add to sums of their own where there is room, not to wait for each other.)
+        const int copies = kParts / p.chunks, copy = threadIdx.x % copies * p.chunks;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
+        __syncthreads();
 #pragma unroll 1
         for (int i = threadIdx.x; i < listed; i += kThreads) {
             const uint64_t w = weigh(s.list[i]);
-            if (w) add(&s.chunks[row.chunk_of((int)(uint32_t)s.list[i])], w);
+            if (w) add(&s.bins[copy + row.chunk_of((int)(uint32_t)s.list[i])], w);
         }
+        __syncthreads();
+        if (has)
+            for (int i = 0; i < copies; ++i) s.chunks[threadIdx.x] += s.bins[i * p.chunks + threadIdx.x];
     }
     __syncthreads();
     const uint64_t mine = has ? s.chunks[threadIdx.x] : 0, up = block_before(s, mine, total), goal = set.goal(total);
@@ -872,6 +869,112 @@ static __device__ __forceinline__ void choose(const Params& p) {
     const uint64_t within = goal - s.before;
     choose_in_chunk(s, p, r, row, target, within, (double)total, [&](float v, int w) { return weigh(entry_of(key_of(v), w)); });
 }
+
+// Lists a chunk's words that may be the cut (all that may stay, where they are few), and sums the weights of those
+// that surely stay.
+template <typename T>
+static __device__ __forceinline__ void list_chunk(Listing& s, const Params& p, int64_t r, int chunk, const Row<T>& row, Chunk<T>& x, const Settings& set, const Plan& plan) {
+    const Way way = (Way)plan.way;
+    const Weights weights = set.weights(p, value_of(plan.best), plan.offset);
+    const float reference = plan.reference;
+    const int cut_bin = plan.cut_bin;
+    const bool few = plan.few;
+    uint32_t* const listed = &p.plans[r].listed;
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    x.take(row);
+    uint64_t sum = 0;
+    if (way == kWeight && set.min_p == 0.0f) {
+        // Survey's histogram has the weights of the bins ahead of the cut's.
+        const Record& record = p.records[r * p.chunks + chunk];
+        const int over = (int)fmin(plan.offset - record.offset, 63.0);
+        const uint64_t* const bins = p.bins + (r * p.chunks + chunk) * kBins;
+        for (int i = record.low + threadIdx.x; i < min(record.high, cut_bin); i += kThreads) sum += gbl(bins)[i];
+        sum = block_sum(s, sum) >> (weights.infinite && record.key != kInfinity ? 63 : over);
+        sum = threadIdx.x == 0 ? sum : 0;
+    } else if (!few) {
+        x.each(row, [&](float v, int) {
+            const double t = weights.log2_of(v);
+            const uint64_t w = weights.of(t);
+            sum += t >= weights.low && (way == kMinP || bin_of(v, reference) < cut_bin) ? w : 0;
+        });
+    }
+    if (way != kMinP) {
+        x.each(row, [&](float v, int w) {
+            const int bin = v > -INFINITY ? bin_of(v, reference) : kBins;
+            if (bin == cut_bin || (few && bin < cut_bin)) {
+                const uint64_t e = entry_of(key_of(v), w);
+                const uint32_t at = atomicAdd(&s.count, 1u);
+                if (at < kStaged) {
+                    s.staged[at] = e;
+                } else {
+                    const uint32_t to = atomicAdd(listed, 1u);
+                    if (to < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + to, e);
+                }
+            }
+        });
+    }
+    if (!few) {
+        sum = block_sum(s, sum);
+        if (threadIdx.x == 0) share_out(p.sums + r * p.chunks + chunk, sum);
+    }
+    __syncthreads();
+    const uint32_t count = std::min<uint32_t>(s.count, kStaged);
+    if (threadIdx.x == 0 && count) s.base = atomicAdd(listed, count);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count; i += kThreads)
+        if (s.base + i < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + s.base + i, s.staged[i]);
+}
+
+// Few rows: a chunk's workgroup makes the row's plan for itself, and the last one of the row to be done goes on.
+template <typename T>
+static __device__ __forceinline__ void choose(const Params& p) {
+    __shared__ struct {
+        Listing listing;
+        Choice choice;
+    } s;
+    const int64_t r = blockIdx.x;
+    const int chunk = blockIdx.y;
+    const Row<T> row(p, r);
+    begin(s.listing);
+    begin(s.choice);
+    Chunk<T> x(row, chunk);
+    const Settings set(p, r);
+    const Plan made = plan(s.choice, p, r, row, set, chunk == 0);
+    if (made.way == kDone || (made.alone && chunk != 0)) return;
+    if (!made.alone) {
+        list_chunk(s.listing, p, r, chunk, row, x, set, made);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave shares has arrived
+        __syncthreads();
+        if (threadIdx.x == 0) s.listing.digit = __hip_atomic_fetch_add(&p.plans[r].done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)p.chunks;
+        __syncthreads();
+        if (!s.listing.digit) return;
+        asm volatile("" ::: "memory");
+    }
+    finish(s.choice, p, r, row, set, made);
+}
+
+// Many rows: a launch each.
+template <typename T>
+static __device__ __forceinline__ void list_chunks(const Params& p) {
+    __shared__ Listing s;
+    const int64_t r = blockIdx.x;
+    const Plan& made = p.plans[r];
+    if (made.way == kDone || made.alone) return;
+    begin(s);
+    const Row<T> row(p, r);
+    Chunk<T> x(row, blockIdx.y);
+    list_chunk(s, p, r, blockIdx.y, row, x, Settings(p, r), made);
+}
+template <typename T>
+static __device__ __forceinline__ void finish_rows(const Params& p) {
+    __shared__ Choice s;
+    const int64_t r = blockIdx.x;
+    const Plan& made = p.plans[r];
+    if (made.way == kDone) return;
+    begin(s);
+    finish(s, p, r, Row<T>(p, r), Settings(p, r), made);
+}
 };
 
 template <typename T, int THREADS>
@@ -880,7 +983,15 @@ __global__ __launch_bounds__(THREADS) void survey_kernel(const Params p) {
 }
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void plan_kernel(const Params p) {
-    Block<THREADS>::template plan<T>(p);
+    Block<THREADS>::template plan_rows<T>(p);
+}
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void list_kernel(const Params p) {
+    Block<THREADS>::template list_chunks<T>(p);
+}
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void finish_kernel(const Params p) {
+    Block<THREADS>::template finish_rows<T>(p);
 }
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void choose_kernel(const Params p) {
@@ -941,17 +1052,18 @@ size_t workspace_of(int64_t rows, int64_t vocab, int64_t dtype) {
     return lay_out(p, nullptr);
 }
 
-template <typename T, int THREADS>
-void launch_as(const Params& p, hipStream_t st) {
-    const dim3 grid((unsigned)p.c.rows, (unsigned)p.chunks), block(THREADS);
-    hipLaunchKernelGGL((survey_kernel<T, THREADS>), grid, block, 0, st, p);
-    hipLaunchKernelGGL((plan_kernel<T, kFewThreads>), dim3((unsigned)p.c.rows), dim3(kFewThreads), 0, st, p);
-    hipLaunchKernelGGL((choose_kernel<T, THREADS>), grid, block, 0, st, p);
-}
 template <typename T>
 void launch(const Params& p, hipStream_t st) {
-    if (p.c.rows * p.chunks < 512) launch_as<T, kFewThreads>(p, st);
-    else launch_as<T, kManyThreads>(p, st);
+    const dim3 rows((unsigned)p.c.rows), chunks((unsigned)p.c.rows, (unsigned)p.chunks), few(kFewThreads), many(kManyThreads);
+    if (p.c.rows * p.chunks < 512) {
+        hipLaunchKernelGGL((survey_kernel<T, kFewThreads>), chunks, few, 0, st, p);
+        hipLaunchKernelGGL((choose_kernel<T, kFewThreads>), chunks, few, 0, st, p);
+    } else {
+        hipLaunchKernelGGL((survey_kernel<T, kManyThreads>), chunks, many, 0, st, p);
+        hipLaunchKernelGGL((plan_kernel<T, kFewThreads>), rows, few, 0, st, p);
+        hipLaunchKernelGGL((list_kernel<T, kManyThreads>), chunks, many, 0, st, p);
+        hipLaunchKernelGGL((finish_kernel<T, kFewThreads>), rows, few, 0, st, p);
+    }
 }
 
 }  // namespace
