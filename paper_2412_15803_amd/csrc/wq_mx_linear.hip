@@ -210,7 +210,7 @@ __device__ __forceinline__ void unrolled(F f) {
     }
 }
 
-// Rows of BYTES (64 or 128) in LDS.  A load fetches them with consecutive lanes on
+// Rows of BYTES (64, 128 or 256) in LDS.  A load fetches them with consecutive lanes on
 // consecutive pieces of 16 bytes of a row, for which the cache looks up a line once;
 // lanes on different rows cost it a look-up each, which bounded the kernel.  A row's
 // pieces lie in an order of its own, so that the same piece of 16 rows comes from all
@@ -219,26 +219,26 @@ __device__ __forceinline__ void unrolled(F f) {
 template <int BYTES>
 struct Places {
     static constexpr uint32_t kPieces = BYTES / 16, kRows = 1024 / BYTES;  // rows of a load
-    static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (BYTES == 64 ? 0u - row / 4 : row / 2) % kPieces; }
+    static __device__ __forceinline__ uint32_t turn(uint32_t row) { return (BYTES == 64 ? 0u - row / 4 : BYTES == 128 ? row / 2 : row) % kPieces; }
     static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece) { return row * BYTES + (piece ^ turn(row)) * 16; }
 };
 
-// How BM rows of x and BN of W are multiplied by WM x WN waves.
-template <int XF, int BM_, int BN_, int WM_, int WN_, int STAGES>
+// How BM rows of x and BN of W are multiplied by WM x WN waves, SUB steps of 128 to a stage.
+template <int XF, int BM_, int BN_, int WM_, int WN_, int SUB, int STAGES>
 struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kWaves = WM * WN;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kWaves = WM * WN, kSub = SUB;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // tiles of 16 of a wave
-    static constexpr int kXRegs = Piece<XF>::kRegs, kXRow = 64 * kXRegs;
-    static constexpr int kWBytes = BN * 64, kXBytes = BM * kXRow;  // of a step
-    static constexpr int kStage = kWBytes + kXBytes, kStages = STAGES, kAhead = STAGES - 1;  // loads run kAhead steps ahead of the products
+    static constexpr int kXRegs = Piece<XF>::kRegs, kWRow = 64 * SUB, kXRow = 64 * kXRegs * SUB, kBlocks = 4 * SUB;  // of a stage
+    static constexpr int kWBytes = BN * kWRow, kXBytes = BM * kXRow;
+    static constexpr int kStage = kWBytes + kXBytes, kStages = STAGES, kAhead = STAGES - 1;  // loads run kAhead stages ahead of the products
     static constexpr int kWLoads = kWBytes / 1024 / kWaves, kXLoads = kXBytes / 1024 / kWaves, kLoads = kWLoads + kXLoads;  // of a wave
-    static constexpr int kScaleBytes = (BM + BN) * 16;  // of kSteps steps
+    static constexpr int kScaleRows = BN + (BM < 64 ? 64 : BM), kScaleBytes = kScaleRows * 16;  // of kSteps steps; 64 rows to a load
     static constexpr int kScaleAt = kStages * kStage;
     static constexpr int kLds = kScaleAt + 2 * kScaleBytes;
     static constexpr bool kTurns = kWaves == 8;  // two waves to a SIMD
     static constexpr int kPerCu = 160 * 1024 / kLds;
     static constexpr int kOutTiles = FN < 4 ? FN : 4;  // tiles of 16 outputs side by side that are stored together
-    static_assert(kWLoads * kWaves * 1024 == kWBytes && kXLoads * kWaves * 1024 == kXBytes && (BM + BN) / 64 <= kWaves && kPerCu >= 1, "");
+    static_assert(kWLoads * kWaves * 1024 == kWBytes && kXLoads * kWaves * 1024 == kXBytes && kScaleRows / 64 <= kWaves && BN % 64 == 0 && kPerCu >= 1, "");
     static_assert(FN % kOutTiles == 0 && kOutTiles * 512 <= kWLoads * 1024, "outputs pass through the wave's own part of a stage");
 };
 
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     // What is being loaded: item `order.at` (a tile, a part of K), step `load_step` of it, into stage `load_slot`.
     const uint8_t *w_base, *x_base, *scale_base;
     uint32_t most_n, most_m, scale_most, load_steps, load_last, load_step = 0, load_slot = 0;
-    constexpr uint32_t kScaleLoads = (S::BM + S::BN) / 64;
+    constexpr uint32_t kScaleLoads = S::kScaleRows / 64;
     // Blocks of 32 of an item.
     auto part_blocks = [&](uint32_t item) { return std::min(p.blocks - item % p.parts * p.part_supers * 16, p.part_supers * 16); };
     auto tile_rows = [&](uint32_t item, int64_t& m0, int64_t& n0) {
@@ -297,22 +297,23 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         most_n = (uint32_t)std::min<int64_t>(p.n - n0, S::BN) - 1;
         const uint32_t first = order.at % p.parts * p.part_supers, blocks = part_blocks(order.at);
         w_base = p.w_codes + n0 * w_row + first * (kSuper / 2);
-        x_base = p.x_codes + m0 * x_row + first * (kSteps * S::kXRow);
-        load_steps = (blocks + 3) / 4;
-        load_last = blocks % 4;
+        x_base = p.x_codes + m0 * x_row + first * (kSteps * 64 * S::kXRegs);
+        load_steps = (blocks + S::kBlocks - 1) / S::kBlocks;
+        load_last = blocks % S::kBlocks;
         // Scales: 64 rows to a wave, those of W first.
         const bool of_w = wave * 64 < S::BN;
         scale_base = (of_w ? p.w_scales + n0 * p.scale_stride : p.x_scales + m0 * p.scale_stride) + first * 16;
         scale_most = of_w ? most_n : most_m;
     };
-    const uint32_t w_first = wave * S::kWLoads * Places<64>::kRows + lane / 4, w_piece = lane % 4 ^ Places<64>::turn(lane / 4);
-    const uint32_t x_first = wave * S::kXLoads * Places<S::kXRow>::kRows + lane / Places<S::kXRow>::kPieces;
-    const uint32_t x_piece = lane % Places<S::kXRow>::kPieces ^ Places<S::kXRow>::turn(x_first);
+    using WPlaces = Places<S::kWRow>;
+    using XPlaces = Places<S::kXRow>;
+    const uint32_t w_first = wave * S::kWLoads * WPlaces::kRows + lane / WPlaces::kPieces, x_first = wave * S::kXLoads * XPlaces::kRows + lane / XPlaces::kPieces;
+    auto w_piece = [&](int i) { return lane % WPlaces::kPieces ^ WPlaces::turn(w_first + i * WPlaces::kRows); };
+    auto x_piece = [&](int i) { return lane % XPlaces::kPieces ^ XPlaces::turn(x_first + i * XPlaces::kRows); };
     // Rows past the end stand in for the last one.
-    auto w_offset = [&](int i) { return __umul24(std::min(w_first + i * Places<64>::kRows, most_n), w_row) + w_piece * 16; };
-    auto x_turned = [&](int i) { return x_piece ^ (S::kXRow == 128 && i % 2 ? 4u : 0u); };  // (Every second load's rows are 8 further on.)
-    auto x_offset = [&](int i) { return __umul24(std::min(x_first + i * Places<S::kXRow>::kRows, most_m), x_row) + x_turned(i) * 16; };
-    // Loads the next step; of the last tile's last one, nothing.
+    auto w_offset = [&](int i) { return __umul24(std::min(w_first + i * WPlaces::kRows, most_n), w_row) + w_piece(i) * 16; };
+    auto x_offset = [&](int i) { return __umul24(std::min(x_first + i * XPlaces::kRows, most_m), x_row) + x_piece(i) * 16; };
+    // Loads the next stage; past the last tile's last one, nothing.
     auto load_stage = [&]() -> bool {
         if (order.at >= order.end) return false;
         const uint32_t w_to = lds + load_slot * S::kStage + wave * (S::kWLoads * 1024), x_to = lds + load_slot * S::kStage + S::kWBytes + wave * (S::kXLoads * 1024);
@@ -324,11 +325,11 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
         } else {
             // The last blocks of a row: what lies past them counts as zeros, and is not read.
 #pragma unroll
-            for (int i = 0; i < S::kWLoads; ++i) dma16(w_piece < load_last ? w_base + w_offset(i) : kZeros, w_to + i * 1024);
+            for (int i = 0; i < S::kWLoads; ++i) dma16(w_piece(i) < load_last ? w_base + w_offset(i) : kZeros, w_to + i * 1024);
 #pragma unroll
-            for (int i = 0; i < S::kXLoads; ++i) dma16(x_turned(i) / S::kXRegs < load_last ? x_base + x_offset(i) : kZeros, x_to + i * 1024);
+            for (int i = 0; i < S::kXLoads; ++i) dma16(x_piece(i) / S::kXRegs < load_last ? x_base + x_offset(i) : kZeros, x_to + i * 1024);
         }
-        w_base += 64;
+        w_base += S::kWRow;
         x_base += S::kXRow;
         load_slot = load_slot + 1 == S::kStages ? 0 : load_slot + 1;
         if (++load_step == load_steps) {
@@ -381,20 +382,23 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
     turn_over();
     if (S::kTurns && wave >= S::kWaves / 2) turn_over();
 
-    const uint32_t w_at = wn * S::FN * 1024 + Places<64>::place(r, q);
-    uint32_t x_at[S::kXRegs];
+    uint32_t w_at[S::kSub], x_at[S::kSub][S::kXRegs];
 #pragma unroll
-    for (int h = 0; h < S::kXRegs; ++h) x_at[h] = S::kWBytes + wm * S::FM * 16 * S::kXRow + Places<S::kXRow>::place(r, h * 4 + q);
+    for (int u = 0; u < S::kSub; ++u) {
+        w_at[u] = wn * S::FN * 16 * S::kWRow + WPlaces::place(r, u * 4 + q);
+#pragma unroll
+        for (int h = 0; h < S::kXRegs; ++h) x_at[u][h] = S::kWBytes + wm * S::FM * 16 * S::kXRow + XPlaces::place(r, (u * S::kXRegs + h) * 4 + q);
+    }
     const uint32_t sw_at = S::kScaleAt + wn * S::FN * 256 + r * 16 + q * 4, sx_at = S::kScaleAt + S::BN * 16 + wm * S::FM * 256 + r * 16 + q * 4;
 
     for (;;) {
-        const uint32_t next = tile + order.by, blocks = part_blocks(tile), steps = (blocks + 3) / 4, supers = (blocks + 15) / 16;
+        const uint32_t next = tile + order.by, blocks = part_blocks(tile), steps = (blocks + S::kBlocks - 1) / S::kBlocks, supers = (blocks + 15) / 16;
         float4v acc[S::FN][S::FM] = {};
         uint32_t sw[S::FN], sx[S::FM];
         for (uint32_t super = 0; super < supers; ++super) {
-            unrolled<kSteps>([&](auto T_) {
+            unrolled<kSteps / S::kSub>([&](auto T_) {
                 constexpr int t = decltype(T_)::value;
-                const uint32_t step = super * kSteps + t;
+                const uint32_t step = super * (kSteps / S::kSub) + t;
                 if (step >= steps) return;
                 if constexpr (t == 0) {
                     const uint32_t from = opaque(lds + buffer * S::kScaleBytes);
@@ -416,31 +420,38 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                     }
                 }
                 loaded = load_stage();
-                const uint32_t from = lds + slot * S::kStage, w_from = opaque(from + w_at);
+                const uint32_t from = lds + slot * S::kStage;
                 slot = slot + 1 == S::kStages ? 0 : slot + 1;
-                Piece<XF> xv[S::FM];
-                u32x4 wv[S::FN];
+                Piece<XF> xv[S::kSub][S::FM];
+                u32x4 wv[S::kSub][S::FN];
 #pragma unroll
-                for (int h = 0; h < S::kXRegs; ++h) {
-                    const uint32_t x_from = opaque(from + x_at[h]);
+                for (int u = 0; u < S::kSub; ++u) {
 #pragma unroll
-                    for (int j = 0; j < S::FM; ++j) xv[j].v[h] = lds_read<u32x4>(x_from + j * 16 * S::kXRow);
+                    for (int h = 0; h < S::kXRegs; ++h) {
+                        const uint32_t x_from = opaque(from + x_at[u][h]);
+#pragma unroll
+                        for (int j = 0; j < S::FM; ++j) xv[u][j].v[h] = lds_read<u32x4>(x_from + j * 16 * S::kXRow);
+                    }
+                    const uint32_t w_from = opaque(from + w_at[u]);
+#pragma unroll
+                    for (int i = 0; i < S::FN; ++i) wv[u][i] = lds_read<u32x4>(w_from + i * 16 * S::kWRow);
                 }
-#pragma unroll
-                for (int i = 0; i < S::FN; ++i) wv[i] = lds_read<u32x4>(w_from + i * 1024);
                 // The next step's stage has arrived, and before they are turned the scales, which were loaded ahead of the
                 // stages of this super-step.
-                const bool turn = t == kSteps - 1 || step + 1 == steps;
+                const bool turn = t == kSteps / S::kSub - 1 || step + 1 == steps;
                 if (!loaded) wait_vector<0>();
                 else if (turn) wait_vector<std::min(S::kAhead - 1, t + 1) * S::kLoads>();
                 else wait_vector<(S::kAhead - 1) * S::kLoads>();
                 if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? blocks - (super + 1) * 16 : part_blocks(next), buffer);
                 turn_over();
                 if constexpr (S::kTurns) __builtin_amdgcn_s_setprio(1);
+unrolled<S::kSub>([&](auto U_) {
+                    constexpr int u = decltype(U_)::value, of = t * S::kSub + u;
 #pragma unroll
-                for (int i = 0; i < S::FN; ++i)
+                    for (int i = 0; i < S::FN; ++i)
 #pragma unroll
-                    for (int j = 0; j < S::FM; ++j) acc[i][j] = mma<XF, t, t>(wv[i], xv[j], acc[i][j], sw[i], sx[j]);
+                        for (int j = 0; j < S::FM; ++j) acc[i][j] = mma<XF, of, of>(wv[u][i], xv[u][j], acc[i][j], sw[i], sx[j]);
+                });
                 if constexpr (S::kTurns) {
                     __builtin_amdgcn_s_setprio(0);
                     turn_over();
@@ -559,11 +570,13 @@ struct Cut {
 };
 Cut cut_of(int64_t n, int64_t k, int64_t m) {
     const int64_t supers = (k + kSuper - 1) / kSuper;
+    // (Where half of a tile's rows or more would be none, smaller ones waste less: 28672 x 4096, 33 rows, tiles of 64
+    // instead of 128: 28 -> 21.8 us.)
     for (int64_t side : {256, 128})
-        if (tiles(n, m, side) >= 192) return {side, 1, supers};
+        if (m > side / 2 && tiles(n, m, side) >= 192) return {side, 1, supers};
     // Few tiles: K is cut, so that every CU has a workgroup, into parts of two steps of 512 at least.  (4096 x 14336, 33
-    // rows, 64 tiles: 38.3 us whole, 14.7 in four parts; 4096 x 4096, 100 rows, 128 tiles: 13.2 and 11.9 in two; two to a CU
-    // gain nothing there, and cost 1003 x 2080, 777 rows, 208 tiles, 13.3 us instead of 9.7.)
+    // rows, 64 tiles: 38.3 us whole, 14.7 in four parts.  Two workgroups to a CU gain nothing there, and cost 4096 x 4096, 100
+    // rows, 128 tiles, 12.9 us instead of 11.8, 1003 x 2080, 777 rows, 208 tiles, 12.9 instead of 9.4.)
     const int64_t wanted = std::max<int64_t>(1, std::min(supers / 2, 256 / tiles(n, m, 64))), each = (supers + wanted - 1) / wanted;
     return {64, (supers + each - 1) / each, each};
 }
@@ -585,14 +598,23 @@ void launch_tiles_as(Params p, hipStream_t st) {
 
 template <typename T, int XF>
 void launch_tiles(Params p, float* sums, hipStream_t st) {
+    // Shorter stages, or more of them, where that is faster.  Two steps of 128 to a stage halve the barriers and fetch
+    // whole lines of the caches (4096 x 14336, 33 rows: 16.8 -> 14.8 us; 300 rows of 4 bits: 48 -> 41); four steps leave
+    // room for fewer workgroups (400 rows: 52 -> 81).  Tiles of 64 that come out at one to a CU have four stages, others
+    // three, with which a CU holds two (4096 x 14336, 200 and 400 rows: 36.7 and 52.6 us with three, 34.3 and 63.9 with
+    // four).  Tiles of 128 with 8 bits have two waves to a SIMD that take turns (1024 rows: 82 -> 70 us; with 4 bits, whose
+    // products take half the time, 55 -> 60).  Tiles of 32 rows: 17 rows 14.8 -> 13.2 us.  Tiles of 256 with 4 bits have
+    // room for a stage more (8192 x 8192 x 8192: 303 -> 294 us).
     const Cut cut = cut_of(p.n, p.k, p.m);
     p.parts = (uint32_t)cut.parts;
     p.part_supers = (uint32_t)cut.part_supers;
     p.sums = sums;
     p.sums_stride = sums_stride(p.n);
-    if (cut.side == 256) launch_tiles_as<T, XF, Shape<XF, 256, 256, 4, 2, 3>>(p, st);
-    else if (cut.side == 128) launch_tiles_as<T, XF, Shape<XF, 128, 128, 2, 2, 3>>(p, st);
-    else launch_tiles_as<T, XF, Shape<XF, 64, 64, 2, 2, 4>>(p, st);
+    if (cut.side == 256) launch_tiles_as<T, XF, Shape<XF, 256, 256, 4, 2, 1, (XF == WQ_MX_FP4 ? 4 : 3)>>(p, st);
+    else if (cut.side == 128) launch_tiles_as<T, XF, Shape<XF, 128, 128, (XF == WQ_MX_FP4 ? 2 : 4), 2, 2, 3>>(p, st);
+    else if (p.m <= 32) launch_tiles_as<T, XF, Shape<XF, 32, 64, 2, 2, 2, 4>>(p, st);
+    else if (tiles(p.n, p.m, 64) * cut.parts <= 256) launch_tiles_as<T, XF, Shape<XF, 64, 64, 2, 2, 2, 4>>(p, st);
+    else launch_tiles_as<T, XF, Shape<XF, 64, 64, 2, 2, 2, 3>>(p, st);
 }
 
 template <typename T, int XF>
