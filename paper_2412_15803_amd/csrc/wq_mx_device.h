@@ -27,19 +27,21 @@ typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 constexpr int kPiece = 8;
 constexpr int kBlock = WQ_MX_BLOCK;
 
-// Eight values as they lie in memory, and as fp32.
+// Eight values as they lie in memory, and as fp32.  load_once leaves no room in the caches to what is not read again.
 template <typename T>
 struct Raw;
 template <>
 struct Raw<_Float16> {
     u32x4 v;
     __device__ __forceinline__ void load(const _Float16* p) { v = *gbl(reinterpret_cast<const u32x4*>(p)); }
+    __device__ __forceinline__ void load_once(const _Float16* p) { v = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(p))); }
     __device__ __forceinline__ float8v f32() const { return __builtin_convertvector(__builtin_bit_cast(half8v, v), float8v); }
 };
 template <>
 struct Raw<__bf16> {
     u32x4 v;
     __device__ __forceinline__ void load(const __bf16* p) { v = *gbl(reinterpret_cast<const u32x4*>(p)); }
+    __device__ __forceinline__ void load_once(const __bf16* p) { v = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(p))); }
     __device__ __forceinline__ float8v f32() const {
         float8v f;
 #pragma unroll
@@ -56,6 +58,10 @@ struct Raw<float> {
     __device__ __forceinline__ void load(const float* p) {
         a = gbl(reinterpret_cast<const u32x4*>(p))[0];
         b = gbl(reinterpret_cast<const u32x4*>(p))[1];
+    }
+    __device__ __forceinline__ void load_once(const float* p) {
+        a = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(p)));
+        b = __builtin_nontemporal_load(gbl(reinterpret_cast<const u32x4*>(p)) + 1);
     }
     __device__ __forceinline__ float8v f32() const {
         const float4v x = __builtin_bit_cast(float4v, a), y = __builtin_bit_cast(float4v, b);
