@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 # The in-tree build.  WQ_LIBRARY names another build of the same library to
 # load instead (the host-sanitizer test loads one built with AddressSanitizer
@@ -94,6 +95,11 @@ class WqNormCall(ctypes.Structure):
 class WqSampleCall(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in ("logits", "random", "temperature", "top_k", "top_p", "min_p", "token", "share")] + [
         (name, ctypes.c_int64) for name in ("rows", "vocab", "logits_stride", "dtype")]
+
+
+# The same two as bytes, which a small call's time allows sooner than a Structure.
+_NORM_CALL = struct.Struct("7Q8qf4x").pack
+_SAMPLE_CALL = struct.Struct("8Q4q").pack
 
 
 class WQError(RuntimeError):
@@ -857,8 +863,7 @@ def add_rmsnorm(x, weight, eps: float, out=None, residual=None, total=None, code
     rows, dim = shape
     px, xs = _row_stride(x, "x", shape)
     pw = _dev_tensor(weight, "weight", (dtype,), (dim,))
-    pr = pt = po = pc = ps = None
-    rs = ts = os_ = bits = 0
+    pr = pt = po = pc = ps = rs = ts = os_ = bits = 0
     if residual is not None:
         pr, rs = _typed_rows(residual, "residual", dtype, shape)
     if total is not None:
@@ -871,8 +876,8 @@ def add_rmsnorm(x, weight, eps: float, out=None, residual=None, total=None, code
         pc, ps, r, d, bits = _mx_matrix(codes, scales, ("codes", "scales"))
         if r != rows or d != dim:
             raise ValueError(f"codes hold {r} rows of {d}, expected {rows} of {dim}")
-    call = WqNormCall(px, pr, pw, pt, po, pc, ps, rows, dim, xs, rs, ts, os_, kind, bits, eps)
-    _check((_lib or lib()).wq_add_rmsnorm(ctypes.addressof(call), _stream(stream, x)))
+    call = _NORM_CALL(px, pr, pw, pt, po, pc, ps, rows, dim, xs, rs, ts, os_, kind, bits, eps)
+    _check((_lib or lib()).wq_add_rmsnorm(call, _stream(stream, x)))
 
 
 # ------------------------------------------------------- the next word by chance
@@ -901,7 +906,7 @@ def sample_logits(logits, random, token, temperature=None, top_k=None, top_p=Non
     px, xs = _row_stride(logits, "logits", logits.shape)
     pr = _dev_tensor(random, "random", _FLOATS, one)
     po = _dev_tensor(token, "token", _INTS, one)
-    pt = pk = pp = pm = psh = None
+    pt = pk = pp = pm = psh = 0
     if temperature is not None:
         pt = _dev_tensor(temperature, "temperature", _FLOATS, one)
     if top_k is not None:
@@ -916,8 +921,8 @@ def sample_logits(logits, random, token, temperature=None, top_k=None, top_p=Non
         with _torch.cuda.stream(stream):  # memory that is `stream`'s (None: the current one's)
             workspace = sample_workspace(logits)
     pw, nw = _workspace(workspace, logits)
-    call = WqSampleCall(px, pr, pt, pk, pp, pm, po, psh, rows, vocab, xs, kind)
-    _check((_lib or lib()).wq_sample_logits(ctypes.addressof(call), pw, nw, _stream(stream, logits)))
+    call = _SAMPLE_CALL(px, pr, pt, pk, pp, pm, po, psh, rows, vocab, xs, kind)
+    _check((_lib or lib()).wq_sample_logits(call, pw, nw, _stream(stream, logits)))
 
 
 # ------------------------------------------------------- measurement probe

@@ -153,3 +153,10 @@ def test_binding_refuses_before_the_library(wq):
         wq.add_rmsnorm(x[0], x[0], 1e-5, out=x[0])
     with pytest.raises(ValueError, match=r"\[R, V\]"):
         wq.sample_logits(x[0], x[0], x[0])
+
+
+def test_packed_calls(wq):
+    """The bytes that the binding passes are those of the structures."""
+    pointers, sizes = list(range(1, 9)), [1 << (4 * i) for i in range(8)]
+    assert wq._NORM_CALL(*pointers[:7], *sizes, 0.5) == bytes(wq.WqNormCall(*pointers[:7], *sizes, 0.5))
+    assert wq._SAMPLE_CALL(*pointers, *sizes[:4]) == bytes(wq.WqSampleCall(*pointers, *sizes[:4]))
