@@ -17,7 +17,7 @@
 //            and in it the word.
 // Few rows take two launches, as launches and waiting bound them: the second has the
 // chunks' workgroups each make the plan for themselves, and the row's last one to be
-// done with its list finish it (1 x 128256: 20.2 us; with a launch for plan 22.6).  In
+// done with its list finish it (1 x 128256, top-k and top-p: 19 us; with a launch for plan 2.4 more).  In
 // many rows plans by every chunk would read the histograms over and over, and finish,
 // in the last of small workgroups with room for a whole list, kept others from their
 // CUs: each has a launch (256 x 100277 fp32: 114 us; list and finish in one 124).
@@ -57,6 +57,7 @@ constexpr int kAbove = 512, kBelow = 1024, kBins = kAbove + kBelow;  // of a his
 constexpr int kList = 4096;     // words that are listed
 constexpr int kStaged = 512;    // of a chunk's that are listed together
 constexpr int kRanked = 256;    // words of a list that are put in order by comparing all with all
+constexpr int kCompared = 64;   // numbers that are searched so, where their weights are read too (237: 15 us; by parts 4)
 constexpr int kPartBits = 9, kParts = 1 << kPartBits;  // of a list's range
 constexpr int kAhead = 16;      // histograms that are read at once
 
@@ -541,9 +542,8 @@ static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p
     }
 }
 
-struct Survey : Small {  // what plan looks up of the chunks
-    int overs[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
-    int ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+struct Survey : Small {  // what plan looks up of the chunks: their bins' first, end and shift
+    uint32_t ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
 };
 
 // What is to be done with a row, by a workgroup whose lanes are at least as many as the chunks.  Rows that need no
@@ -577,32 +577,38 @@ static __device__ __forceinline__ Plan plan(Survey& s, const Params& p, int64_t 
             const uint64_t mine = record.sum >> over;
             uint64_t total;
             const uint64_t up = block_before(s, mine, total), goal = set.goal(total);
-            if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = (goal - up) << over, s.base = record.key, s.ranges[0] = over, s.found = __builtin_bit_cast(uint64_t, record.offset);
+            if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = (goal - up) << over, s.base = record.key, s.ranges[0] = (uint32_t)over, s.found = __builtin_bit_cast(uint64_t, record.offset);
             __syncthreads();
             const Weights own = set.weights(p, value_of(s.base), __builtin_bit_cast(double, s.found));
-            choose_in_chunk(s, p, r, row, (int)s.digit, s.before, __builtin_ldexp((double)total, s.ranges[0]), [&](float v, int) { return own.of(own.log2_of(v)); });
+            choose_in_chunk(s, p, r, row, (int)s.digit, s.before, __builtin_ldexp((double)total, (int)s.ranges[0]), [&](float v, int) { return own.of(own.log2_of(v)); });
         } else if (plan.way != kMinP) {
             // The bin that the cut lies in, and what lies before it.
-            if ((int)threadIdx.x < p.chunks + kAhead) s.overs[threadIdx.x] = plan.way == kCount ? 0 : over, s.ranges[threadIdx.x] = has ? record.low | record.high << 16 : 0;
+            if ((int)threadIdx.x < p.chunks + kAhead)
+                s.ranges[threadIdx.x] = has ? (uint32_t)record.low | (uint32_t)record.high << 11 | (plan.way == kCount ? 0u : (uint32_t)over) << 22 : 0;
             __syncthreads();
-            constexpr int kMine = (kBins + kThreads - 1) / kThreads;  // (Of the last lanes none.)
+            constexpr int kMine = 2;
+            static_assert(kThreads * kMine >= kBins, "(Of the last lanes none.)");
+            typedef uint64_t u64x2 __attribute__((ext_vector_type(kMine)));
             uint64_t v[kMine] = {}, sum = 0, total;
-            const int first = threadIdx.x * kMine;
+            const int first = threadIdx.x * kMine, wave_first = __builtin_amdgcn_readfirstlane(first);
 #pragma unroll 1
             for (int c = 0; c < p.chunks; c += kAhead) {
-                uint64_t b[kAhead][kMine];
+                // (One look into LDS for each wave; its broadcasts for every chunk took longer than the bins.)
+                const uint32_t ranges = s.ranges[c + threadIdx.x % kAhead];
+                u64x2 b[kAhead];
 #pragma unroll
                 for (int a = 0; a < kAhead; ++a) {
-                    // (Lanes whose bins are empty, and were not written, all read the same ones: most are.)
-                    const int low = s.ranges[c + a] & 0xFFFF, high = s.ranges[c + a] >> 16, from = first + kMine > low && first < high ? first : low;
-                    const uint64_t* const bins = p.bins + (r * p.chunks + min(c + a, p.chunks - 1)) * kBins + min(from, kBins - kMine);
-#pragma unroll
-                    for (int i = 0; i < kMine; ++i) b[a][i] = gbl(bins)[i];
+                    // (Most waves have no bin of a chunk that was written, and need no load: those bounded this.)
+                    const uint32_t range = (uint32_t)__builtin_amdgcn_readlane((int)ranges, a);
+                    const int low = range & 0x7FF, high = range >> 11 & 0x7FF;
+                    const uint64_t* const bins = p.bins + (r * p.chunks + c + a) * kBins + min(first, kBins - kMine);
+                    b[a] = u64x2{0, 0};
+                    if (wave_first + 64 * kMine > low && wave_first < high) b[a] = *gbl(reinterpret_cast<const u64x2*>(bins));
                 }
 #pragma unroll
                 for (int a = 0; a < kAhead; ++a) {
-                    const int low = s.ranges[c + a] & 0xFFFF, high = s.ranges[c + a] >> 16;
-                    const int by = s.overs[c + a];
+                    const uint32_t range = (uint32_t)__builtin_amdgcn_readlane((int)ranges, a);
+                    const int low = range & 0x7FF, high = range >> 11 & 0x7FF, by = (int)(range >> 22);
 #pragma unroll
                     for (int i = 0; i < kMine; ++i) v[i] += first + i >= low && first + i < high ? b[a][i] >> by : 0;  // (What lies outside was not written.)
                 }
@@ -667,7 +673,7 @@ static __device__ __forceinline__ void each_number(Choice& s, const Row<T>& row,
 template <typename T>
 static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& row, bool of_row, int listed, uint64_t target, const Weigh& weigh) {
     uint64_t low = 0, high = ~0ull;  // it lies in here
-    const bool all_few = !of_row && listed <= kRanked;
+    const bool all_few = !of_row && listed <= kCompared;
     bool first = true;
 #pragma unroll 1
     for (;;) {
@@ -681,12 +687,12 @@ static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& 
             each_number(s, row, of_row, listed, [&](uint64_t e) {
                 if (e < low || e > high) return;
                 const uint32_t at = atomicAdd(&s.count, 1u);
-                if (at < kRanked) s.active[at] = e;
+                if (at < kCompared) s.active[at] = e;
             });
             __syncthreads();
             total = s.count;
         }
-        if (of_row || total > kRanked) {
+        if (of_row || total > kCompared) {
             uint32_t left = 0;
             each_number(s, row, of_row, listed, [&](uint64_t e) {
                 if (e >= low && e <= high) least = std::min(least, e), most = std::max(most, e), ++left;
@@ -696,7 +702,7 @@ static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& 
             if (of_row) total = (uint32_t)block_sum(s, left);
         }
         first = false;
-        if (total <= kRanked) {
+        if (total <= kCompared) {
             if (of_row) {
                 if (threadIdx.x == 0) s.count = 0;
                 __syncthreads();
@@ -848,7 +854,7 @@ static __device__ __forceinline__ void finish(Choice& s, const Params& p, int64_
         }
     } else {
         // (Lanes add to sums of their own where there is room, not to wait for each other.)
-        const int copies = kParts / p.chunks, copy = threadIdx.x % copies * p.chunks;
+        const int copies = min(8, kParts / p.chunks), copy = threadIdx.x % copies * p.chunks;
         __syncthreads();
         for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
         __syncthreads();
@@ -1014,6 +1020,7 @@ int64_t chunks_of(int64_t vocab, int64_t dtype) {
     return (vocab + lead + kChunk - 1) / kChunk;
 }
 constexpr int kFewThreads = 1024, kManyThreads = 256;  // of a workgroup, in small batches and in large ones
+static_assert(kBins < 1 << 11, "a range in 22 bits");
 static_assert(WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead <= kManyThreads && kRanked <= kManyThreads, "a lane for every chunk and for every word compared");
 
 // The parts of the workspace, each a multiple of 16 bytes.

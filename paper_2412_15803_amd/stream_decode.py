@@ -134,16 +134,17 @@ class Sampler:
 
     def __init__(self, temperature=1.0, top_k=None, top_p=None, min_p=None, seed=0):
         self.settings = dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
-        self.seed, self.rows, self.lists, self.generator = seed, None, {}, None
+        self.seed, self.like, self.lists, self.generator = seed, None, {}, None
 
     def __call__(self, logits, token):
-        if self.rows != logits.shape[0]:
-            self.rows = logits.shape[0]
-            self.lists = {name: torch.full((self.rows,), v, dtype=torch.int32 if name == "top_k" else torch.float32, device=logits.device)
+        rows, like = logits.shape[0], (logits.shape, logits.dtype, logits.device)
+        if self.like != like:
+            self.like = like
+            self.lists = {name: torch.full((rows,), v, dtype=torch.int32 if name == "top_k" else torch.float32, device=logits.device)
                           for name, v in self.settings.items() if v is not None}
             self.workspace = wq.sample_workspace(logits)
             self.generator = torch.Generator(device=logits.device).manual_seed(self.seed)
-        random = torch.rand(self.rows, generator=self.generator, device=logits.device)
+        random = torch.rand(rows, generator=self.generator, device=logits.device)
         wq.sample_logits(logits, random, token, workspace=self.workspace, **self.lists)
 
 
