@@ -25,7 +25,7 @@
  *
  * The device holds w as multiples of 2^-s, s = min(51, 62 - ceil(log2(vocab)))
  * (2^-45 for 128256 words), formed in fp64, and adds them as whole numbers: the
- * token is the exact one unless random, or top_p, lies within a few of these
+ * token is the exact one unless random, top_p or min_p lies within a few of these
  * steps per word of a border, and is the same whatever order the hardware runs in.
  */
 #ifndef WQ_SAMPLE_H
