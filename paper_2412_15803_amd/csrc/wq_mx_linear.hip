@@ -548,9 +548,9 @@ void launch_few_as(const Params& p, hipStream_t st) {
     using F = Few<XF, ROWS>;
     const int64_t grid = (p.n + 15) / 16;
     const int supers = (int)((p.blocks + 15) / 16);
-    // As many waves as LDS has room for, three workgroups to a CU where there are more than one, and as take equal
-    // numbers of steps.
-    const int most = std::min(kFewWaves, (grid > 256 ? 53 : 160) * 1024 / F::kBytes), rounds = (supers + most - 1) / most, waves = (supers + rounds - 1) / rounds;
+    // As many waves as LDS has room for, three or four workgroups to a CU where there are more than one, and as take equal
+    // numbers of steps.  (28672 x 4096: one row 14.2 us with three, 13.4 with four; 16 rows 19.6 and 20.3.)
+    const int most = std::min(kFewWaves, (grid > 256 ? (ROWS <= 8 ? 40 : 53) : 160) * 1024 / F::kBytes), rounds = (supers + most - 1) / most, waves = (supers + rounds - 1) / rounds;
     hipLaunchKernelGGL((few_kernel<T, XF, ROWS>), dim3((unsigned)grid), dim3(waves * 64), waves * F::kBytes, st, p);
 }
 

@@ -1062,7 +1062,9 @@ size_t workspace_of(int64_t rows, int64_t vocab, int64_t dtype) {
 template <typename T>
 void launch(const Params& p, hipStream_t st) {
     const dim3 rows((unsigned)p.c.rows), chunks((unsigned)p.c.rows, (unsigned)p.chunks), few(kFewThreads), many(kManyThreads);
-    if (p.c.rows * p.chunks < 512) {
+    // While each large workgroup has a CU of its own.  (128256 words, top-p and top-k with top-p: 16 rows 33 and 20 us,
+    // in the launches of many rows 41 and 27; 24 rows 46 and 30, 43 and 27.)
+    if (p.c.rows * p.chunks <= 256) {
         hipLaunchKernelGGL((survey_kernel<T, kFewThreads>), chunks, few, 0, st, p);
         hipLaunchKernelGGL((choose_kernel<T, kFewThreads>), chunks, few, 0, st, p);
     } else {
