@@ -767,10 +767,16 @@ def _mx_matrix(codes, scales, names):
     element type."""
     if isinstance(codes, _Tensor) and isinstance(scales, _Tensor):
         shape, kind = codes.shape, codes.dtype
-        if len(shape) == 2 and len(scales.shape) == 2:
+        if len(shape) == 2:
             rows, width = shape
             bits, cols = (MX_FP4, 2 * width) if kind is _torch.uint8 else (MX_FP8, width)
-            return (_dev_tensor(codes, names[0], _CODES, shape), _dev_tensor(scales, names[1], _SCALES, (rows, -(-cols // 512) * 16)), rows, cols, bits)
+            scale_shape = (rows, -(-cols // 512) * 16)
+            if kind in _CODES and scales.dtype in _SCALES and scales.shape == scale_shape and codes.is_cuda and scales.is_cuda and \
+                    codes.is_contiguous() and scales.is_contiguous():
+                return codes.data_ptr(), scales.data_ptr(), rows, cols, bits
+            if len(scales.shape) == 2:  # Something is wrong with one of them: say what.
+                _dev_tensor(codes, names[0], _CODES, shape)
+                _dev_tensor(scales, names[1], _SCALES, scale_shape)
     for t, name in zip((codes, scales), names):
         if not isinstance(t, _Tensor):
             raise TypeError(f"{name} must be a torch.Tensor")
