@@ -13,9 +13,14 @@
  *   out[c]   = v[c] rounded to `dtype`, and / or v as an MX matrix (wq_mx.h)
  *
  * All of it in fp32, each result rounded once: the norm is that of s, not of
- * total.  In fp32 arithmetic a row's v are within a relative 2^-18 of the exact
- * values, where eps > 0 or the row is not all zeros and the sum of squares does
- * not overflow.
+ * total.  Squares that pass fp32's range on either side are formed of scaled
+ * numbers, so that in fp32 arithmetic a row's v are within
+ *
+ *     2^-18 * |v| + 2^-149 * (1 + |weight|)
+ *
+ * of the exact values, whatever the size of finite s and of eps.  A row of zeros
+ * with eps = 0 is 0 / 0, NaN.  Where s holds an infinity, v is NaN there and 0
+ * elsewhere; where it holds a NaN, all of v is NaN.
  */
 #ifndef WQ_NORM_H
 #define WQ_NORM_H

@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "wq_host.h"
 #include "wq_internal.h"
@@ -34,11 +35,16 @@ struct Params {
     int64_t code_stride, scale_stride;
 };
 
+// Below this mean of squares (with eps), what fp32 drops of squares under its smallest number, 2^-150 of each, may
+// count: it is less than 2^-40 of this.
+constexpr float kLeastMean = 0x1p-110f;
+constexpr int kScaledExponent = 50;  // of a row's largest magnitude where its squares are formed anew
+
 // One row to a workgroup of blockDim.x lanes, each holding the pieces threadIdx.x
 // + i * blockDim.x.  FMT 0: no MX result.
 template <typename T, int FMT, int PIECES>
 __global__ __launch_bounds__(kMaxThreads) void norm_kernel(const Params p) {
-    __shared__ float parts[kMaxThreads / 64];
+    __shared__ float parts[kMaxThreads / 64], tops[kMaxThreads / 64], sums[kMaxThreads / 64];
     const wq_norm_call& c = p.c;
     const int64_t row = blockIdx.x;
     const uint32_t threads = blockDim.x, pieces = (uint32_t)c.dim / kPiece;
@@ -69,15 +75,61 @@ __global__ __launch_bounds__(kMaxThreads) void norm_kernel(const Params p) {
     if (threadIdx.x % 64 == 63) parts[threadIdx.x / 64] = sum;
     __syncthreads();
     // Every wave adds the waves' sums in the same order.
+    const uint32_t waves = (threads + 63) / 64;
     float total = 0.0f;
-    for (uint32_t w = 0; w < (threads + 63) / 64; ++w) total += parts[w];
-    const float inv = 1.0f / sqrtf(total / (float)c.dim + c.eps);
+    for (uint32_t w = 0; w < waves; ++w) total += parts[w];
+    float mean = total / (float)c.dim + c.eps;
+    // Squares that leave fp32's range: they are formed anew of s 2^up, which brings the largest magnitude of the row
+    // (or the root of eps) to 2^49 .. 2^50, and the mean and its root follow.  A row of zeros without eps, and one that
+    // holds an infinity, stay as they are.  (All lanes have the same mean; binary16's squares lie well inside.)
+    bool scaled = false;
+    if constexpr (!std::is_same<T, _Float16>::value) {
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(mean < kLeastMean || mean == INFINITY), 0)) {
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                if (threadIdx.x + i * threads < pieces) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(s[i][j]));
+                }
+            }
+            for (int lanes = 32; lanes > 0; lanes /= 2) top = fmaxf(top, __shfl_xor(top, lanes));
+            if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+            __syncthreads();
+            top = sqrtf(c.eps);
+            for (uint32_t w = 0; w < waves; ++w) top = fmaxf(top, tops[w]);
+            scaled = __builtin_amdgcn_readfirstlane(top > 0.0f && top < INFINITY);
+            if (scaled) {
+                const int up = __builtin_amdgcn_readfirstlane(kScaledExponent - __builtin_amdgcn_frexp_expf(top));
+                sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    const uint32_t at = threadIdx.x + i * threads;
+                    if (at < pieces) {
+                        if (c.total) store8(static_cast<T*>(c.total) + row * c.total_stride + at * kPiece, s[i]);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            s[i][j] = ldexpf(s[i][j], up);
+                            sum = fmaf(s[i][j], s[i][j], sum);
+                        }
+                    }
+                }
+                sum = dev::segment_sum<64>(sum);
+                if (threadIdx.x % 64 == 63) sums[threadIdx.x / 64] = sum;
+                __syncthreads();
+                total = 0.0f;
+                for (uint32_t w = 0; w < waves; ++w) total += sums[w];
+                mean = total / (float)c.dim + ldexpf(c.eps, 2 * up);
+            }
+        }
+    }
+    const float inv = 1.0f / sqrtf(mean);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
         const uint32_t at = threadIdx.x + i * threads;
         // (Four lanes of a block are in here together: a row's pieces are a multiple of four.)
         if (at < pieces) {
-            if (c.total) store8(static_cast<T*>(c.total) + row * c.total_stride + at * kPiece, s[i]);
+            if (c.total && !scaled) store8(static_cast<T*>(c.total) + row * c.total_stride + at * kPiece, s[i]);
             const float8v w = rw[i].f32();
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] = s[i][j] * inv * w[j];
