@@ -49,8 +49,9 @@ extern "C" {
  *
  *   v = x[r][c]                                    gated = 0
  *   v = silu(x[r][c]) * x[r][cols + c]             gated = 1 (x has 2 * cols
- *       columns, the gate and up projections; silu(a) = a / (1 + exp(-a)),
- *       in fp32; of a below -87 it may come out as -0)
+ *       columns, the gate and up projections; silu(a) = a / (1 + exp(-a)); in
+ *       fp32, within 2^-20 * |v| + 2^-148 * (1 + |up|) of the exact value, but
+ *       silu of a below -87 may come out as -0)
  *   scale   of a block: the smallest power of two, at least 2^-127, with which
  *           max |v| / scale does not pass the type's largest value (6 or 448)
  *   element v / scale rounded to nearest, ties to even

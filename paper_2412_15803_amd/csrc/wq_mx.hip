@@ -42,9 +42,16 @@ struct QuantizeParams {
     Divisor per_row;        // pieces of a row
 };
 
+// g / (1 + exp(-g)) u.  exp(-g) = 2^t e^r, t = -g log2(e) as it comes out and r = -g - t ln 2 what its rounding left out,
+// up to 2^-18 far from 0, to first order.  Relative error in units of 2^-24: exp(-g) 7 (the hardware's exponential 2, the
+// correction 1, the constant in r 4 at most), 1 + exp(-g) 1, the reciprocal 2, products 2: below 2^-20.  The exponent takes
+// g in [-88, 128]: beyond, exp(-g) is 0 on one side, and on the other, from -87.34 on, the reciprocal is below the
+// normal numbers, for which the hardware gives 0, and g times it -0.  (2048 x 14336 fp16
+// to 8 bits, inputs from beyond the caches: 25.8 us, 25.4 with r left out.)
 __device__ __forceinline__ float silu_mul(float g, float u) {
-    // exp(-g) passes to infinity for large -g, and g over it to -0.
-    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f)) * u;
+    const float a = __builtin_amdgcn_fmed3f(g, -88.0f, 128.0f), t = a * -0x1.715476p+0f, r = fmaf(t, -0x1.62e43p-1f, -a);
+    const float p = __builtin_amdgcn_exp2f(t);
+    return g * __builtin_amdgcn_rcpf(1.0f + fmaf(p, r, p)) * u;
 }
 
 template <typename T, int FMT, bool GATED>
