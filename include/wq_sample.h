@@ -26,7 +26,9 @@
  * The device holds w as multiples of 2^-s, s = min(51, 62 - ceil(log2(vocab)))
  * (2^-45 for 128256 words), formed in fp64, and adds them as whole numbers: the
  * token is the exact one unless random, top_p or min_p lies within a few of these
- * steps per word of a border, and is the same whatever order the hardware runs in.
+ * steps per word of a border (always where the words that weigh anything are of
+ * one logit: shares of the sum are taken exactly), and is the same whatever order
+ * the hardware runs in.
  */
 #ifndef WQ_SAMPLE_H
 #define WQ_SAMPLE_H
@@ -48,7 +50,7 @@ extern "C" {
  * optional may be NULL. */
 typedef struct wq_sample_call {
     const void* logits;       /* [rows][vocab], rows logits_stride elements apart; aligned to its elements */
-    const float* random;      /* [rows], in [0, 1): below 0 or NaN counts as 0, 1 and above as the largest below 1 */
+    const float* random;      /* [rows], in [0, 1): below 0 or NaN counts as 0; 1 and above: the last word that stays */
     const float* temperature; /* [rows]; optional: 1 */
     const int32_t* top_k;     /* [rows], 0 or below: all; optional: all */
     const float* top_p;       /* [rows], 1 or above or NaN: all; 0 or below: the first word; optional: all */

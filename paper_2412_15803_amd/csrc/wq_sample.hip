@@ -209,10 +209,34 @@ struct Cut {
     __device__ __forceinline__ bool keeps(uint32_t k, int w) const { return k > key || (k == key && w <= word); }
 };
 
+// The whole part of share * total, 0 <= share < 1, and whether that leaves something.  Exactly: of equal words, the number
+// that reaches top_p of their sum, or that a random number is passed by, does not depend on a rounding.
+__device__ __forceinline__ uint64_t part_of(float share, uint64_t total, bool& more) {
+    // (The same in all lanes, and so worked out once.)
+    const uint32_t bits = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, share)), e = bits >> 23;
+    const uint64_t m = (bits & 0x7FFFFF) | (e ? 0x800000 : 0);
+    const int down = 150 - (int)max(e, 1u);  // share = m 2^-down, down >= 24; total < 2^63
+    const uint64_t lo = m * total, hi = __umul64hi(m, total);
+    if (down < 64) {
+        more = (lo << (64 - down)) != 0;
+        return hi << (64 - down) | lo >> down;
+    }
+    const uint64_t below = down - 64 < 24 ? ((uint64_t)1 << (down - 64)) - 1 : ~0ull;  // hi has 23 bits
+    more = lo != 0 || (hi & below) != 0;
+    return hi > below ? hi >> (down - 64) : 0;
+}
+// The least whole number of steps that reaches a share below 1 of the total, at least one.
+__device__ __forceinline__ uint64_t share_of(float share, uint64_t total) {
+    bool more;
+    const uint64_t whole = part_of(share, total, more);
+    return max(whole + (more ? 1 : 0), (uint64_t)1);
+}
+
 // A row's settings, those that change nothing left out.
 struct Settings {
-    double temperature, random;
+    double temperature;
     int top_k;      // 0: all
+    float random;   // 1: the last word
     float top_p;    // 1: all
     float min_p;    // 0: all
     bool greedy;
@@ -228,7 +252,7 @@ struct Settings {
         top_k = k > 0 && k < c.vocab ? k : 0;
         top_p = tp < 1.0f ? fmaxf(tp, 0.0f) : 1.0f;
         min_p = mp > 0.0f ? fminf(mp, 1.0f) : 0.0f;
-        random = u > 0.0f ? fmin((double)u, 0.99999999999999989) : 0.0;
+        random = u > 0.0f ? fminf(u, 1.0f) : 0.0f;
     }
     // The smallest offset with which no logit up to `top` weighs more than 1.
     __device__ __forceinline__ double offset_of(float top) const { return ceil((double)top * (1.44269504088896340736 / temperature)); }
@@ -244,8 +268,8 @@ struct Settings {
         return w;
     }
     __device__ __forceinline__ uint64_t goal(uint64_t total) const {
-        const uint64_t g = (uint64_t)(random * (double)total);
-        return g < total ? g : total - 1;
+        bool more;
+        return random < 1.0f ? part_of(random, total, more) : total - 1;
     }
 };
 
@@ -259,12 +283,6 @@ __device__ __forceinline__ int bin_of(float x, float reference) {
     return kAbove + min(max((bits >> 17) - ((127 - 5) << 6), 0), kBelow - 1);
 }
 __device__ __forceinline__ Way way_of(const Settings& set) { return set.top_k ? kCount : set.top_p < 1.0f ? kWeight : set.min_p > 0.0f ? kMinP : kDone; }
-
-// The least whole number of steps that reaches a share of the total, at least one.
-__device__ __forceinline__ uint64_t share_of(float share, uint64_t total) {
-    const double want = ceil((double)share * (double)total);
-    return want < 1.0 ? 1 : want >= (double)total ? total : (uint64_t)want;
-}
 
 // A listed word as a number, the smaller the earlier in the order of words; with its halves exchanged, the
 // smaller the lower the word.
