@@ -50,25 +50,33 @@ __global__ __launch_bounds__(kMaxThreads) void norm_kernel(const Params p) {
     const uint32_t threads = blockDim.x, pieces = (uint32_t)c.dim / kPiece;
     const T* const x = static_cast<const T*>(c.x) + row * c.x_stride;
     const T* const r = c.residual ? static_cast<const T*>(c.residual) + row * c.residual_stride : nullptr;
+    // A long row's weight is read when its sum is known, and fp32 ones are read half by half: registers hold no more.
+    // (1024 rows of 32768 fp32, residual, to 8 bits: 90 us; all at once, with up to 100 registers in scratch memory, 159.
+    // 2048 of binary16: 96 and 169.)
+    constexpr bool kLate = PIECES == kMaxPieces;
+    constexpr int kAtOnce = kLate && sizeof(T) == 4 ? 2 : PIECES;
     Raw<T> rx[PIECES], rr[PIECES], rw[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const uint32_t at = threadIdx.x + i * threads;
-        if (at < pieces) {
-            rx[i].load_once(x + at * kPiece);
-            if (r) rr[i].load_once(r + at * kPiece);
-            rw[i].load(static_cast<const T*>(c.weight) + at * kPiece);
-        }
-    }
     float8v s[PIECES];
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        if (threadIdx.x + i * threads < pieces) {
-            s[i] = rx[i].f32();
-            if (r) s[i] += rr[i].f32();
+    for (int first = 0; first < PIECES; first += kAtOnce) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(s[i][j], s[i][j], sum);
+        for (int i = first; i < first + kAtOnce; ++i) {
+            const uint32_t at = threadIdx.x + i * threads;
+            if (at < pieces) {
+                rx[i].load_once(x + at * kPiece);
+                if (r) rr[i].load_once(r + at * kPiece);
+                if constexpr (!kLate) rw[i].load(static_cast<const T*>(c.weight) + at * kPiece);
+            }
+        }
+#pragma unroll
+        for (int i = first; i < first + kAtOnce; ++i) {
+            if (threadIdx.x + i * threads < pieces) {
+                s[i] = rx[i].f32();
+                if (r) s[i] += rr[i].f32();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = fmaf(s[i][j], s[i][j], sum);
+            }
         }
     }
     sum = dev::segment_sum<64>(sum);
@@ -130,6 +138,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_kernel(const Params p) {
         // (Four lanes of a block are in here together: a row's pieces are a multiple of four.)
         if (at < pieces) {
             if (c.total && !scaled) store8(static_cast<T*>(c.total) + row * c.total_stride + at * kPiece, s[i]);
+            if constexpr (kLate) rw[i].load(static_cast<const T*>(c.weight) + at * kPiece);
             const float8v w = rw[i].f32();
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] = s[i][j] * inv * w[j];
