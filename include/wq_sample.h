@@ -29,6 +29,13 @@
  * steps per word of a border (always where the words that weigh anything are of
  * one logit: shares of the sum are taken exactly), and is the same whatever order
  * the hardware runs in.
+ *
+ * Time: a histogram of at most 1/64 of a logit's distance from the best ones tells
+ * where the cut is; up to 4096 words of its bin are listed.  Where the bin has
+ * more, one workgroup reads the row again and again: thousands of equal logits at
+ * the cut, and from about 170000 words on also top-p cuts in the middle of a broad
+ * row (262144 normal logits, temperature 2 / 3 of their deviation, top-p 0.95:
+ * 0.62 ms; at temperature 1 / 3 of it and top-p 0.9 0.04 ms).
  */
 #ifndef WQ_SAMPLE_H
 #define WQ_SAMPLE_H

@@ -134,7 +134,7 @@ __device__ __forceinline__ void turn_over() {
 // steps of K in turn.  Everything goes through LDS, each wave's own part of it, in whole
 // rows: loads in the matrix cores' order, consecutive lanes on different rows, cost a
 // look-up of the cache for each lane, which bounded one token at 4.2 TB/s (x too in that
-// order) and 5.3 TB/s (W alone).  In LDS a row's pieces of 16 bytes lie in an order of its
+// order) and 5.3 TB/s (W alone), W in the memory-side cache.  In LDS a row's pieces of 16 bytes lie in an order of its
 // own, for the banks.
 constexpr int kFewWaves = 16;
 
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(S::kWaves * 64, 1) void tile_kernel(const Params p)
                 if (turn && (super + 1 < supers || next < order.end)) turn_scales(super + 1 < supers ? blocks - (super + 1) * 16 : part_blocks(next), buffer);
                 turn_over();
                 if constexpr (S::kTurns) __builtin_amdgcn_s_setprio(1);
-unrolled<S::kSub>([&](auto U_) {
+                unrolled<S::kSub>([&](auto U_) {
                     constexpr int u = decltype(U_)::value, of = t * S::kSub + u;
 #pragma unroll
                     for (int i = 0; i < S::FN; ++i)

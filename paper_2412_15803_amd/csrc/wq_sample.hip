@@ -356,649 +356,648 @@ __device__ __forceinline__ void add(uint64_t* at, uint64_t v) { atomicAdd(reinte
 // What workgroups of kThreads lanes do.
 template <int kThreads>
 struct Block {
-static constexpr int kWaves = kThreads / 64;
-template <typename T>
-static constexpr int kEach = kVectors<T> / kThreads;  // vectors of a lane
+    static constexpr int kWaves = kThreads / 64;
+    template <typename T>
+    static constexpr int kEach = kVectors<T> / kThreads;  // vectors of a lane
 
-struct Small {  // what a block's lanes exchange
-    uint64_t parts[2][kWaves];
-    uint64_t before, found;
-    uint32_t digit, base, count;
-    int low, high;
-    int turn[kWaves];  // of parts; each wave has its own
-};
-static __device__ __forceinline__ void begin(Small& s) {
-    if (threadIdx.x % 64 == 0) s.turn[threadIdx.x / 64] = 0;
-}
-
-
-// A chunk's words of a lane.
-template <typename T>
-struct Chunk {
-    u32x4 bits[kEach<T>];
-    float x[kEach<T>][kPer<T>];
-    int first;
-    __device__ __forceinline__ Chunk(const Row<T>& row, int chunk) {
-        first = chunk * kVectors<T> + threadIdx.x;
-#pragma unroll
-        for (int i = 0; i < kEach<T>; ++i) bits[i] = row.fetch(first + i * kThreads);
+    struct Small {  // what a block's lanes exchange
+        uint64_t parts[2][kWaves];
+        uint64_t before, found;
+        uint32_t digit, base, count;
+        int low, high;
+        int turn[kWaves];  // of parts; each wave has its own
+    };
+    static __device__ __forceinline__ void begin(Small& s) {
+        if (threadIdx.x % 64 == 0) s.turn[threadIdx.x / 64] = 0;
     }
-    __device__ __forceinline__ void take(const Row<T>& row) {
+
+    // A chunk's words of a lane.
+    template <typename T>
+    struct Chunk {
+        u32x4 bits[kEach<T>];
+        float x[kEach<T>][kPer<T>];
+        int first;
+        __device__ __forceinline__ Chunk(const Row<T>& row, int chunk) {
+            first = chunk * kVectors<T> + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < kEach<T>; ++i) row.words(first + i * kThreads, bits[i], x[i]);
-    }
+            for (int i = 0; i < kEach<T>; ++i) bits[i] = row.fetch(first + i * kThreads);
+        }
+        __device__ __forceinline__ void take(const Row<T>& row) {
+#pragma unroll
+            for (int i = 0; i < kEach<T>; ++i) row.words(first + i * kThreads, bits[i], x[i]);
+        }
+        template <typename F>
+        __device__ __forceinline__ void each(const Row<T>& row, F f) const {
+#pragma unroll
+            for (int i = 0; i < kEach<T>; ++i)
+#pragma unroll
+                for (int j = 0; j < kPer<T>; ++j) f(x[i][j], (first + i * kThreads) * kPer<T> - row.lead + j);
+        }
+    };
+
+    // Over the block: in the lanes before this one, and in all.  (Two places in turn, so that one barrier does.)
     template <typename F>
-    __device__ __forceinline__ void each(const Row<T>& row, F f) const {
-#pragma unroll
-        for (int i = 0; i < kEach<T>; ++i)
-#pragma unroll
-            for (int j = 0; j < kPer<T>; ++j) f(x[i][j], (first + i * kThreads) * kPer<T> - row.lead + j);
+    static __device__ __forceinline__ uint64_t block_scan(Small& s, uint64_t v, uint64_t& all, F f) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+        uint64_t* const parts = s.parts[s.turn[wave]];
+        const uint64_t up = scan64(v, f);
+        if (lane == 63) parts[wave] = up, s.turn[wave] ^= 1;
+        __syncthreads();
+        const uint64_t waves = scan16(lane < kWaves ? parts[lane] : 0, f);
+        all = lane_of(waves, kWaves - 1);
+        const uint64_t before = wave ? lane_of(waves, wave - 1) : 0;
+        const uint64_t mine = dpp64<0x138, 0xF>(up);  // wave_shr:1
+        return f(before, mine);
     }
-};
+    // Sum of v in the lanes before this one; `total` that of all.
+    static __device__ __forceinline__ uint64_t block_before(Small& s, uint64_t v, uint64_t& total) { return block_scan(s, v, total, Sum()); }
+    static __device__ __forceinline__ uint64_t block_sum(Small& s, uint64_t v) {
+        uint64_t total;
+        block_scan(s, v, total, Sum());
+        return total;
+    }
+    static __device__ __forceinline__ uint64_t block_most(Small& s, uint64_t v) {
+        uint64_t most;
+        block_scan(s, v, most, Most());
+        return most;
+    }
+    // The best word of the block's words, the same in all lanes: the largest key, of equal ones the lowest word.
+    static __device__ __forceinline__ void block_best(Small& s, uint32_t& key, int& word) {
+        const uint64_t best = block_most(s, (uint64_t)key << 32 | ~(uint32_t)word);
+        key = (uint32_t)(best >> 32), word = (int)~(uint32_t)best;
+    }
 
-// Over the block: in the lanes before this one, and in all.  (Two places in turn, so that one barrier does.)
-template <typename F>
-static __device__ __forceinline__ uint64_t block_scan(Small& s, uint64_t v, uint64_t& all, F f) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    uint64_t* const parts = s.parts[s.turn[wave]];
-    const uint64_t up = scan64(v, f);
-    if (lane == 63) parts[wave] = up, s.turn[wave] ^= 1;
-    __syncthreads();
-    const uint64_t waves = scan16(lane < kWaves ? parts[lane] : 0, f);
-    all = lane_of(waves, kWaves - 1);
-    const uint64_t before = wave ? lane_of(waves, wave - 1) : 0;
-    const uint64_t mine = dpp64<0x138, 0xF>(up);  // wave_shr:1
-    return f(before, mine);
-}
-// Sum of v in the lanes before this one; `total` that of all.
-static __device__ __forceinline__ uint64_t block_before(Small& s, uint64_t v, uint64_t& total) { return block_scan(s, v, total, Sum()); }
-static __device__ __forceinline__ uint64_t block_sum(Small& s, uint64_t v) {
-    uint64_t total;
-    block_scan(s, v, total, Sum());
-    return total;
-}
-static __device__ __forceinline__ uint64_t block_most(Small& s, uint64_t v) {
-    uint64_t most;
-    block_scan(s, v, most, Most());
-    return most;
-}
-// The best word of the block's words, the same in all lanes: the largest key, of equal ones the lowest word.
-static __device__ __forceinline__ void block_best(Small& s, uint32_t& key, int& word) {
-    const uint64_t best = block_most(s, (uint64_t)key << 32 | ~(uint32_t)word);
-    key = (uint32_t)(best >> 32), word = (int)~(uint32_t)best;
-}
+    // The reference: the largest logit of the row's first vectors, the same for all of its chunks; 0 where that is no
+    // logit that words worth choosing have (the lowest value of a type stands for a mask), as all of those would lie in
+    // one bin.
+    template <typename T>
+    static __device__ __forceinline__ float reference_of(Small& s, const Row<T>& row, u32x4 bits) {
+        uint32_t key = kNothing;
+        int word = 0;
+        float y[kPer<T>];
+        row.words(threadIdx.x, bits, y);
+#pragma unroll
+        for (int i = 0; i < kPer<T>; ++i) key = max(key, key_of(y[i]));
+        block_best(s, key, word);
+        const float most = value_of(key);
+        return fabsf(most) < 1024.0f ? most : 0.0f;
+    }
 
-// The reference: the largest logit of the row's first vectors, the same for all of its chunks; 0 where that is no
-// logit that words worth choosing have (the lowest value of a type stands for a mask), as all of those would lie in
-// one bin.
-template <typename T>
-static __device__ __forceinline__ float reference_of(Small& s, const Row<T>& row, u32x4 bits) {
-    uint32_t key = kNothing;
-    int word = 0;
-    float y[kPer<T>];
-    row.words(threadIdx.x, bits, y);
+    // Workgroups of a row are `rows` apart, so that a row's run at the same time.
+    template <typename T>
+    static __device__ __forceinline__ void survey(const Params& p) {
+        __shared__ struct : Small {
+            uint64_t bins[kBins];
+        } s;
+        const int64_t r = blockIdx.x;
+        const int chunk = blockIdx.y;
+        const Row<T> row(p, r);
+        begin(s);
+        Chunk<T> x(row, chunk);
+        const u32x4 ahead = row.fetch(threadIdx.x);
+        const Settings set(p, r);
+        const Way way = way_of(set);
+        const bool binned = !set.greedy && (way == kCount || way == kWeight);
+        for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
+        if (threadIdx.x == 0) s.low = kBins, s.high = 0;
+        x.take(row);
+        uint32_t best = kNothing;
+        int word = INT32_MAX;
+        x.each(row, [&](float v, int w) {
+            const uint32_t key = key_of(v);
+            word = key > best ? w : word;  // (A lane's words rise.)
+            best = max(best, key);
+        });
+        const uint32_t own = best;
+        block_best(s, best, word);
+        Record record{0, 0.0, best, word, 0, 0, reference_of(s, row, ahead), 0};
+        const int64_t at = r * p.chunks + chunk;
+        if (!set.greedy && best != kNothing && way != kMinP) {
+            const bool infinite = best == kInfinity;
+            record.offset = infinite ? 0.0 : set.offset_of(value_of(best));
+            const Weights weights = set.weights(p, value_of(best), record.offset);
+            uint64_t sum = 0;
+            if (way == kCount) {
+                // Where top_k groups of lanes have a word each that is no smaller than this, smaller ones are not among the
+                // row's first top_k, and not counted.
+                uint32_t least = own;
+                if (set.top_k <= kThreads / 4) least = most_of_lanes<4>(least);
+                if (set.top_k <= kThreads / 16) least = most_of_lanes<16>(least);
+                least = set.top_k <= kThreads ? ~(uint32_t)block_most(s, (uint32_t)~least) : 0;
+                x.each(row, [&](float v, int) {
+                    if (v > -INFINITY && key_of(v) >= least) add(&s.bins[bin_of(v, record.reference)], 1);
+                });
+            } else {
+                // A vector's weights first, so that their chains of operations run side by side.
 #pragma unroll
-    for (int i = 0; i < kPer<T>; ++i) key = max(key, key_of(y[i]));
-    block_best(s, key, word);
-    const float most = value_of(key);
-    return fabsf(most) < 1024.0f ? most : 0.0f;
-}
-
-// Workgroups of a row are `rows` apart, so that a row's run at the same time.
-template <typename T>
-static __device__ __forceinline__ void survey(const Params& p) {
-    __shared__ struct : Small {
-        uint64_t bins[kBins];
-    } s;
-    const int64_t r = blockIdx.x;
-    const int chunk = blockIdx.y;
-    const Row<T> row(p, r);
-    begin(s);
-    Chunk<T> x(row, chunk);
-    const u32x4 ahead = row.fetch(threadIdx.x);
-    const Settings set(p, r);
-    const Way way = way_of(set);
-    const bool binned = !set.greedy && (way == kCount || way == kWeight);
-    for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
-    if (threadIdx.x == 0) s.low = kBins, s.high = 0;
-    x.take(row);
-    uint32_t best = kNothing;
-    int word = INT32_MAX;
-    x.each(row, [&](float v, int w) {
-        const uint32_t key = key_of(v);
-        word = key > best ? w : word;  // (A lane's words rise.)
-        best = max(best, key);
-    });
-    const uint32_t own = best;
-    block_best(s, best, word);
-    Record record{0, 0.0, best, word, 0, 0, reference_of(s, row, ahead), 0};
-    const int64_t at = r * p.chunks + chunk;
-    if (!set.greedy && best != kNothing && way != kMinP) {
-        const bool infinite = best == kInfinity;
-        record.offset = infinite ? 0.0 : set.offset_of(value_of(best));
-        const Weights weights = set.weights(p, value_of(best), record.offset);
-        uint64_t sum = 0;
-        if (way == kCount) {
-            // Where top_k groups of lanes have a word each that is no smaller than this, smaller ones are not among the
-            // row's first top_k, and not counted.
-            uint32_t least = own;
-            if (set.top_k <= kThreads / 4) least = most_of_lanes<4>(least);
-            if (set.top_k <= kThreads / 16) least = most_of_lanes<16>(least);
-            least = set.top_k <= kThreads ? ~(uint32_t)block_most(s, (uint32_t)~least) : 0;
-            x.each(row, [&](float v, int) {
-                if (v > -INFINITY && key_of(v) >= least) add(&s.bins[bin_of(v, record.reference)], 1);
-            });
-        } else {
-            // A vector's weights first, so that their chains of operations run side by side.
+                for (int i = 0; i < kEach<T>; ++i) {
+                    uint64_t w[kPer<T>];
 #pragma unroll
-            for (int i = 0; i < kEach<T>; ++i) {
-                uint64_t w[kPer<T>];
+                    for (int j = 0; j < kPer<T>; ++j) w[j] = weights.of(weights.log2_of(x.x[i][j]));
 #pragma unroll
-                for (int j = 0; j < kPer<T>; ++j) w[j] = weights.of(weights.log2_of(x.x[i][j]));
-#pragma unroll
-                for (int j = 0; j < kPer<T>; ++j) {
-                    sum += w[j];
-                    if (binned && w[j]) add(&s.bins[bin_of(x.x[i][j], record.reference)], w[j]);
+                    for (int j = 0; j < kPer<T>; ++j) {
+                        sum += w[j];
+                        if (binned && w[j]) add(&s.bins[bin_of(x.x[i][j], record.reference)], w[j]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (binned) {
+                __syncthreads();
+                int low = kBins, high = 0;
+                for (int i = threadIdx.x; i < kBins; i += kThreads)
+                    if (s.bins[i]) low = min(low, i), high = max(high, i + 1);
+                if (high) atomicMin(&s.low, low), atomicMax(&s.high, high);
+                __syncthreads();
+                record.low = s.low, record.high = s.high;
+                for (int i = s.low + threadIdx.x; i < s.high; i += kThreads) gbl(p.bins)[at * kBins + i] = s.bins[i];
+            } else {
+                record.sum = block_sum(s, sum);
             }
         }
-        if (binned) {
-            __syncthreads();
-            int low = kBins, high = 0;
-            for (int i = threadIdx.x; i < kBins; i += kThreads)
-                if (s.bins[i]) low = min(low, i), high = max(high, i + 1);
-            if (high) atomicMin(&s.low, low), atomicMax(&s.high, high);
-            __syncthreads();
-            record.low = s.low, record.high = s.high;
-            for (int i = s.low + threadIdx.x; i < s.high; i += kThreads) gbl(p.bins)[at * kBins + i] = s.bins[i];
-        } else {
-            record.sum = block_sum(s, sum);
+        if (threadIdx.x == 0) {
+            p.records[at] = record;
+            if (chunk == 0) p.plans[r].done = p.plans[r].listed = 0;
         }
     }
-    if (threadIdx.x == 0) {
-        p.records[at] = record;
-        if (chunk == 0) p.plans[r].done = p.plans[r].listed = 0;
-    }
-}
 
-// The word of a chunk at which the sum of weights passes `goal`.  Where it does not quite (the chunk's weight was
-// summed from other roundings than these), it is the chunk's best word, which stays if any of the chunk does.
-template <typename T, typename F>
-static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p, int64_t r, const Row<T>& row, int chunk, uint64_t goal, double total, F weight) {
-    // Words in their order are vector by vector, and the lanes of a round are consecutive ones.
-    const Chunk<T> x(row, chunk);
+    // The word of a chunk at which the sum of weights passes `goal`.  Where it does not quite (the chunk's weight was
+    // summed from other roundings than these), it is the chunk's best word, which stays if any of the chunk does.
+    template <typename T, typename F>
+    static __device__ __forceinline__ void choose_in_chunk(Small& s, const Params& p, int64_t r, const Row<T>& row, int chunk, uint64_t goal, double total, F weight) {
+        // Words in their order are vector by vector, and the lanes of a round are consecutive ones.
+        const Chunk<T> x(row, chunk);
 #pragma unroll
-    for (int i = 0; i < kEach<T>; ++i) {
-        const int v = x.first + i * kThreads;
-        float y[kPer<T>];
-        row.words(v, x.bits[i], y);
-        uint64_t w[kPer<T>], sum = 0, all;
-#pragma unroll
-        for (int j = 0; j < kPer<T>; ++j) {
-            w[j] = weight(y[j], v * kPer<T> + j - row.lead);
-            sum += w[j];
-        }
-        uint64_t up = block_before(s, sum, all);
-        if (goal < all) {
+        for (int i = 0; i < kEach<T>; ++i) {
+            const int v = x.first + i * kThreads;
+            float y[kPer<T>];
+            row.words(v, x.bits[i], y);
+            uint64_t w[kPer<T>], sum = 0, all;
 #pragma unroll
             for (int j = 0; j < kPer<T>; ++j) {
-                if (up <= goal && goal < up + w[j]) {
-                    gbl(p.c.token)[r] = v * kPer<T> + j - row.lead;
-                    if (p.c.share) gbl(p.c.share)[r] = (float)((double)w[j] / total);
-                }
-                up += w[j];
+                w[j] = weight(y[j], v * kPer<T> + j - row.lead);
+                sum += w[j];
             }
-            return;
+            uint64_t up = block_before(s, sum, all);
+            if (goal < all) {
+#pragma unroll
+                for (int j = 0; j < kPer<T>; ++j) {
+                    if (up <= goal && goal < up + w[j]) {
+                        gbl(p.c.token)[r] = v * kPer<T> + j - row.lead;
+                        if (p.c.share) gbl(p.c.share)[r] = (float)((double)w[j] / total);
+                    }
+                    up += w[j];
+                }
+                return;
+            }
+            goal -= all;
         }
-        goal -= all;
-    }
-    if (threadIdx.x == 0) {
-        const Record& record = p.records[r * p.chunks + chunk];
-        gbl(p.c.token)[r] = record.word;
-        if (p.c.share) gbl(p.c.share)[r] = (float)((double)weight(value_of(record.key), record.word) / total);
-    }
-}
-
-struct Survey : Small {  // what plan looks up of the chunks: their bins' first, end and shift
-    uint32_t ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
-};
-
-// What is to be done with a row, by a workgroup whose lanes are at least as many as the chunks.  Rows that need no
-// cut are answered here, where `answers`.
-template <typename T>
-static __device__ __forceinline__ Plan plan(Survey& s, const Params& p, int64_t r, const Row<T>& row, const Settings& set, bool answers) {
-    // What survey left: thread i has chunk i's.
-    const bool has = (int)threadIdx.x < p.chunks;
-    Record record{0, 0.0, kNothing, INT32_MAX, 0, 0, 0.0f, 0};
-    if (has) record = p.records[r * p.chunks + threadIdx.x];
-    uint32_t best = record.key;
-    int word = record.word;
-    block_best(s, best, word);
-    const float reference = p.records[r * p.chunks].reference;
-    Plan plan{};
-    plan.best = best, plan.word = word, plan.cut_bin = kBins, plan.reference = reference;
-    plan.way = best == kNothing || set.greedy ? kDone : way_of(set);
-    if (plan.way == kDone && !answers) return plan;
-    if (best == kNothing || set.greedy) {
         if (threadIdx.x == 0) {
-            gbl(p.c.token)[r] = best == kNothing ? -1 : word;
-            if (p.c.share) gbl(p.c.share)[r] = best == kNothing ? 0.0f : 1.0f;
-        }
-    } else {
-        // A chunk's offset differs from the row's by a whole number: by as many bits its weights are too large.  (Where the
-        // largest logit is +infinity, only the chunks that have it weigh anything.)
-        const bool infinite = best == kInfinity;
-        plan.offset = infinite ? 0.0 : set.offset_of(value_of(best));
-        const int over = record.key == kNothing || (infinite && record.key != kInfinity) ? 63 : (int)fmin(plan.offset - record.offset, 63.0);
-        if (plan.way == kDone) {
-            const uint64_t mine = record.sum >> over;
-            uint64_t total;
-            const uint64_t up = block_before(s, mine, total), goal = set.goal(total);
-            if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = (goal - up) << over, s.base = record.key, s.ranges[0] = (uint32_t)over, s.found = __builtin_bit_cast(uint64_t, record.offset);
-            __syncthreads();
-            const Weights own = set.weights(p, value_of(s.base), __builtin_bit_cast(double, s.found));
-            choose_in_chunk(s, p, r, row, (int)s.digit, s.before, __builtin_ldexp((double)total, (int)s.ranges[0]), [&](float v, int) { return own.of(own.log2_of(v)); });
-        } else if (plan.way != kMinP) {
-            // The bin that the cut lies in, and what lies before it.
-            if ((int)threadIdx.x < p.chunks + kAhead)
-                s.ranges[threadIdx.x] = has ? (uint32_t)record.low | (uint32_t)record.high << 11 | (plan.way == kCount ? 0u : (uint32_t)over) << 22 : 0;
-            __syncthreads();
-            constexpr int kMine = 2;
-            static_assert(kThreads * kMine >= kBins, "(Of the last lanes none.)");
-            typedef uint64_t u64x2 __attribute__((ext_vector_type(kMine)));
-            uint64_t v[kMine] = {}, sum = 0, total;
-            const int first = threadIdx.x * kMine, wave_first = __builtin_amdgcn_readfirstlane(first);
-#pragma unroll 1
-            for (int c = 0; c < p.chunks; c += kAhead) {
-                // (One look into LDS for each wave; its broadcasts for every chunk took longer than the bins.)
-                const uint32_t ranges = s.ranges[c + threadIdx.x % kAhead];
-                u64x2 b[kAhead];
-#pragma unroll
-                for (int a = 0; a < kAhead; ++a) {
-                    // (Most waves have no bin of a chunk that was written, and need no load: those bounded this.)
-                    const uint32_t range = (uint32_t)__builtin_amdgcn_readlane((int)ranges, a);
-                    const int low = range & 0x7FF, high = range >> 11 & 0x7FF;
-                    const uint64_t* const bins = p.bins + (r * p.chunks + c + a) * kBins + min(first, kBins - kMine);
-                    b[a] = u64x2{0, 0};
-                    if (wave_first + 64 * kMine > low && wave_first < high) b[a] = *gbl(reinterpret_cast<const u64x2*>(bins));
-                }
-#pragma unroll
-                for (int a = 0; a < kAhead; ++a) {
-                    const uint32_t range = (uint32_t)__builtin_amdgcn_readlane((int)ranges, a);
-                    const int low = range & 0x7FF, high = range >> 11 & 0x7FF, by = (int)(range >> 22);
-#pragma unroll
-                    for (int i = 0; i < kMine; ++i) v[i] += first + i >= low && first + i < high ? b[a][i] >> by : 0;  // (What lies outside was not written.)
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) sum += v[i];
-            uint64_t up = block_before(s, sum, total);
-            const uint64_t target = plan.way == kCount ? std::min<uint64_t>(set.top_k, total) : share_of(set.top_p, total);
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                if (up < target && up + v[i] >= target) s.digit = first + i, s.before = up, s.found = v[i];
-                up += v[i];
-            }
-            __syncthreads();
-            plan.cut_bin = (int)s.digit, plan.ahead = s.before, plan.need = target - s.before;
-            // While all words that may stay are few, all are listed.  A long list, and top-p behind a long
-            // top-k, are worked out by one workgroup.
-            if (plan.way == kCount) {
-                plan.few = s.before + s.found <= (uint64_t)p.list_size;
-                plan.alone = !plan.few && (set.top_p < 1.0f || s.found > (uint64_t)p.list_size);
-            }
+            const Record& record = p.records[r * p.chunks + chunk];
+            gbl(p.c.token)[r] = record.word;
+            if (p.c.share) gbl(p.c.share)[r] = (float)((double)weight(value_of(record.key), record.word) / total);
         }
     }
-    return plan;
-}
 
-template <typename T>
-static __device__ __forceinline__ void plan_rows(const Params& p) {
-    __shared__ Survey s;
-    const int64_t r = blockIdx.x;
-    begin(s);
-    const Plan made = plan(s, p, r, Row<T>(p, r), Settings(p, r), true);
-    if (threadIdx.x == 0) p.plans[r] = made;
-}
+    struct Survey : Small {  // what plan looks up of the chunks: their bins' first, end and shift
+        uint32_t ranges[WQ_SAMPLE_MAX_VOCAB / kChunk + 1 + kAhead];
+    };
 
-struct Listing : Small {
-    uint64_t staged[kStaged];
-};
-struct Choice : Survey {
-    uint64_t list[kList];
-    uint64_t bins[kParts];
-    uint64_t active[kRanked];
-    uint64_t chunks[WQ_SAMPLE_MAX_VOCAB / kChunk + 1];
-};
-
-// f for every number of the list, or for every word of the row.
-template <typename T, typename F>
-static __device__ __forceinline__ void each_number(Choice& s, const Row<T>& row, bool of_row, int listed, F f) {
-    if (of_row) {
-        row.each(0, row.vectors, [&](float v, int w) {
-            if (v > -INFINITY) f(entry_of(key_of(v), w));
-        });
-    } else {
+    // What is to be done with a row, by a workgroup whose lanes are at least as many as the chunks.  Rows that need no
+    // cut are answered here, where `answers`.
+    template <typename T>
+    static __device__ __forceinline__ Plan plan(Survey& s, const Params& p, int64_t r, const Row<T>& row, const Settings& set, bool answers) {
+        // What survey left: thread i has chunk i's.
+        const bool has = (int)threadIdx.x < p.chunks;
+        Record record{0, 0.0, kNothing, INT32_MAX, 0, 0, 0.0f, 0};
+        if (has) record = p.records[r * p.chunks + threadIdx.x];
+        uint32_t best = record.key;
+        int word = record.word;
+        block_best(s, best, word);
+        const float reference = p.records[r * p.chunks].reference;
+        Plan plan{};
+        plan.best = best, plan.word = word, plan.cut_bin = kBins, plan.reference = reference;
+        plan.way = best == kNothing || set.greedy ? kDone : way_of(set);
+        if (plan.way == kDone && !answers) return plan;
+        if (best == kNothing || set.greedy) {
+            if (threadIdx.x == 0) {
+                gbl(p.c.token)[r] = best == kNothing ? -1 : word;
+                if (p.c.share) gbl(p.c.share)[r] = best == kNothing ? 0.0f : 1.0f;
+            }
+        } else {
+            // A chunk's offset differs from the row's by a whole number: by as many bits its weights are too large.  (Where the
+            // largest logit is +infinity, only the chunks that have it weigh anything.)
+            const bool infinite = best == kInfinity;
+            plan.offset = infinite ? 0.0 : set.offset_of(value_of(best));
+            const int over = record.key == kNothing || (infinite && record.key != kInfinity) ? 63 : (int)fmin(plan.offset - record.offset, 63.0);
+            if (plan.way == kDone) {
+                const uint64_t mine = record.sum >> over;
+                uint64_t total;
+                const uint64_t up = block_before(s, mine, total), goal = set.goal(total);
+                if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = (goal - up) << over, s.base = record.key, s.ranges[0] = (uint32_t)over, s.found = __builtin_bit_cast(uint64_t, record.offset);
+                __syncthreads();
+                const Weights own = set.weights(p, value_of(s.base), __builtin_bit_cast(double, s.found));
+                choose_in_chunk(s, p, r, row, (int)s.digit, s.before, __builtin_ldexp((double)total, (int)s.ranges[0]), [&](float v, int) { return own.of(own.log2_of(v)); });
+            } else if (plan.way != kMinP) {
+                // The bin that the cut lies in, and what lies before it.
+                if ((int)threadIdx.x < p.chunks + kAhead)
+                    s.ranges[threadIdx.x] = has ? (uint32_t)record.low | (uint32_t)record.high << 11 | (plan.way == kCount ? 0u : (uint32_t)over) << 22 : 0;
+                __syncthreads();
+                constexpr int kMine = 2;
+                static_assert(kThreads * kMine >= kBins, "(Of the last lanes none.)");
+                typedef uint64_t u64x2 __attribute__((ext_vector_type(kMine)));
+                uint64_t v[kMine] = {}, sum = 0, total;
+                const int first = threadIdx.x * kMine, wave_first = __builtin_amdgcn_readfirstlane(first);
 #pragma unroll 1
-        for (int i = threadIdx.x; i < listed; i += kThreads) f(s.list[i]);
+                for (int c = 0; c < p.chunks; c += kAhead) {
+                    // (One look into LDS for each wave; its broadcasts for every chunk took longer than the bins.)
+                    const uint32_t ranges = s.ranges[c + threadIdx.x % kAhead];
+                    u64x2 b[kAhead];
+#pragma unroll
+                    for (int a = 0; a < kAhead; ++a) {
+                        // (Most waves have no bin of a chunk that was written, and need no load: those bounded this.)
+                        const uint32_t range = (uint32_t)__builtin_amdgcn_readlane((int)ranges, a);
+                        const int low = range & 0x7FF, high = range >> 11 & 0x7FF;
+                        const uint64_t* const bins = p.bins + (r * p.chunks + c + a) * kBins + min(first, kBins - kMine);
+                        b[a] = u64x2{0, 0};
+                        if (wave_first + 64 * kMine > low && wave_first < high) b[a] = *gbl(reinterpret_cast<const u64x2*>(bins));
+                    }
+#pragma unroll
+                    for (int a = 0; a < kAhead; ++a) {
+                        const uint32_t range = (uint32_t)__builtin_amdgcn_readlane((int)ranges, a);
+                        const int low = range & 0x7FF, high = range >> 11 & 0x7FF, by = (int)(range >> 22);
+#pragma unroll
+                        for (int i = 0; i < kMine; ++i) v[i] += first + i >= low && first + i < high ? b[a][i] >> by : 0;  // (What lies outside was not written.)
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) sum += v[i];
+                uint64_t up = block_before(s, sum, total);
+                const uint64_t target = plan.way == kCount ? std::min<uint64_t>(set.top_k, total) : share_of(set.top_p, total);
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    if (up < target && up + v[i] >= target) s.digit = first + i, s.before = up, s.found = v[i];
+                    up += v[i];
+                }
+                __syncthreads();
+                plan.cut_bin = (int)s.digit, plan.ahead = s.before, plan.need = target - s.before;
+                // While all words that may stay are few, all are listed.  A long list, and top-p behind a long
+                // top-k, are worked out by one workgroup.
+                if (plan.way == kCount) {
+                    plan.few = s.before + s.found <= (uint64_t)p.list_size;
+                    plan.alone = !plan.few && (set.top_p < 1.0f || s.found > (uint64_t)p.list_size);
+                }
+            }
+        }
+        return plan;
     }
-}
 
-// The number up to which, in rising order, the numbers' weights reach `target` (which their sum does).  Their
-// range is cut into kParts; of the part that it lies in, the range again, until each lane has one number left
-// and can add up those below it.
-template <typename T>
-static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& row, bool of_row, int listed, uint64_t target, const Weigh& weigh) {
-    uint64_t low = 0, high = ~0ull;  // it lies in here
-    const bool all_few = !of_row && listed <= kCompared;
-    bool first = true;
+    template <typename T>
+    static __device__ __forceinline__ void plan_rows(const Params& p) {
+        __shared__ Survey s;
+        const int64_t r = blockIdx.x;
+        begin(s);
+        const Plan made = plan(s, p, r, Row<T>(p, r), Settings(p, r), true);
+        if (threadIdx.x == 0) p.plans[r] = made;
+    }
+
+    struct Listing : Small {
+        uint64_t staged[kStaged];
+    };
+    struct Choice : Survey {
+        uint64_t list[kList];
+        uint64_t bins[kParts];
+        uint64_t active[kRanked];
+        uint64_t chunks[WQ_SAMPLE_MAX_VOCAB / kChunk + 1];
+    };
+
+    // f for every number of the list, or for every word of the row.
+    template <typename T, typename F>
+    static __device__ __forceinline__ void each_number(Choice& s, const Row<T>& row, bool of_row, int listed, F f) {
+        if (of_row) {
+            row.each(0, row.vectors, [&](float v, int w) {
+                if (v > -INFINITY) f(entry_of(key_of(v), w));
+            });
+        } else {
 #pragma unroll 1
-    for (;;) {
-        uint64_t least = ~0ull, most = 0;
-        uint32_t total = listed;
-        __syncthreads();
-        if (!of_row && !first) {
-            // Those that are left are put together, if they are few.
-            if (threadIdx.x == 0) s.count = 0;
-            __syncthreads();
-            each_number(s, row, of_row, listed, [&](uint64_t e) {
-                if (e < low || e > high) return;
-                const uint32_t at = atomicAdd(&s.count, 1u);
-                if (at < kCompared) s.active[at] = e;
-            });
-            __syncthreads();
-            total = s.count;
+            for (int i = threadIdx.x; i < listed; i += kThreads) f(s.list[i]);
         }
-        if (of_row || total > kCompared) {
-            uint32_t left = 0;
-            each_number(s, row, of_row, listed, [&](uint64_t e) {
-                if (e >= low && e <= high) least = std::min(least, e), most = std::max(most, e), ++left;
-            });
-            least = ~block_most(s, ~least);
-            most = block_most(s, most);
-            if (of_row) total = (uint32_t)block_sum(s, left);
-        }
-        first = false;
-        if (total <= kCompared) {
-            if (of_row) {
+    }
+
+    // The number up to which, in rising order, the numbers' weights reach `target` (which their sum does).  Their
+    // range is cut into kParts; of the part that it lies in, the range again, until each lane has one number left
+    // and can add up those below it.
+    template <typename T>
+    static __device__ __forceinline__ uint64_t find_number(Choice& s, const Row<T>& row, bool of_row, int listed, uint64_t target, const Weigh& weigh) {
+        uint64_t low = 0, high = ~0ull;  // it lies in here
+        const bool all_few = !of_row && listed <= kCompared;
+        bool first = true;
+#pragma unroll 1
+        for (;;) {
+            uint64_t least = ~0ull, most = 0;
+            uint32_t total = listed;
+            __syncthreads();
+            if (!of_row && !first) {
+                // Those that are left are put together, if they are few.
                 if (threadIdx.x == 0) s.count = 0;
                 __syncthreads();
                 each_number(s, row, of_row, listed, [&](uint64_t e) {
-                    if (e >= low && e <= high) s.active[atomicAdd(&s.count, 1u)] = e;
+                    if (e < low || e > high) return;
+                    const uint32_t at = atomicAdd(&s.count, 1u);
+                    if (at < kCompared) s.active[at] = e;
                 });
                 __syncthreads();
+                total = s.count;
             }
-            const uint64_t* const numbers = all_few ? s.list : s.active;
-            const bool mine = threadIdx.x < total;
-            const uint64_t e = mine ? numbers[threadIdx.x] : 0, w = mine ? weigh(e) : 0;
-            if (mine) s.bins[threadIdx.x] = w;
+            if (of_row || total > kCompared) {
+                uint32_t left = 0;
+                each_number(s, row, of_row, listed, [&](uint64_t e) {
+                    if (e >= low && e <= high) least = std::min(least, e), most = std::max(most, e), ++left;
+                });
+                least = ~block_most(s, ~least);
+                most = block_most(s, most);
+                if (of_row) total = (uint32_t)block_sum(s, left);
+            }
+            first = false;
+            if (total <= kCompared) {
+                if (of_row) {
+                    if (threadIdx.x == 0) s.count = 0;
+                    __syncthreads();
+                    each_number(s, row, of_row, listed, [&](uint64_t e) {
+                        if (e >= low && e <= high) s.active[atomicAdd(&s.count, 1u)] = e;
+                    });
+                    __syncthreads();
+                }
+                const uint64_t* const numbers = all_few ? s.list : s.active;
+                const bool mine = threadIdx.x < total;
+                const uint64_t e = mine ? numbers[threadIdx.x] : 0, w = mine ? weigh(e) : 0;
+                if (mine) s.bins[threadIdx.x] = w;
+                __syncthreads();
+                uint64_t below = 0;
+                if (mine) {
+#pragma unroll 8
+                    for (uint32_t i = 0; i < total; ++i) below += numbers[i] < e ? s.bins[i] : 0;
+                    if (below < target && below + w >= target) s.found = e;
+                }
+                __syncthreads();
+                return s.found;
+            }
+            const int bits = 64 - __builtin_clzll(most - least), shift = bits > kPartBits ? bits - kPartBits : 0;
+            for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
             __syncthreads();
-            uint64_t below = 0;
+            each_number(s, row, of_row, listed, [&](uint64_t e) {
+                if (e >= low && e <= high) add(&s.bins[(e - least) >> shift], weigh(e));
+            });
+            __syncthreads();
+            constexpr int kMine = (kParts + kThreads - 1) / kThreads;
+            uint64_t own[kMine], sum = 0, all;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int at = threadIdx.x * kMine + i;
+                own[i] = at < kParts ? s.bins[at] : 0;
+                sum += own[i];
+            }
+            uint64_t up = block_before(s, sum, all);
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                if (up < target && up + own[i] >= target) s.digit = threadIdx.x * kMine + i, s.before = up;
+                up += own[i];
+            }
+            __syncthreads();
+            low = least + ((uint64_t)s.digit << shift);
+            high = low + (((uint64_t)1 << shift) - 1);
+            target -= s.before;
+        }
+    }
+
+    // The cut, from the listed words, and the word that the random number falls on.
+    template <typename T>
+    static __device__ __forceinline__ void finish(Choice& s, const Params& p, int64_t r, const Row<T>& row, const Settings& set, const Plan& plan) {
+        const Way way = (Way)plan.way;
+        Weigh weigh{set.weights(p, value_of(plan.best), plan.offset), ~0ull, false, false, false};
+        const Weights& weights = weigh.weights;
+        const uint64_t need = plan.need, ahead = plan.ahead;
+        const bool few = plan.few, alone = plan.alone;
+        const bool has = (int)threadIdx.x < p.chunks;
+        int listed = alone ? 0 : (int)__hip_atomic_load(&p.plans[r].listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const bool of_row = alone || listed > p.list_size;  // no list, or one that did not hold all
+        __syncthreads();
+        if (!of_row)
+            for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = share_in(p.list + r * p.list_size + i);
+        if (has) s.chunks[threadIdx.x] = few || of_row ? 0 : share_in(p.sums + r * p.chunks + threadIdx.x);
+        __syncthreads();
+        if (few && !of_row && listed <= kRanked) {
+            // Each lane has a word, and finds by comparing it with all others its places in the order of words and by
+            // number.
+            const bool mine = (int)threadIdx.x < listed;
+            const uint64_t e = mine ? s.list[threadIdx.x] : 0;
+            const double t = mine ? weights.log2_of(value_of_entry(e)) : -2000.0;
+            uint64_t w = mine ? weights.of(t) : 0, all;
+            int rank = 0, place = 0;
             if (mine) {
 #pragma unroll 8
-                for (uint32_t i = 0; i < total; ++i) below += numbers[i] < e ? s.bins[i] : 0;
-                if (below < target && below + w >= target) s.found = e;
+                for (int i = 0; i < listed; ++i) {
+                    const uint64_t other = s.list[i];
+                    rank += other < e;
+                    place += (uint32_t)other < (uint32_t)e;
+                }
             }
+            if (rank >= (int)(ahead + need)) w = 0;  // top-k
+            if (mine) s.bins[rank] = w;
             __syncthreads();
-            return s.found;
-        }
-        const int bits = 64 - __builtin_clzll(most - least), shift = bits > kPartBits ? bits - kPartBits : 0;
-        for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
-        __syncthreads();
-        each_number(s, row, of_row, listed, [&](uint64_t e) {
-            if (e >= low && e <= high) add(&s.bins[(e - least) >> shift], weigh(e));
-        });
-        __syncthreads();
-        constexpr int kMine = (kParts + kThreads - 1) / kThreads;
-        uint64_t own[kMine], sum = 0, all;
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int at = threadIdx.x * kMine + i;
-            own[i] = at < kParts ? s.bins[at] : 0;
-            sum += own[i];
-        }
-        uint64_t up = block_before(s, sum, all);
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            if (up < target && up + own[i] >= target) s.digit = threadIdx.x * kMine + i, s.before = up;
-            up += own[i];
-        }
-        __syncthreads();
-        low = least + ((uint64_t)s.digit << shift);
-        high = low + (((uint64_t)1 << shift) - 1);
-        target -= s.before;
-    }
-}
-
-// The cut, from the listed words, and the word that the random number falls on.
-template <typename T>
-static __device__ __forceinline__ void finish(Choice& s, const Params& p, int64_t r, const Row<T>& row, const Settings& set, const Plan& plan) {
-    const Way way = (Way)plan.way;
-    Weigh weigh{set.weights(p, value_of(plan.best), plan.offset), ~0ull, false, false, false};
-    const Weights& weights = weigh.weights;
-    const uint64_t need = plan.need, ahead = plan.ahead;
-    const bool few = plan.few, alone = plan.alone;
-    const bool has = (int)threadIdx.x < p.chunks;
-    int listed = alone ? 0 : (int)__hip_atomic_load(&p.plans[r].listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool of_row = alone || listed > p.list_size;  // no list, or one that did not hold all
-    __syncthreads();
-    if (!of_row)
-        for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = share_in(p.list + r * p.list_size + i);
-    if (has) s.chunks[threadIdx.x] = few || of_row ? 0 : share_in(p.sums + r * p.chunks + threadIdx.x);
-    __syncthreads();
-    if (few && !of_row && listed <= kRanked) {
-        // Each lane has a word, and finds by comparing it with all others its places in the order of words and by
-        // number.
-        const bool mine = (int)threadIdx.x < listed;
-        const uint64_t e = mine ? s.list[threadIdx.x] : 0;
-        const double t = mine ? weights.log2_of(value_of_entry(e)) : -2000.0;
-        uint64_t w = mine ? weights.of(t) : 0, all;
-        int rank = 0, place = 0;
-        if (mine) {
-#pragma unroll 8
-            for (int i = 0; i < listed; ++i) {
-                const uint64_t other = s.list[i];
-                rank += other < e;
-                place += (uint32_t)other < (uint32_t)e;
-            }
-        }
-        if (rank >= (int)(ahead + need)) w = 0;  // top-k
-        if (mine) s.bins[rank] = w;
-        __syncthreads();
-        const uint64_t ordered = mine ? s.bins[threadIdx.x] : 0, before = block_before(s, ordered, all);
-        if (mine) s.active[threadIdx.x] = before;
-        __syncthreads();
-        // A word stays for top-p while those before it do not weigh enough.
-        if (mine && (t < weights.low || (set.top_p < 1.0f && s.active[rank] >= share_of(set.top_p, all)))) w = 0;
-        if (mine) s.bins[place] = w;
-        __syncthreads();
-        const uint64_t placed = mine ? s.bins[threadIdx.x] : 0, up = block_before(s, placed, all), goal = set.goal(all);
-        if (mine) s.active[threadIdx.x] = up;
-        __syncthreads();
-        if (mine && s.active[place] <= goal && goal < s.active[place] + w) {
-            gbl(p.c.token)[r] = (int)(uint32_t)e;
-            if (p.c.share) gbl(p.c.share)[r] = (float)((double)w / (double)all);
-        }
-        return;
-    }
-    // The searches: the last word that stays, by number for top-k and by weight for top-p; where all words that stay
-    // are listed, then the word that the random number falls on, in the order of words.
-    const bool complete = few || of_row;  // the list, or the row, holds what lies ahead of the cut's bin too
-    uint64_t total = 0;
-#pragma unroll 1
-    for (int search = 0; search < 3; ++search) {
-        uint64_t target;
-        if (search == 0) {
-            if (way != kCount) continue;
-            weigh.ones = true;
-            target = complete ? ahead + need : need;
-        } else if (search == 1) {
-            if (way == kMinP || set.top_p >= 1.0f) continue;
-            weigh.ones = false;
-            uint64_t sum = 0;
-            each_number(s, row, of_row, listed, [&](uint64_t e) { sum += weigh(e); });
-            sum = block_sum(s, sum);
-            target = complete ? share_of(set.top_p, sum) : std::min(need, sum);
-            if (target == 0) continue;  // words too light to weigh anything: it does not matter which stay
-        } else {
-            weigh.ones = false, weigh.min_p = true;
-            if (!few || of_row) continue;
-            uint64_t sum = 0;
-            each_number(s, row, of_row, listed, [&](uint64_t e) { sum += weigh(e); });
-            total = block_sum(s, sum);
-            target = set.goal(total) + 1;
-            for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = turned(s.list[i]);
-            weigh.by_word = true;
-        }
-        const uint64_t found = find_number(s, row, of_row, listed, target, weigh);
-        if (search < 2) {
-            weigh.last = found;
-        } else {
-            if (threadIdx.x == 0) {
-                gbl(p.c.token)[r] = (int)(found >> 32);
-                if (p.c.share) gbl(p.c.share)[r] = (float)((double)weigh(found) / (double)total);
+            const uint64_t ordered = mine ? s.bins[threadIdx.x] : 0, before = block_before(s, ordered, all);
+            if (mine) s.active[threadIdx.x] = before;
+            __syncthreads();
+            // A word stays for top-p while those before it do not weigh enough.
+            if (mine && (t < weights.low || (set.top_p < 1.0f && s.active[rank] >= share_of(set.top_p, all)))) w = 0;
+            if (mine) s.bins[place] = w;
+            __syncthreads();
+            const uint64_t placed = mine ? s.bins[threadIdx.x] : 0, up = block_before(s, placed, all), goal = set.goal(all);
+            if (mine) s.active[threadIdx.x] = up;
+            __syncthreads();
+            if (mine && s.active[place] <= goal && goal < s.active[place] + w) {
+                gbl(p.c.token)[r] = (int)(uint32_t)e;
+                if (p.c.share) gbl(p.c.share)[r] = (float)((double)w / (double)all);
             }
             return;
         }
-    }
-    // The chunks' weights, those of the list among them, and the chunk that the random number falls into.
-    if (of_row) {
+        // The searches: the last word that stays, by number for top-k and by weight for top-p; where all words that stay
+        // are listed, then the word that the random number falls on, in the order of words.
+        const bool complete = few || of_row;  // the list, or the row, holds what lies ahead of the cut's bin too
+        uint64_t total = 0;
 #pragma unroll 1
-        for (int c = 0; c < p.chunks; ++c) {
-            uint64_t sum = 0;
-            row.each(c * kVectors<T>, min((c + 1) * kVectors<T>, row.vectors), [&](float v, int w) { sum += weigh(entry_of(key_of(v), w)); });
-            if (sum) add(&s.chunks[c], sum);
-        }
-    } else {
-        // (Lanes add to sums of their own where there is room, not to wait for each other.)
-        const int copies = min(8, kParts / p.chunks), copy = threadIdx.x % copies * p.chunks;
-        __syncthreads();
-        for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
-        __syncthreads();
-#pragma unroll 1
-        for (int i = threadIdx.x; i < listed; i += kThreads) {
-            const uint64_t w = weigh(s.list[i]);
-            if (w) add(&s.bins[copy + row.chunk_of((int)(uint32_t)s.list[i])], w);
-        }
-        __syncthreads();
-        if (has)
-            for (int i = 0; i < copies; ++i) s.chunks[threadIdx.x] += s.bins[i * p.chunks + threadIdx.x];
-    }
-    __syncthreads();
-    const uint64_t mine = has ? s.chunks[threadIdx.x] : 0, up = block_before(s, mine, total), goal = set.goal(total);
-    if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = up;
-    __syncthreads();
-    const int target = (int)s.digit;
-    const uint64_t within = goal - s.before;
-    choose_in_chunk(s, p, r, row, target, within, (double)total, [&](float v, int w) { return weigh(entry_of(key_of(v), w)); });
-}
-
-// Lists a chunk's words that may be the cut (all that may stay, where they are few), and sums the weights of those
-// that surely stay.
-template <typename T>
-static __device__ __forceinline__ void list_chunk(Listing& s, const Params& p, int64_t r, int chunk, const Row<T>& row, Chunk<T>& x, const Settings& set, const Plan& plan) {
-    const Way way = (Way)plan.way;
-    const Weights weights = set.weights(p, value_of(plan.best), plan.offset);
-    const float reference = plan.reference;
-    const int cut_bin = plan.cut_bin;
-    const bool few = plan.few;
-    uint32_t* const listed = &p.plans[r].listed;
-    if (threadIdx.x == 0) s.count = 0;
-    __syncthreads();
-    x.take(row);
-    uint64_t sum = 0;
-    if (way == kWeight && set.min_p == 0.0f) {
-        // Survey's histogram has the weights of the bins ahead of the cut's.
-        const Record& record = p.records[r * p.chunks + chunk];
-        const int over = (int)fmin(plan.offset - record.offset, 63.0);
-        const uint64_t* const bins = p.bins + (r * p.chunks + chunk) * kBins;
-        for (int i = record.low + threadIdx.x; i < min(record.high, cut_bin); i += kThreads) sum += gbl(bins)[i];
-        sum = block_sum(s, sum) >> (weights.infinite && record.key != kInfinity ? 63 : over);
-        sum = threadIdx.x == 0 ? sum : 0;
-    } else if (!few) {
-        x.each(row, [&](float v, int) {
-            const double t = weights.log2_of(v);
-            const uint64_t w = weights.of(t);
-            sum += t >= weights.low && (way == kMinP || bin_of(v, reference) < cut_bin) ? w : 0;
-        });
-    }
-    if (way != kMinP) {
-        x.each(row, [&](float v, int w) {
-            const int bin = v > -INFINITY ? bin_of(v, reference) : kBins;
-            if (bin == cut_bin || (few && bin < cut_bin)) {
-                const uint64_t e = entry_of(key_of(v), w);
-                const uint32_t at = atomicAdd(&s.count, 1u);
-                if (at < kStaged) {
-                    s.staged[at] = e;
-                } else {
-                    const uint32_t to = atomicAdd(listed, 1u);
-                    if (to < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + to, e);
-                }
+        for (int search = 0; search < 3; ++search) {
+            uint64_t target;
+            if (search == 0) {
+                if (way != kCount) continue;
+                weigh.ones = true;
+                target = complete ? ahead + need : need;
+            } else if (search == 1) {
+                if (way == kMinP || set.top_p >= 1.0f) continue;
+                weigh.ones = false;
+                uint64_t sum = 0;
+                each_number(s, row, of_row, listed, [&](uint64_t e) { sum += weigh(e); });
+                sum = block_sum(s, sum);
+                target = complete ? share_of(set.top_p, sum) : std::min(need, sum);
+                if (target == 0) continue;  // words too light to weigh anything: it does not matter which stay
+            } else {
+                weigh.ones = false, weigh.min_p = true;
+                if (!few || of_row) continue;
+                uint64_t sum = 0;
+                each_number(s, row, of_row, listed, [&](uint64_t e) { sum += weigh(e); });
+                total = block_sum(s, sum);
+                target = set.goal(total) + 1;
+                for (int i = threadIdx.x; i < listed; i += kThreads) s.list[i] = turned(s.list[i]);
+                weigh.by_word = true;
             }
-        });
-    }
-    if (!few) {
-        sum = block_sum(s, sum);
-        if (threadIdx.x == 0) share_out(p.sums + r * p.chunks + chunk, sum);
-    }
-    __syncthreads();
-    const uint32_t count = std::min<uint32_t>(s.count, kStaged);
-    if (threadIdx.x == 0 && count) s.base = atomicAdd(listed, count);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < count; i += kThreads)
-        if (s.base + i < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + s.base + i, s.staged[i]);
-}
-
-// Few rows: a chunk's workgroup makes the row's plan for itself, and the last one of the row to be done goes on.
-template <typename T>
-static __device__ __forceinline__ void choose(const Params& p) {
-    __shared__ struct {
-        Listing listing;
-        Choice choice;
-    } s;
-    const int64_t r = blockIdx.x;
-    const int chunk = blockIdx.y;
-    const Row<T> row(p, r);
-    begin(s.listing);
-    begin(s.choice);
-    Chunk<T> x(row, chunk);
-    const Settings set(p, r);
-    const Plan made = plan(s.choice, p, r, row, set, chunk == 0);
-    if (made.way == kDone || (made.alone && chunk != 0)) return;
-    if (!made.alone) {
-        list_chunk(s.listing, p, r, chunk, row, x, set, made);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave shares has arrived
+            const uint64_t found = find_number(s, row, of_row, listed, target, weigh);
+            if (search < 2) {
+                weigh.last = found;
+            } else {
+                if (threadIdx.x == 0) {
+                    gbl(p.c.token)[r] = (int)(found >> 32);
+                    if (p.c.share) gbl(p.c.share)[r] = (float)((double)weigh(found) / (double)total);
+                }
+                return;
+            }
+        }
+        // The chunks' weights, those of the list among them, and the chunk that the random number falls into.
+        if (of_row) {
+#pragma unroll 1
+            for (int c = 0; c < p.chunks; ++c) {
+                uint64_t sum = 0;
+                row.each(c * kVectors<T>, min((c + 1) * kVectors<T>, row.vectors), [&](float v, int w) { sum += weigh(entry_of(key_of(v), w)); });
+                if (sum) add(&s.chunks[c], sum);
+            }
+        } else {
+            // (Lanes add to sums of their own where there is room, not to wait for each other.)
+            const int copies = min(8, kParts / p.chunks), copy = threadIdx.x % copies * p.chunks;
+            __syncthreads();
+            for (int i = threadIdx.x; i < kParts; i += kThreads) s.bins[i] = 0;
+            __syncthreads();
+#pragma unroll 1
+            for (int i = threadIdx.x; i < listed; i += kThreads) {
+                const uint64_t w = weigh(s.list[i]);
+                if (w) add(&s.bins[copy + row.chunk_of((int)(uint32_t)s.list[i])], w);
+            }
+            __syncthreads();
+            if (has)
+                for (int i = 0; i < copies; ++i) s.chunks[threadIdx.x] += s.bins[i * p.chunks + threadIdx.x];
+        }
         __syncthreads();
-        if (threadIdx.x == 0) s.listing.digit = __hip_atomic_fetch_add(&p.plans[r].done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)p.chunks;
+        const uint64_t mine = has ? s.chunks[threadIdx.x] : 0, up = block_before(s, mine, total), goal = set.goal(total);
+        if (up <= goal && goal < up + mine) s.digit = threadIdx.x, s.before = up;
         __syncthreads();
-        if (!s.listing.digit) return;
-        asm volatile("" ::: "memory");
+        const int target = (int)s.digit;
+        const uint64_t within = goal - s.before;
+        choose_in_chunk(s, p, r, row, target, within, (double)total, [&](float v, int w) { return weigh(entry_of(key_of(v), w)); });
     }
-    finish(s.choice, p, r, row, set, made);
-}
 
-// Many rows: a launch each.
-template <typename T>
-static __device__ __forceinline__ void list_chunks(const Params& p) {
-    __shared__ Listing s;
-    const int64_t r = blockIdx.x;
-    const Plan& made = p.plans[r];
-    if (made.way == kDone || made.alone) return;
-    begin(s);
-    const Row<T> row(p, r);
-    Chunk<T> x(row, blockIdx.y);
-    list_chunk(s, p, r, blockIdx.y, row, x, Settings(p, r), made);
-}
-template <typename T>
-static __device__ __forceinline__ void finish_rows(const Params& p) {
-    __shared__ Choice s;
-    const int64_t r = blockIdx.x;
-    const Plan& made = p.plans[r];
-    if (made.way == kDone) return;
-    begin(s);
-    finish(s, p, r, Row<T>(p, r), Settings(p, r), made);
-}
+    // Lists a chunk's words that may be the cut (all that may stay, where they are few), and sums the weights of those
+    // that surely stay.
+    template <typename T>
+    static __device__ __forceinline__ void list_chunk(Listing& s, const Params& p, int64_t r, int chunk, const Row<T>& row, Chunk<T>& x, const Settings& set, const Plan& plan) {
+        const Way way = (Way)plan.way;
+        const Weights weights = set.weights(p, value_of(plan.best), plan.offset);
+        const float reference = plan.reference;
+        const int cut_bin = plan.cut_bin;
+        const bool few = plan.few;
+        uint32_t* const listed = &p.plans[r].listed;
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        x.take(row);
+        uint64_t sum = 0;
+        if (way == kWeight && set.min_p == 0.0f) {
+            // Survey's histogram has the weights of the bins ahead of the cut's.
+            const Record& record = p.records[r * p.chunks + chunk];
+            const int over = (int)fmin(plan.offset - record.offset, 63.0);
+            const uint64_t* const bins = p.bins + (r * p.chunks + chunk) * kBins;
+            for (int i = record.low + threadIdx.x; i < min(record.high, cut_bin); i += kThreads) sum += gbl(bins)[i];
+            sum = block_sum(s, sum) >> (weights.infinite && record.key != kInfinity ? 63 : over);
+            sum = threadIdx.x == 0 ? sum : 0;
+        } else if (!few) {
+            x.each(row, [&](float v, int) {
+                const double t = weights.log2_of(v);
+                const uint64_t w = weights.of(t);
+                sum += t >= weights.low && (way == kMinP || bin_of(v, reference) < cut_bin) ? w : 0;
+            });
+        }
+        if (way != kMinP) {
+            x.each(row, [&](float v, int w) {
+                const int bin = v > -INFINITY ? bin_of(v, reference) : kBins;
+                if (bin == cut_bin || (few && bin < cut_bin)) {
+                    const uint64_t e = entry_of(key_of(v), w);
+                    const uint32_t at = atomicAdd(&s.count, 1u);
+                    if (at < kStaged) {
+                        s.staged[at] = e;
+                    } else {
+                        const uint32_t to = atomicAdd(listed, 1u);
+                        if (to < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + to, e);
+                    }
+                }
+            });
+        }
+        if (!few) {
+            sum = block_sum(s, sum);
+            if (threadIdx.x == 0) share_out(p.sums + r * p.chunks + chunk, sum);
+        }
+        __syncthreads();
+        const uint32_t count = std::min<uint32_t>(s.count, kStaged);
+        if (threadIdx.x == 0 && count) s.base = atomicAdd(listed, count);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < count; i += kThreads)
+            if (s.base + i < (uint32_t)p.list_size) share_out(p.list + r * p.list_size + s.base + i, s.staged[i]);
+    }
+
+    // Few rows: a chunk's workgroup makes the row's plan for itself, and the last one of the row to be done goes on.
+    template <typename T>
+    static __device__ __forceinline__ void choose(const Params& p) {
+        __shared__ struct {
+            Listing listing;
+            Choice choice;
+        } s;
+        const int64_t r = blockIdx.x;
+        const int chunk = blockIdx.y;
+        const Row<T> row(p, r);
+        begin(s.listing);
+        begin(s.choice);
+        Chunk<T> x(row, chunk);
+        const Settings set(p, r);
+        const Plan made = plan(s.choice, p, r, row, set, chunk == 0);
+        if (made.way == kDone || (made.alone && chunk != 0)) return;
+        if (!made.alone) {
+            list_chunk(s.listing, p, r, chunk, row, x, set, made);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave shares has arrived
+            __syncthreads();
+            if (threadIdx.x == 0) s.listing.digit = __hip_atomic_fetch_add(&p.plans[r].done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)p.chunks;
+            __syncthreads();
+            if (!s.listing.digit) return;
+            asm volatile("" ::: "memory");
+        }
+        finish(s.choice, p, r, row, set, made);
+    }
+
+    // Many rows: a launch each.
+    template <typename T>
+    static __device__ __forceinline__ void list_chunks(const Params& p) {
+        __shared__ Listing s;
+        const int64_t r = blockIdx.x;
+        const Plan& made = p.plans[r];
+        if (made.way == kDone || made.alone) return;
+        begin(s);
+        const Row<T> row(p, r);
+        Chunk<T> x(row, blockIdx.y);
+        list_chunk(s, p, r, blockIdx.y, row, x, Settings(p, r), made);
+    }
+    template <typename T>
+    static __device__ __forceinline__ void finish_rows(const Params& p) {
+        __shared__ Choice s;
+        const int64_t r = blockIdx.x;
+        const Plan& made = p.plans[r];
+        if (made.way == kDone) return;
+        begin(s);
+        finish(s, p, r, Row<T>(p, r), Settings(p, r), made);
+    }
 };
 
 template <typename T, int THREADS>

@@ -172,3 +172,12 @@ def test_captured_and_replayed():
         token.fill_(-9)
         step()
         assert torch.equal(kept[0], token) and torch.equal(kept[1], share) and int(token.min()) >= 0
+
+
+@pytest.mark.parametrize("vocab,options", [
+    (262144, [dict(top_p=0.95, temperature=2.0), dict(top_p=0.9), dict(top_k=50, top_p=0.95), dict(top_k=30000, min_p=0.001)]),
+    (1 << 20, [dict(top_p=0.95, temperature=2.0), dict(top_k=200, temperature=0.9)])])
+def test_the_largest_vocabularies(vocab, options):
+    """Up to the largest that there may be; cuts in bins of more words than a list holds among them."""
+    rng = np.random.default_rng(vocab)
+    compare(normal(rng, len(options), vocab, torch.float32), options, 9, rng)
